@@ -7,7 +7,8 @@
  *
  *     X  = encode(x, labels)             tfm_encode_fwd   (+ tfm_thinking_rows_fwd)
  *     Y  = blocks(X)                     tfm_layer_fwd per block
- *     loss, dY, decoder grads            tfm_decode_loss
+ *     loss, dY, decoder grads            tfm_decode_loss  (or tfm_decode_fwd, a loss on the logits
+ *                                        such as tfm_vocab.h's, and tfm_decode_bwd)
  *     dX, block grads                    tfm_layer_bwd per block
  *     encoder grads                      tfm_encode_bwd   (+ tfm_thinking_rows_bwd)
  *
@@ -40,8 +41,8 @@
  *   - params, grads: device float32, one packed vector of tfm_ends_param_count() floats:
  *         W_fe[E][G] b_fe[E] W_te[E] b_te[E]          encoders
  *         W_d1[Hd][E] b_d1[Hd] W_d2[K][Hd] b_d2[K]     decoder
- *     tfm_encode_bwd writes the encoder entries of grads, tfm_decode_loss the decoder entries;
- *     neither touches the other's.  accumulate != 0 adds to grads instead of overwriting.
+ *     tfm_encode_bwd writes the encoder entries of grads, tfm_decode_loss and tfm_decode_bwd the
+ *     decoder entries; neither touches the other's.  accumulate != 0 adds to grads instead of overwriting.
  *   - workspace: device scratch of tfm_ends_workspace_bytes(); contents are not preserved.
  *   - Parameter gradients and the loss are reduced in a fixed order (bitwise reproducible).
  *   - All device pointers must be non-null and 16-byte aligned; the caller owns every buffer,
@@ -107,6 +108,15 @@ int tfm_decode_loss(const tfm_dims* dims, const tfm_ends* ends, const int32_t* n
                     const void* Y, const float* params, float* loss, float* logits, void* dY,
                     float* grads, int accumulate, void* workspace, size_t workspace_bytes,
                     void* stream);
+
+/* Decoder backward for a given gradient of its logits: dlogits, device float32 [T_test][K] in the
+ * row order of tfm_decode_fwd's logits, gives dY and the decoder entries of grads as
+ * tfm_decode_loss gives them for its own loss.  n_train[b] in [0, R] as for tfm_decode_fwd.  The
+ * decoder's hidden layer is formed again from Y; dlogits is only read. */
+int tfm_decode_bwd(const tfm_dims* dims, const tfm_ends* ends, const int32_t* n_train,
+                   const int32_t* n_feat, const void* Y, const float* params,
+                   const float* dlogits, void* dY, float* grads, int accumulate, void* workspace,
+                   size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -165,3 +165,28 @@ def decode_loss(Y, y, n_train, n_feat, n_class, C, P, mode):
             dY[b, n:, :m] = dZ[row:row + cnt][:, None, :] / m
         row += cnt
     return loss, dY, dP, logits
+
+
+def decode_logits(Y, n_train, n_feat, C, P, mode):
+    """Logits of every test row, in (dataset, row) order."""
+    Z = decode_tokens(np.asarray(Y, dtype=np.float64), n_train, n_feat, C, mode)
+    return gelu(Z @ P["W_d1"].T + P["b_d1"]) @ P["W_d2"].T + P["b_d2"]
+
+
+def decode_backward(Y, n_train, n_feat, C, P, mode, dlog):
+    """Gradients (dY, dP) of sum(dlog * decode_logits) for a given dlog."""
+    Y = np.asarray(Y, dtype=np.float64)
+    Z = decode_tokens(Y, n_train, n_feat, C, mode)
+    h = Z @ P["W_d1"].T + P["b_d1"]
+    dh = gelu_grad(h) * (dlog @ P["W_d2"])
+    dP = {"W_d2": dlog.T @ gelu(h), "b_d2": dlog.sum(0), "W_d1": dh.T @ Z, "b_d1": dh.sum(0)}
+    dZ = dh @ P["W_d1"]
+    dY = np.zeros_like(Y)
+    cells = [slice(C, C + 1) if mode == "target" else slice(0, int(m)) for m in n_feat]
+    at = 0
+    for b, n in enumerate(n_train):
+        rows = Y.shape[1] - int(n)
+        width = cells[b].stop - cells[b].start
+        dY[b, int(n):, cells[b]] = dZ[at:at + rows, None] / width
+        at += rows
+    return dY, dP

@@ -177,9 +177,9 @@ int common(const tfm_dims* dims, const tfm_ends* ends, void* workspace, size_t w
   return TFM_OK;
 }
 
-// Decoder forward: Z, H1 = Z W1^T + b1, A1 = GELU(H1), logits = A1 W2^T + b2.
-int decoder_forward(const Shape& s, const EndsGeo& g, const void* Y, const float* prm,
-                    float* logits, char* ws, const Ws& W, hipStream_t st) {
+// Decoder's hidden layer: Z, H1 = Z W1^T + b1, A1 = GELU(H1).
+int decoder_hidden(const Shape& s, const EndsGeo& g, const void* Y, const float* prm, char* ws,
+                   const Ws& W, hipStream_t st) {
   const Offsets o = param_offsets(s);
   float* Z = (float*)(ws + W.Z);
   if (s.dtype == TFM_BF16)
@@ -193,6 +193,15 @@ int decoder_forward(const Shape& s, const EndsGeo& g, const void* Y, const float
   a.bias = prm + o.bd1;
   a.M = (int)g.Ttot; a.N = s.Hd; a.K = s.E;
   STEP("dec_hidden/mfma", tfm::launch_sgemm(a, false, true, tfm::SG_GELU, st));
+  return TFM_OK;
+}
+
+// Decoder forward: the hidden layer, logits = A1 W2^T + b2.
+int decoder_forward(const Shape& s, const EndsGeo& g, const void* Y, const float* prm,
+                    float* logits, char* ws, const Ws& W, hipStream_t st) {
+  const int rc = decoder_hidden(s, g, Y, prm, ws, W, st);
+  if (rc) return rc;
+  const Offsets o = param_offsets(s);
   tfm::SgemmArgs b{};
   b.A = (const float*)(ws + W.A1); b.lda = s.Hd;
   b.B = prm + o.Wd2; b.ldb = s.Hd;
@@ -224,6 +233,61 @@ int column_sums(const float* A, int64_t lda, int N, int64_t rows, float* part, f
   STEP("dec_bgrad/hbm", tfm::launch_colsum(rows, N, A, lda, kColChunk, part, st));
   STEP("dec_bgrad_reduce/hbm", tfm::launch_reduce_z(nz, N, N, part, out, accumulate, st));
   return TFM_OK;
+}
+
+// dY and the decoder's gradients where no row is decoded: zeros.
+int decoder_zero(const Shape& s, const EndsGeo& g, void* dY, float* grads, int accumulate, char* ws,
+                 const Ws& W, hipStream_t st) {
+  const Offsets o = param_offsets(s);
+  float* DZ = (float*)(ws + W.DZ);
+  if (s.dtype == TFM_BF16)
+    STEP("dec_scatter/hbm", tfm::launch_decode_scatter(g, DZ, (tfm::bf16*)dY, st));
+  else
+    STEP("dec_scatter/hbm", tfm::launch_decode_scatter(g, DZ, (float*)dY, st));
+  if (!accumulate)
+    STEP("dec_zero/hbm", tfm::launch_fill_f32(grads + o.Wd1, (int64_t)(o.total - o.Wd1), 0.f, st));
+  return TFM_OK;
+}
+
+// Decoder backward from the logits' gradient DL and the hidden layer in the workspace: dY and the
+// decoder's gradients.
+int decoder_backward(const Shape& s, const EndsGeo& g, const float* DL, const float* params,
+                     void* dY, float* grads, int accumulate, char* ws, const Ws& W,
+                     hipStream_t st) {
+  const Offsets o = param_offsets(s);
+  const int64_t T = g.Ttot;
+  float* DZ = (float*)(ws + W.DZ);
+  // dH1 = (dL W2) * GELU'(H1)
+  tfm::SgemmArgs a{};
+  a.A = DL; a.lda = s.K;
+  a.B = params + o.Wd2; a.ldb = s.Hd;
+  a.C = (float*)(ws + W.DH1); a.ldc = s.Hd;
+  a.aux = (const float*)(ws + W.H1);
+  a.M = (int)T; a.N = s.Hd; a.K = s.K;
+  STEP("dec_dhidden/mfma", tfm::launch_sgemm(a, false, false, tfm::SG_GELU_GRAD, st));
+  // dZ = dH1 W1
+  tfm::SgemmArgs b{};
+  b.A = (const float*)(ws + W.DH1); b.lda = s.Hd;
+  b.B = params + o.Wd1; b.ldb = s.E;
+  b.C = DZ; b.ldc = s.E;
+  b.M = (int)T; b.N = s.E; b.K = s.Hd;
+  STEP("dec_dinput/mfma", tfm::launch_sgemm(b, false, false, tfm::SG_BIAS, st));
+  if (s.dtype == TFM_BF16)
+    STEP("dec_scatter/hbm", tfm::launch_decode_scatter(g, DZ, (tfm::bf16*)dY, st));
+  else
+    STEP("dec_scatter/hbm", tfm::launch_decode_scatter(g, DZ, (float*)dY, st));
+  float* wpart = (float*)(ws + W.wpart);
+  float* bpart = (float*)(ws + W.bpart);
+  int rc = row_contraction((const float*)(ws + W.DH1), s.Hd, (const float*)(ws + W.Z), s.E, s.Hd,
+                           s.E, T, wpart, grads + o.Wd1, accumulate, st);
+  if (rc) return rc;
+  rc = column_sums((const float*)(ws + W.DH1), s.Hd, s.Hd, T, bpart, grads + o.bd1, accumulate,
+                   st);
+  if (rc) return rc;
+  rc = row_contraction(DL, s.K, (const float*)(ws + W.A1), s.Hd, s.K, s.Hd, T, wpart,
+                       grads + o.Wd2, accumulate, st);
+  if (rc) return rc;
+  return column_sums(DL, s.K, s.K, T, bpart, grads + o.bd2, accumulate, st);
 }
 
 }  // namespace
@@ -326,19 +390,11 @@ int tfm_decode_loss(const tfm_dims* dims, const tfm_ends* ends, const int32_t* n
   EndsGeo g;
   rc = setup(s, n_train, n_feat, n_class, ws, W, g, st);
   if (rc) return rc;
-  const Offsets o = param_offsets(s);
   const int64_t T = g.Ttot;
-  float* DZ = (float*)(ws + W.DZ);
   if (T == 0) {
     // No unlabelled rows: zero loss, zero dY, zero decoder gradients.
     STEP("dec_loss/hbm", tfm::launch_fill_f32(loss, 1, 0.f, st));
-    if (s.dtype == TFM_BF16)
-      STEP("dec_scatter/hbm", tfm::launch_decode_scatter(g, DZ, (tfm::bf16*)dY, st));
-    else
-      STEP("dec_scatter/hbm", tfm::launch_decode_scatter(g, DZ, (float*)dY, st));
-    if (!accumulate)
-      STEP("dec_zero/hbm", tfm::launch_fill_f32(grads + o.Wd1, (int64_t)(o.total - o.Wd1), 0.f, st));
-    return TFM_OK;
+    return decoder_zero(s, g, dY, grads, accumulate, ws, W, st);
   }
   float* LG = logits ? logits : (float*)(ws + W.LG);
   rc = decoder_forward(s, g, Y, params, LG, ws, W, st);
@@ -347,37 +403,29 @@ int tfm_decode_loss(const tfm_dims* dims, const tfm_ends* ends, const int32_t* n
   float* LROW = (float*)(ws + W.LROW);
   STEP("dec_xent/valu", tfm::launch_cross_entropy(g, LG, labels, LROW, DL, st));
   STEP("dec_loss/hbm", tfm::launch_reduce_z((int)T, 1, 1, LROW, loss, 0, st));
-  // dH1 = (dL W2) * GELU'(H1)
-  tfm::SgemmArgs a{};
-  a.A = DL; a.lda = s.K;
-  a.B = params + o.Wd2; a.ldb = s.Hd;
-  a.C = (float*)(ws + W.DH1); a.ldc = s.Hd;
-  a.aux = (const float*)(ws + W.H1);
-  a.M = (int)T; a.N = s.Hd; a.K = s.K;
-  STEP("dec_dhidden/mfma", tfm::launch_sgemm(a, false, false, tfm::SG_GELU_GRAD, st));
-  // dZ = dH1 W1
-  tfm::SgemmArgs b{};
-  b.A = (const float*)(ws + W.DH1); b.lda = s.Hd;
-  b.B = params + o.Wd1; b.ldb = s.E;
-  b.C = DZ; b.ldc = s.E;
-  b.M = (int)T; b.N = s.E; b.K = s.Hd;
-  STEP("dec_dinput/mfma", tfm::launch_sgemm(b, false, false, tfm::SG_BIAS, st));
-  if (s.dtype == TFM_BF16)
-    STEP("dec_scatter/hbm", tfm::launch_decode_scatter(g, DZ, (tfm::bf16*)dY, st));
-  else
-    STEP("dec_scatter/hbm", tfm::launch_decode_scatter(g, DZ, (float*)dY, st));
-  float* wpart = (float*)(ws + W.wpart);
-  float* bpart = (float*)(ws + W.bpart);
-  rc = row_contraction((const float*)(ws + W.DH1), s.Hd, (const float*)(ws + W.Z), s.E, s.Hd,
-                       s.E, T, wpart, grads + o.Wd1, accumulate, st);
+  return decoder_backward(s, g, DL, params, dY, grads, accumulate, ws, W, st);
+}
+
+int tfm_decode_bwd(const tfm_dims* dims, const tfm_ends* ends, const int32_t* n_train,
+                   const int32_t* n_feat, const void* Y, const float* params,
+                   const float* dlogits, void* dY, float* grads, int accumulate, void* workspace,
+                   size_t workspace_bytes, void* stream) {
+  Shape s;
+  Ws W;
+  int rc = common(dims, ends, workspace, workspace_bytes, s, W);
   if (rc) return rc;
-  rc = column_sums((const float*)(ws + W.DH1), s.Hd, s.Hd, T, bpart, grads + o.bd1, accumulate,
-                   st);
+  if (!aligned(Y) || !aligned(params) || !aligned(dlogits) || !aligned(dY) || !aligned(grads))
+    return fail(TFM_ERR_POINTER, "Y, params, dlogits, dY and grads must be non-null and 16-byte "
+                                 "aligned");
+  hipStream_t st = (hipStream_t)stream;
+  char* ws = (char*)workspace;
+  EndsGeo g;
+  rc = setup(s, n_train, n_feat, nullptr, ws, W, g, st, 0);
   if (rc) return rc;
-  rc = row_contraction(DL, s.K, (const float*)(ws + W.A1), s.Hd, s.K, s.Hd, T, wpart,
-                       grads + o.Wd2, accumulate, st);
+  if (g.Ttot == 0) return decoder_zero(s, g, dY, grads, accumulate, ws, W, st);
+  rc = decoder_hidden(s, g, Y, params, ws, W, st);
   if (rc) return rc;
-  return column_sums(DL, s.K, s.K, T, bpart, grads + o.bd2, accumulate, st);
+  return decoder_backward(s, g, dlogits, params, dY, grads, accumulate, ws, W, st);
 }
 
 }  // extern "C"

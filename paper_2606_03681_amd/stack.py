@@ -157,14 +157,33 @@ class InferStack:
         return h
 
 
+def cat_embed(dims, T, cat_cols, V, scale):
+    """The embedding of the first cat_cols feature cells of the data rows of a stack input (ids
+    [B, R-T, cat_cols] into a float32 table of V rows), and the element of the stack input at which
+    its rows start."""
+    S = dims.C + 1
+    if not 1 <= cat_cols <= dims.C:
+        raise ValueError(f"{cat_cols} categorical columns of {dims.C} feature cells")
+    e = tfm.make_embed((dims.B, dims.R - T, cat_cols), (dims.R * S * dims.E, S * dims.E, dims.E),
+                       dims.E, V, dims.dtype, tfm.TFM_F32, scale)
+    return e, T * S * dims.E
+
+
 class TrainStep:
     """One training step through the whole model: the encoders build the stack input (and the
     thinking-row table fills its first T rows), the stack runs forward, the decoder computes the
     loss and the gradient of the stack output, the stack runs backward and the encoders (and the
-    table) receive their gradients.  Allocation and call order only."""
+    table) receive their gradients.  Allocation and call order only.
+
+    cat_table: float32 [V, E], for tables whose first cat_cols feature columns are categorical:
+    cat_scale times the row of each cell's id is added to the encoders' output (give such columns
+    the value 0 in x), and cat_grad receives its gradient.
+    distill: dict(k=..., temperature=..., alpha=..., tail=...) takes the loss from a teacher's top
+    k logits per unlabelled row (tfm_distill_loss) in place of the labels' cross entropy."""
 
     def __init__(self, dims, ends, n_train, n_feat, n_class, params, ends_params, table=None,
-                 device="cuda", decay_base=0.95):
+                 device="cuda", decay_base=0.95, cat_table=None, cat_cols=0, cat_scale=1.0,
+                 distill=None):
         self.dims, self.ends = dims, ends
         self.n_train = np.ascontiguousarray(n_train, dtype=np.int32)
         self.n_feat = np.ascontiguousarray(n_feat, dtype=np.int32)
@@ -193,21 +212,72 @@ class TrainStep:
         self.loss = torch.empty(4, dtype=torch.float32, device=device)
         self.ends_grads = torch.empty_like(self.ends_params)
         self.Y = self.dX = None
+        self.cat_table = self.distill = None
+        if cat_table is not None:
+            self.cat_table = cat_table if isinstance(cat_table, torch.Tensor) else \
+                torch.from_numpy(np.ascontiguousarray(cat_table, dtype=np.float32)).to(device)
+            self.cat, self.cat_at = cat_embed(dims, self.T, cat_cols, self.cat_table.shape[0],
+                                              cat_scale)
+            self.cat_grad = torch.empty_like(self.cat_table)
+            self.cat_ws = torch.empty(tfm.embed_workspace_bytes(self.cat), dtype=torch.uint8,
+                                      device=device)
+        if distill is not None:
+            rows = dims.R - self.n_train
+            N, K = int(rows.sum()), ends.K
+            self.distill = tfm.make_distill(N, K, distill["k"], K, tfm.TFM_F32,
+                                            distill.get("temperature", 1.0),
+                                            distill.get("alpha", 1.0), distill.get("tail", 0))
+            nb = tfm.distill_workspace_bytes(self.distill)
+            if nb == 0:
+                raise tfm.TfmError(-1, tfm.last_error())
+            self.distill_ws = torch.empty(nb, dtype=torch.uint8, device=device)
+            self.logits = torch.empty((max(N, 1), K), dtype=torch.float32, device=device)
+            self.dlogits = torch.empty_like(self.logits)
+            self.row_class = torch.from_numpy(np.repeat(self.n_class, rows)).to(device)
+            # the unlabelled rows among the data rows [B, R-T]
+            self.test_rows = torch.from_numpy(np.concatenate(
+                [b * (dims.R - self.T) + np.arange(n - self.T, dims.R - self.T)
+                 for b, n in enumerate(self.n_train)]).astype(np.int64)).to(device)
 
-    def run(self, x, labels):
+    def _distill_loss(self, labels, teacher):
+        d, e, N = self.dims, self.ends, self.distill.N
+        top_idx, top_logit, top_lse = (tuple(teacher) + (None,))[:3]
+        lab = labels.reshape(-1)[self.test_rows] if self.distill.alpha < 1 else None
+        tfm.decode_fwd(d, e, self.n_train, self.n_feat, self.Y, self.ends_params, self.logits,
+                       self.ends_ws)
+        tfm.distill_loss(self.distill, self.logits[:N], top_idx, top_logit, top_lse, lab, None,
+                         self.row_class, self.loss, None, self.dlogits[:N], self.distill_ws)
+        tfm.decode_bwd(d, e, self.n_train, self.n_feat, self.Y, self.ends_params, self.dlogits,
+                       self.dY, self.ends_grads, False, self.ends_ws)
+
+    def run(self, x, labels, cat_ids=None, teacher=None):
         """x: device float32 [B, R-T, F]; labels: device int32 [B, R-T].  Returns the loss as a
-        device tensor of one element; gradients land in stack.grads, ends_grads, table_grad."""
+        device tensor of one element; gradients land in stack.grads, ends_grads, table_grad (and
+        cat_grad).  With a cat_table: cat_ids, device int32 [B, R-T, cat_cols].  With distill:
+        teacher = (top_idx int32 [N, k], top_logit float32 [N, k]) and, with tail, top_lse float32
+        [N], for the N unlabelled rows in (dataset, row) order."""
         d, e = self.dims, self.ends
+        if (cat_ids is None) != (self.cat_table is None) or \
+                (teacher is None) != (self.distill is None):
+            raise ValueError("cat_ids goes with a cat_table, teacher with distill")
         if self.T:
             tfm.thinking_rows_fwd(d, self.n_train, self.cell_mask, self.T, self.table, self.X,
                                   self.stack.workspace)
         tfm.encode_fwd(d, e, self.n_train, self.n_feat, x, labels, self.ends_params, self.X,
                        self.ends_ws)
+        if cat_ids is not None:
+            tfm.embed_fwd(self.cat, cat_ids, self.cat_table, self.X.view(-1)[self.cat_at:], True)
         self.Y = self.stack.forward(self.X)
-        tfm.decode_loss(d, e, self.n_train, self.n_feat, self.n_class, labels, self.Y,
-                        self.ends_params, self.loss, None, self.dY, self.ends_grads, False,
-                        self.ends_ws)
+        if teacher is not None:
+            self._distill_loss(labels, teacher)
+        else:
+            tfm.decode_loss(d, e, self.n_train, self.n_feat, self.n_class, labels, self.Y,
+                            self.ends_params, self.loss, None, self.dY, self.ends_grads, False,
+                            self.ends_ws)
         self.dX = self.stack.backward(self.dY)
+        if cat_ids is not None:
+            tfm.embed_bwd(self.cat, cat_ids, self.dX.view(-1)[self.cat_at:], self.cat_grad, False,
+                          self.cat_ws)
         if self.T:
             tfm.thinking_rows_bwd(d, self.n_train, self.cell_mask, self.T, self.dX,
                                   self.table_grad, False, self.stack.workspace)
@@ -274,6 +344,8 @@ class Optimizer:
         extra = [(ts.ends_params, ts.ends_grads)]
         if ts.T:
             extra.append((ts.table.view(-1), ts.table_grad.view(-1)))
+        if ts.cat_table is not None:
+            extra.append((ts.cat_table.view(-1), ts.cat_grad.view(-1)))
         for p, g in extra:
             self.vectors.append((p, g, p.clone(), torch.zeros_like(p), [(0, p.numel())]))
         self.muon = {}
@@ -312,10 +384,12 @@ class InferModel:
     [0, max n_train), which hold every labelled row — run through every layer once and leave
     key/value caches, the remaining rows run through every layer in chunks of unlabelled rows
     against those caches, and the decoder turns the outputs of each dataset's unlabelled rows
-    into logits.  Allocation, call order and the row order of the result only."""
+    into logits.  Allocation, call order and the row order of the result only.  cat_table, cat_cols,
+    cat_scale: as for TrainStep."""
 
     def __init__(self, dims, ends, n_train, n_feat, params, ends_params, table=None,
-                 chunk=256, device="cuda", decay_base=0.95):
+                 chunk=256, device="cuda", decay_base=0.95, cat_table=None, cat_cols=0,
+                 cat_scale=1.0):
         if dims.dtype != tfm.TFM_BF16:
             raise ValueError("the forward-only path runs in bfloat16")
         self.dims, self.ends = dims, ends
@@ -349,18 +423,53 @@ class InferModel:
         self.xq = torch.empty(B * self.chunk * (C + 1) * E, dtype=torch.bfloat16, device=device)
         self.K = ends.K
         self.device = device
+        self.cat_table = None
+        if cat_table is not None:
+            self.cat_table = cat_table if isinstance(cat_table, torch.Tensor) else \
+                torch.from_numpy(np.ascontiguousarray(cat_table, dtype=np.float32)).to(device)
+            self.cat, self.cat_at = cat_embed(dims, ends.T, cat_cols, self.cat_table.shape[0],
+                                              cat_scale)
 
-    def predict(self, x, labels):
+    def draw(self, x, labels, u, cat_ids=None, n_class=None, temperature=None, top_k=None,
+             top_p=None, min_p=None):
+        """One class drawn for every unlabelled row (tfm_sample), in predict's row order: returns
+        (classes int32 [T_test], their log-probabilities, the logits).  u: device float32 [T_test]
+        in [0, 1); n_class: host int32 [B], the classes of each dataset (None: all K); the settings
+        are numbers, or device tensors of a value per row."""
+        logits = self.predict(x, labels, cat_ids)
+        N = logits.shape[0]
+        rows = self.dims.R - self.n_train
+        if n_class is not None:
+            n_class = torch.from_numpy(np.repeat(np.asarray(n_class, np.int32), rows)).to(
+                logits.device)
+
+        def per_row(v, dtype):
+            return v if v is None or isinstance(v, torch.Tensor) else \
+                torch.full((N,), v, dtype=dtype, device=logits.device)
+
+        token = torch.empty(N, dtype=torch.int32, device=logits.device)
+        logprob = torch.empty(N, dtype=torch.float32, device=logits.device)
+        tfm.sample(tfm.make_sampling(N, self.K, self.K, tfm.TFM_F32), logits, n_class,
+                   per_row(temperature, torch.float32), per_row(top_k, torch.int32),
+                   per_row(top_p, torch.float32), per_row(min_p, torch.float32), u, token, logprob)
+        return token, logprob, logits
+
+    def predict(self, x, labels, cat_ids=None):
         """x: device float32 [B, R-T, F]; labels: device int32 [B, R-T] (the labelled rows'
-        entries are read).  Returns logits [T_test, K] of the unlabelled rows in (dataset, row)
-        order, as tfm_decode_loss orders them."""
+        entries are read); with a cat_table: cat_ids, device int32 [B, R-T, cat_cols].  Returns
+        logits [T_test, K] of the unlabelled rows in (dataset, row) order, as tfm_decode_loss
+        orders them."""
         d, e = self.dims, self.ends
+        if (cat_ids is None) != (self.cat_table is None):
+            raise ValueError("cat_ids goes with a cat_table")
         B, C, E = d.B, d.C, d.E
         if e.T:
             tfm.thinking_rows_fwd(d, self.n_train, self.cell_mask, e.T, self.table, self.X,
                                   self.stack.workspace)
         tfm.encode_fwd(d, e, self.n_train, self.n_feat, x, labels, self.ends_params, self.X,
                        self.ends_ws)
+        if cat_ids is not None:
+            tfm.embed_fwd(self.cat, cat_ids, self.cat_table, self.X.view(-1)[self.cat_at:], True)
         Xc = self.X[:, :self.Rc].contiguous()
         parts = []  # (first row, per-dataset row counts, logits of the call)
         Yc = self.stack.context(Xc)

@@ -1,5 +1,5 @@
-"""Thin ctypes binding of libtfmlayer.so (C ABI in include/tfm_layer.h, include/tfm_ends.h and
-include/tfm_optim.h).
+"""Thin ctypes binding of libtfmlayer.so (C ABI in include/tfm_layer.h, include/tfm_ends.h,
+include/tfm_vocab.h and include/tfm_optim.h).
 
 Argument marshalling only: every step of the layer runs in the library's HIP kernels.  torch
 supplies device memory and the stream.  There is no fallback: if the library is missing, every
@@ -29,7 +29,10 @@ EXPORTS = ("tfm_layer_param_count", "tfm_layer_saved_bytes", "tfm_layer_workspac
            "tfm_layer_fwd_query", "tfm_last_error", "tfm_prof_enable", "tfm_prof_collect",
            "tfm_prof_step", "tfm_prof_item_bwd_fused_rows", "tfm_prof_item_bwd_columns",
            "tfm_ends_param_count", "tfm_ends_workspace_bytes", "tfm_encode_fwd",
-           "tfm_encode_bwd", "tfm_decode_fwd", "tfm_decode_loss", "tfm_clip_workspace_bytes",
+           "tfm_encode_bwd", "tfm_decode_fwd", "tfm_decode_loss", "tfm_decode_bwd",
+           "tfm_embed_workspace_bytes", "tfm_embed_fwd", "tfm_embed_bwd",
+           "tfm_distill_workspace_bytes", "tfm_distill_loss", "tfm_sample",
+           "tfm_clip_workspace_bytes",
            "tfm_clip_scale", "tfm_sfadamw_step", "tfm_muon_workspace_bytes", "tfm_muon_step")
 
 
@@ -72,6 +75,42 @@ class tfm_sfadamw(ctypes.Structure):
 class tfm_muon(ctypes.Structure):
     _fields_ = [(n, ctypes.c_float) for n in ("lr", "momentum", "weight_decay")] + \
         [("nesterov", ctypes.c_int32), ("ns_steps", ctypes.c_int32)]
+
+
+_DTYPES = {"f32": TFM_F32, "bf16": TFM_BF16}
+
+
+class tfm_embed(ctypes.Structure):
+    _fields_ = [("n", ctypes.c_int32 * 3)] + \
+        [(n, ctypes.c_int32) for n in ("E", "V", "dtype", "table_dtype")] + \
+        [("scale", ctypes.c_float), ("stride", ctypes.c_int64 * 3)]
+
+
+def make_embed(n, stride, E, V, dtype, table_dtype="f32", scale=1.0):
+    """n: shape (n0, n1, n2) of the ids; stride: elements between rows along each of its axes."""
+    if len(n) != 3 or len(stride) != 3:
+        raise ValueError(f"need three sizes and three strides, got {n} and {stride}")
+    return tfm_embed((ctypes.c_int32 * 3)(*[int(v) for v in n]), int(E), int(V),
+                     int(_DTYPES.get(dtype, dtype)), int(_DTYPES.get(table_dtype, table_dtype)),
+                     float(scale), (ctypes.c_int64 * 3)(*[int(v) for v in stride]))
+
+
+class tfm_distill(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("N", "V", "k", "dtype", "tail")] + \
+        [("temperature", ctypes.c_float), ("alpha", ctypes.c_float), ("ld", ctypes.c_int64)]
+
+
+def make_distill(N, V, k, ld, dtype, temperature=1.0, alpha=1.0, tail=False):
+    return tfm_distill(int(N), int(V), int(k), int(_DTYPES.get(dtype, dtype)), int(tail),
+                       float(temperature), float(alpha), int(ld))
+
+
+class tfm_sampling(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("N", "V", "dtype")] + [("ld", ctypes.c_int64)]
+
+
+def make_sampling(N, V, ld, dtype):
+    return tfm_sampling(int(N), int(V), int(_DTYPES.get(dtype, dtype)), int(ld))
 
 
 def lib():
@@ -120,6 +159,20 @@ def lib():
         L.tfm_decode_loss.restype = i32
         L.tfm_decode_loss.argtypes = [P(tfm_dims), E_, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp,
                                       i32, vp, sz, vp]
+        L.tfm_decode_bwd.restype = i32
+        L.tfm_decode_bwd.argtypes = [P(tfm_dims), E_, vp, vp, vp, vp, vp, vp, vp, i32, vp, sz, vp]
+        L.tfm_embed_workspace_bytes.restype = sz
+        L.tfm_embed_workspace_bytes.argtypes = [P(tfm_embed)]
+        L.tfm_embed_fwd.restype = i32
+        L.tfm_embed_fwd.argtypes = [P(tfm_embed), vp, vp, vp, i32, vp]
+        L.tfm_embed_bwd.restype = i32
+        L.tfm_embed_bwd.argtypes = [P(tfm_embed), vp, vp, vp, i32, vp, sz, vp]
+        L.tfm_distill_workspace_bytes.restype = sz
+        L.tfm_distill_workspace_bytes.argtypes = [P(tfm_distill)]
+        L.tfm_distill_loss.restype = i32
+        L.tfm_distill_loss.argtypes = [P(tfm_distill)] + [vp] * 11 + [sz, vp]
+        L.tfm_sample.restype = i32
+        L.tfm_sample.argtypes = [P(tfm_sampling)] + [vp] * 10
         i64, f32 = ctypes.c_int64, ctypes.c_float
         L.tfm_clip_workspace_bytes.restype = sz
         L.tfm_clip_workspace_bytes.argtypes = [i32, P(i64)]
@@ -337,6 +390,137 @@ def decode_loss(dims, ends, n_train, n_feat, n_class, labels, Y, params, loss, l
                                _ptr(labels), _ptr(Y), _ptr(params), _ptr(loss), _ptr(logits),
                                _ptr(dY), _ptr(grads), int(bool(accumulate)), _ptr(workspace),
                                _nbytes(workspace), _stream(stream))
+    _check(rc)
+
+
+def decode_bwd(dims, ends, n_train, n_feat, Y, params, dlogits, dY, grads, accumulate, workspace,
+               stream=None):
+    """tfm_decode_bwd: dY (device like Y) and the decoder entries of grads for the gradient dlogits
+    (device float32 [T_test, K]) of decode_fwd's logits."""
+    nt, ntp = _host(n_train, np.int32)
+    nf, nfp = _host(n_feat, np.int32)
+    rc = lib().tfm_decode_bwd(ctypes.byref(dims), ctypes.byref(ends), ntp, nfp, _ptr(Y),
+                              _ptr(params), _ptr(dlogits), _ptr(dY), _ptr(grads),
+                              int(bool(accumulate)), _ptr(workspace), _nbytes(workspace),
+                              _stream(stream))
+    _check(rc)
+
+
+def _tensors(call, *wanted):
+    """(name, tensor, type, shape) of a call's device tensors, None for one left out: raises unless
+    every tensor has its type and shape, lies side by side (shape None: not looked at) and all are
+    on the current device."""
+    import torch
+    for name, t, dtype, shape in wanted:
+        if t is None:
+            continue
+        if t.dtype != dtype:
+            raise ValueError(f"{call}: {name} is {t.dtype}, {dtype} wanted")
+        if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+            raise ValueError(f"{call}: {name} has shape {tuple(t.shape)} and strides {t.stride()}, "
+                             f"{tuple(shape)} side by side wanted")
+        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+            raise ValueError(f"{call}: {name} is on {t.device}, not on the current GPU")
+
+
+def _torch_dtype(dtype):
+    import torch
+    return torch.bfloat16 if dtype == TFM_BF16 else torch.float32
+
+
+def _embed_rows(call, e, name, t):
+    """The activations of an embedding call: from their first row on, room for the last."""
+    n, reach = 1, 0
+    for size, step in zip(e.n, e.stride):
+        n *= size
+        reach += (size - 1) * step
+    room = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+    if n and reach + e.E > room:
+        raise ValueError(f"{call}: {name} has room for {room} elements, {reach + e.E} wanted")
+    return name, t, _torch_dtype(e.dtype), None
+
+
+def _logit_rows(call, d, name, t):
+    """Rows of logits, ld elements apart."""
+    if t is None:
+        return name, t, None, None
+    if tuple(t.shape) != (d.N, d.V) or (d.V > 1 and d.N and t.stride(1) != 1) or \
+            (d.N > 1 and t.stride(0) != d.ld):
+        raise ValueError(f"{call}: {name} has shape {tuple(t.shape)} and strides {t.stride()}, "
+                         f"({d.N}, {d.V}) with rows {d.ld} apart wanted")
+    return name, t, _torch_dtype(d.dtype), None
+
+
+def embed_workspace_bytes(e):
+    return lib().tfm_embed_workspace_bytes(ctypes.byref(e))
+
+
+def embed_fwd(e, ids, table, out, accumulate=False, stream=None):
+    """tfm_embed_fwd.  ids: device int32 of shape e.n; table: device [V, E]; out: device tensor
+    whose first element is the first row's (rows e.stride apart)."""
+    import torch
+    _tensors("embed_fwd", ("ids", ids, torch.int32, tuple(e.n)),
+             ("table", table, _torch_dtype(e.table_dtype), (e.V, e.E)),
+             _embed_rows("embed_fwd", e, "out", out))
+    rc = lib().tfm_embed_fwd(ctypes.byref(e), _ptr(ids), _ptr(table), _ptr(out),
+                             int(bool(accumulate)), _stream(stream))
+    _check(rc)
+
+
+def embed_bwd(e, ids, dout, dtable, accumulate, workspace, stream=None):
+    """tfm_embed_bwd: dtable (device float32 [V, E]) gets (or adds) the scaled sums of dout's rows
+    by id; workspace: embed_workspace_bytes(e)."""
+    import torch
+    _tensors("embed_bwd", ("ids", ids, torch.int32, tuple(e.n)),
+             _embed_rows("embed_bwd", e, "dout", dout),
+             ("dtable", dtable, torch.float32, (e.V, e.E)),
+             ("workspace", workspace, workspace.dtype, None))
+    rc = lib().tfm_embed_bwd(ctypes.byref(e), _ptr(ids), _ptr(dout), _ptr(dtable),
+                             int(bool(accumulate)), _ptr(workspace), _nbytes(workspace),
+                             _stream(stream))
+    _check(rc)
+
+
+def distill_workspace_bytes(d):
+    return lib().tfm_distill_workspace_bytes(ctypes.byref(d))
+
+
+def distill_loss(d, logits, top_idx, top_logit, top_lse, labels, weights, n_class, loss, row_loss,
+                 dlogits, workspace, stream=None):
+    """tfm_distill_loss.  logits, dlogits: device [N, V], rows d.ld apart (dlogits None: loss
+    alone; logits itself: in place); top_idx int32, top_logit float32 [N, k]; top_lse float32 [N]
+    (tail); labels int32 [N] (alpha < 1); weights float32 [N], n_class int32 [N], row_loss float32
+    [N] or None; loss: device float32, its first element is written."""
+    import torch
+    i32, f32 = torch.int32, torch.float32
+    _tensors("distill_loss", _logit_rows("distill_loss", d, "logits", logits),
+             _logit_rows("distill_loss", d, "dlogits", dlogits),
+             ("top_idx", top_idx, i32, (d.N, d.k)), ("top_logit", top_logit, f32, (d.N, d.k)),
+             ("top_lse", top_lse, f32, (d.N,)), ("labels", labels, i32, (d.N,)),
+             ("weights", weights, f32, (d.N,)), ("n_class", n_class, i32, (d.N,)),
+             ("loss", loss, f32, None), ("row_loss", row_loss, f32, (d.N,)),
+             ("workspace", workspace, workspace.dtype, None))
+    rc = lib().tfm_distill_loss(ctypes.byref(d), _ptr(logits), _ptr(top_idx), _ptr(top_logit),
+                                _ptr(top_lse), _ptr(labels), _ptr(weights), _ptr(n_class),
+                                _ptr(loss), _ptr(row_loss), _ptr(dlogits), _ptr(workspace),
+                                _nbytes(workspace), _stream(stream))
+    _check(rc)
+
+
+def sample(s, logits, n_class, temperature, top_k, top_p, min_p, u, token, logprob=None,
+           stream=None):
+    """tfm_sample.  logits: device [N, V], rows s.ld apart; n_class, top_k int32 [N],
+    temperature, top_p, min_p float32 [N], each or None; u float32 [N]; token int32 [N]; logprob
+    float32 [N] or None."""
+    import torch
+    i32, f32, N = torch.int32, torch.float32, (s.N,)
+    _tensors("sample", _logit_rows("sample", s, "logits", logits), ("n_class", n_class, i32, N),
+             ("temperature", temperature, f32, N), ("top_k", top_k, i32, N),
+             ("top_p", top_p, f32, N), ("min_p", min_p, f32, N), ("u", u, f32, N),
+             ("token", token, i32, N), ("logprob", logprob, f32, N))
+    rc = lib().tfm_sample(ctypes.byref(s), _ptr(logits), _ptr(n_class), _ptr(temperature),
+                          _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(token),
+                          _ptr(logprob), _stream(stream))
     _check(rc)
 
 
