@@ -1,4 +1,14 @@
 // Embedding rows and their gradient (declarations in vocab.h).
+//
+// Forward: a copy with a factor; rows go to groups of W lanes that move 16 bytes each where the
+// rows allow it, four rows in flight per group.
+// Backward: dtable[v] = scale sum_{n: id_n = v} dout_n.  The positions are sorted by id (stable
+// radix sort, so equal ids keep their order), and the sorted positions are cut into pieces of equal
+// length whatever the ids are: every group of lanes adds up the rows of its piece in registers and
+// writes a sum where the id changes.  Sums that cross a piece's border are joined in LDS within a
+// workgroup and through float32 rows in the workspace between workgroups, in order, so the result
+// does not depend on timing.  Each gradient row is written once, by the one group that completes
+// it; rows of ids that do not occur are zeroed by further workgroups of the same launch.
 #include "vocab.h"
 
 #include <hip/hip_runtime.h>
@@ -6,69 +16,696 @@
 namespace tfm {
 namespace {
 
-// First element of the activations' row n.
-__device__ __forceinline__ int64_t row_at(const EmbedGeo& g, int64_t n) {
-  const int64_t ij = n / g.n2, k = n - ij * g.n2;
-  const int64_t i = ij / g.n1, j = ij - i * g.n1;
+// ---- rows as vectors --------------------------------------------------------------------------
+// VEC elements of type T at p as floats; p is aligned to min(16, VEC sizeof(T)) bytes.
+template <int VEC>
+__device__ __forceinline__ void ldv(const float* p, float* v) {
+  if constexpr (VEC >= 4) {
+#pragma unroll
+    for (int i = 0; i < VEC / 4; ++i) {
+      const float4 a = reinterpret_cast<const float4*>(p)[i];
+      v[4 * i] = a.x; v[4 * i + 1] = a.y; v[4 * i + 2] = a.z; v[4 * i + 3] = a.w;
+    }
+  } else if constexpr (VEC == 2) {
+    const float2 a = *reinterpret_cast<const float2*>(p);
+    v[0] = a.x; v[1] = a.y;
+  } else {
+    v[0] = *p;
+  }
+}
+__device__ __forceinline__ void halves(uint32_t u, float* v) {
+  v[0] = __uint_as_float(u << 16);
+  v[1] = __uint_as_float(u & 0xffff0000u);
+}
+template <int VEC>
+__device__ __forceinline__ void ldv(const bf16* p, float* v) {
+  if constexpr (VEC == 8) {
+    const uint4 u = *reinterpret_cast<const uint4*>(p);
+    halves(u.x, v); halves(u.y, v + 2); halves(u.z, v + 4); halves(u.w, v + 6);
+  } else if constexpr (VEC == 4) {
+    const uint2 u = *reinterpret_cast<const uint2*>(p);
+    halves(u.x, v); halves(u.y, v + 2);
+  } else if constexpr (VEC == 2) {
+    halves(*reinterpret_cast<const uint32_t*>(p), v);
+  } else {
+    v[0] = ld(p);
+  }
+}
+template <int VEC>
+__device__ __forceinline__ void stv(float* p, const float* v) {
+  if constexpr (VEC >= 4) {
+#pragma unroll
+    for (int i = 0; i < VEC / 4; ++i)
+      reinterpret_cast<float4*>(p)[i] =
+          make_float4(v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]);
+  } else if constexpr (VEC == 2) {
+    *reinterpret_cast<float2*>(p) = make_float2(v[0], v[1]);
+  } else {
+    *p = v[0];
+  }
+}
+__device__ __forceinline__ uint32_t pair_of(const float* v) {
+  return (uint32_t)f2bf(v[0]) | (uint32_t)f2bf(v[1]) << 16;
+}
+template <int VEC>
+__device__ __forceinline__ void stv(bf16* p, const float* v) {
+  if constexpr (VEC == 8)
+    *reinterpret_cast<uint4*>(p) = make_uint4(pair_of(v), pair_of(v + 2), pair_of(v + 4), pair_of(v + 6));
+  else if constexpr (VEC == 4)
+    *reinterpret_cast<uint2*>(p) = make_uint2(pair_of(v), pair_of(v + 2));
+  else if constexpr (VEC == 2)
+    *reinterpret_cast<uint32_t*>(p) = pair_of(v);
+  else
+    st(p, v[0]);
+}
+
+// First element of the activations' row n.  n < 2^27, so n / d is the upper half of n (2^64 / d + 1)
+// for every d > 1.
+__device__ __forceinline__ uint32_t div_by(uint32_t n, uint64_t m) {
+  return m ? (uint32_t)__umul64hi(n, m) : n;
+}
+__device__ __forceinline__ int64_t row_at(const EmbedGeo& g, uint32_t n) {
+  const uint32_t ij = div_by(n, g.m2), k = n - ij * (uint32_t)g.n2;
+  const uint32_t i = div_by(ij, g.m1), j = ij - i * (uint32_t)g.n1;
   return i * g.stride[0] + j * g.stride[1] + k * g.stride[2];
 }
 
-template <class TT, class TO, bool ADD>
+// ---- forward -----------------------------------------------------------------------------------
+constexpr int FWD_ROWS = 4;  // rows in flight per group
+
+// Groups of W lanes, each FWD_ROWS consecutive rows of its slice of W * VEC elements (grid.y).
+template <class TT, class TO, int VEC, int W, bool ADD>
 __global__ __launch_bounds__(256) void k_embed_fwd(EmbedGeo g, const int32_t* __restrict__ ids,
                                                    const TT* __restrict__ table,
                                                    TO* __restrict__ out) {
-  for (int64_t n = blockIdx.x; n < g.N; n += gridDim.x) {
-    const int32_t id = ids[n];
-    const bool here = (uint32_t)id < (uint32_t)g.V;
-    if (ADD && !here) continue;
-    TO* o = out + row_at(g, n);
-    const TT* t = table + (int64_t)(here ? id : 0) * g.E;
-    for (int c = threadIdx.x; c < g.E; c += 256) {
-      float v = here ? g.scale * ld(t + c) : 0.f;
-      if (ADD) v += ld(o + c);
-      st(o + c, v);
+  const int lane = threadIdx.x % W;
+  const int c = ((int)blockIdx.y * W + lane) * VEC;
+  if (c >= g.E) return;
+  const int64_t groups = (int64_t)gridDim.x * (256 / W);
+  for (int64_t n0 = ((int64_t)blockIdx.x * (256 / W) + threadIdx.x / W) * FWD_ROWS; n0 < g.N;
+       n0 += groups * FWD_ROWS) {
+    int32_t id[FWD_ROWS];
+    float v[FWD_ROWS][VEC], o[FWD_ROWS][VEC];
+    TO* p[FWD_ROWS];
+#pragma unroll
+    for (int r = 0; r < FWD_ROWS; ++r) {
+      const int64_t n = n0 + r < g.N ? n0 + r : g.N - 1;
+      id[r] = ids[n];
+      p[r] = out + row_at(g, (uint32_t)n) + c;
+    }
+#pragma unroll
+    for (int r = 0; r < FWD_ROWS; ++r) {
+      const bool here = (uint32_t)id[r] < (uint32_t)g.V;
+      ldv<VEC>(table + (int64_t)(here ? id[r] : 0) * g.E + c, v[r]);
+      if (ADD) ldv<VEC>(p[r], o[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < FWD_ROWS; ++r) {
+      const bool here = (uint32_t)id[r] < (uint32_t)g.V;
+#pragma unroll
+      for (int i = 0; i < VEC; ++i) {
+        v[r][i] = here ? g.scale * v[r][i] : 0.f;
+        if (ADD) v[r][i] += o[r][i];
+      }
+      if (n0 + r < g.N && (here || !ADD)) stv<VEC>(p[r], v[r]);
     }
   }
 }
 
-// One workgroup per table row: the positions in order, those that hold the row's id added up.
-template <class TO, bool ADD>
-__global__ __launch_bounds__(256) void k_embed_bwd(EmbedGeo g, const int32_t* __restrict__ ids,
-                                                   const TO* __restrict__ dout,
-                                                   float* __restrict__ dtable) {
-  __shared__ int hit[256];
-  __shared__ int nhit[4];
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
-  for (int v = blockIdx.x; v < g.V; v += gridDim.x) {
-    for (int c0 = 0; c0 < g.E; c0 += 256) {
-      const int c = c0 + tid;
-      float acc = 0.f;
-      bool any = false;
-      for (int64_t n0 = 0; n0 < g.N; n0 += 256) {
-        const int64_t n = n0 + tid;
-        const bool mine = n < g.N && ids[n] == v;
-        const uint64_t b = __ballot(mine);
-        __syncthreads();
-        if (lane == 0) nhit[w] = __popcll(b);
-        __syncthreads();
-        int at = __popcll(b & ((1ull << lane) - 1)), total = 0;
-        for (int i = 0; i < 4; ++i) {
-          if (i < w) at += nhit[i];
-          total += nhit[i];
-        }
-        if (mine) hit[at] = tid;
-        __syncthreads();
-        for (int i = 0; i < total; ++i)
-          if (c < g.E) acc += ld(dout + row_at(g, n0 + hit[i]) + c);
-        any |= total > 0;
+// ---- sort by id ---------------------------------------------------------------------------------
+// Keys: the id, V for an absent one (they end up behind every id).  Radix passes from the lowest
+// digit up; a workgroup ranks a tile of keys, each wave a contiguous part of it, 64 at a time.
+constexpr int SORT_T = 512;                 // threads
+constexpr int SORT_TILE = 4096;             // keys of a workgroup
+constexpr int SORT_R = SORT_TILE / SORT_T;  // keys of a thread
+constexpr int SORT_W = SORT_T / 64;
+constexpr int SORT_BITS = 10;               // widest digit
+constexpr int SORT_FUSE = 24;               // workgroups up to which each sums the counts before it
+                                            // itself: one launch less (2^10 counts from 24 others
+                                            // are read in about the time of a launch)
+
+struct SortGeo {
+  int32_t N, V, nblk;
+  int32_t shift, bits;     // digit of the pass
+  int32_t first, last;     // first pass: keys from ids; last pass: rows' elements as payload
+};
+
+__device__ __forceinline__ int32_t key_at(const SortGeo& s, const int32_t* src, int n) {
+  const int32_t k = src[n];
+  return s.first && (uint32_t)k >= (uint32_t)s.V ? s.V : k;
+}
+
+// Counts of the digits of every tile: cnt[workgroup][digit], or cnt[digit][workgroup] for the scan.
+__global__ __launch_bounds__(SORT_T) void k_sort_count(SortGeo s, const int32_t* __restrict__ src,
+                                                       uint32_t* __restrict__ cnt) {
+  __shared__ uint32_t h[1 << SORT_BITS];
+  const int bins = 1 << s.bits;
+  for (int d = threadIdx.x; d < bins; d += SORT_T) h[d] = 0;
+  __syncthreads();
+  const int n0 = blockIdx.x * SORT_TILE;
+#pragma unroll
+  for (int r = 0; r < SORT_R; ++r) {
+    const int n = n0 + r * SORT_T + threadIdx.x;
+    if (n < s.N) atomicAdd(&h[key_at(s, src, n) >> s.shift & (bins - 1)], 1u);
+  }
+  __syncthreads();
+  for (int d = threadIdx.x; d < bins; d += SORT_T)
+    cnt[s.nblk > SORT_FUSE ? (int64_t)d * s.nblk + blockIdx.x : (int64_t)blockIdx.x * bins + d] = h[d];
+}
+
+// One wave per digit: its counts become the number of earlier equal digits, its total goes behind.
+__global__ __launch_bounds__(256) void k_sort_scan(SortGeo s, uint32_t* __restrict__ cnt) {
+  const int bins = 1 << s.bits, lane = threadIdx.x & 63;
+  const int d = blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (d >= bins) return;
+  uint32_t* c = cnt + (int64_t)d * s.nblk;
+  uint32_t run = 0;
+  for (int b = 0; b < s.nblk; b += 64) {
+    const uint32_t mine = b + lane < s.nblk ? c[b + lane] : 0;
+    uint32_t inc = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const uint32_t q = __shfl_up(inc, o);
+      if (lane >= o) inc += q;
+    }
+    if (b + lane < s.nblk) c[b + lane] = run + inc - mine;
+    run += __shfl(inc, 63);
+  }
+  if (lane == 0) cnt[(int64_t)bins * s.nblk + d] = run;
+}
+
+// Exclusive scan of v[0 .. 2^bits) by the workgroup; v and buf in LDS.
+__device__ __forceinline__ void scan_bins(uint32_t* v, int bins, uint32_t* buf) {
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  constexpr int PER = (1 << SORT_BITS) / SORT_T;
+  uint32_t x[PER], sum = 0;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    x[i] = t * PER + i < bins ? v[t * PER + i] : 0;
+    sum += x[i];
+  }
+  uint32_t inc = sum;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const uint32_t q = __shfl_up(inc, o);
+    if (lane >= o) inc += q;
+  }
+  if (lane == 63) buf[w] = inc;
+  __syncthreads();
+  uint32_t run = inc - sum;
+  for (int i = 0; i < w; ++i) run += buf[i];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    if (t * PER + i < bins) v[t * PER + i] = run;
+    run += x[i];
+  }
+  __syncthreads();
+}
+
+// Ranks of the workgroup's keys among its keys of the same digit, in order: wave w holds keys
+// w SORT_R 64 + r 64 + lane.  wcnt[w][digit] ends as the number of such keys of earlier waves.
+// digit < 0: no key.
+__device__ __forceinline__ void rank_tile(const int (&digit)[SORT_R], int bits,
+                                          uint32_t (*wcnt)[1 << SORT_BITS],
+                                          uint32_t (&rank)[SORT_R], uint32_t* total) {
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, bins = 1 << bits;
+  for (int d = t; d < bins; d += SORT_T)
+#pragma unroll
+    for (int i = 0; i < SORT_W; ++i) wcnt[i][d] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int r = 0; r < SORT_R; ++r) {
+    const bool on = digit[r] >= 0;
+    uint64_t same = __ballot(on);  // lanes that hold the same digit
+    for (int b = 0; b < bits; ++b) {
+      const bool bit = digit[r] >> b & 1;
+      const uint64_t m = __ballot(bit);
+      same &= bit ? m : ~m;
+    }
+    const uint64_t below = same & ((1ull << lane) - 1);
+    volatile uint32_t* c = &wcnt[w][on ? digit[r] : 0];
+    const uint32_t at = *c;
+    rank[r] = at + __popcll(below);
+    __builtin_amdgcn_wave_barrier();
+    if (on && below == 0) *c = at + __popcll(same);
+    __builtin_amdgcn_wave_barrier();
+  }
+  __syncthreads();
+  for (int d = t; d < bins; d += SORT_T) {
+    uint32_t run = 0;
+#pragma unroll
+    for (int i = 0; i < SORT_W; ++i) {
+      const uint32_t q = wcnt[i][d];
+      wcnt[i][d] = run;
+      run += q;
+    }
+    if (total) total[d] = run;
+  }
+  __syncthreads();
+}
+
+// One pass: keys and payload (position, or its row's first element in the last pass) to their
+// places.
+__global__ __launch_bounds__(SORT_T) void k_sort_place(SortGeo s, EmbedGeo g,
+                                                       const int32_t* __restrict__ src,
+                                                       const int32_t* __restrict__ srcpos,
+                                                       const uint32_t* __restrict__ cnt,
+                                                       int32_t* __restrict__ dst,
+                                                       int32_t* __restrict__ dstpos,
+                                                       int64_t* __restrict__ dstrow) {
+  __shared__ uint32_t wcnt[SORT_W][1 << SORT_BITS];
+  __shared__ uint32_t base[1 << SORT_BITS];
+  __shared__ uint32_t before[1 << SORT_BITS];
+  __shared__ uint32_t buf[SORT_W];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6, bins = 1 << s.bits;
+  // first place of every digit, and how many of its keys earlier workgroups hold
+  for (int d = t; d < bins; d += SORT_T) {
+    if (s.nblk > SORT_FUSE) {
+      base[d] = cnt[(int64_t)bins * s.nblk + d];
+      before[d] = cnt[(int64_t)d * s.nblk + blockIdx.x];
+    } else {
+      uint32_t all = 0, mine = 0;
+      for (int b = 0; b < s.nblk; ++b) {
+        const uint32_t q = cnt[b * bins + d];
+        if (b < (int)blockIdx.x) mine += q;
+        all += q;
       }
-      if (c < g.E) {
-        float* o = dtable + (int64_t)v * g.E + c;
-        if (!ADD) *o = g.scale * acc;
-        else if (any) *o += g.scale * acc;
+      base[d] = all;
+      before[d] = mine;
+    }
+  }
+  scan_bins(base, bins, buf);
+  const int n0 = blockIdx.x * SORT_TILE + w * SORT_R * 64 + lane;
+  int32_t key[SORT_R];
+  int digit[SORT_R];
+#pragma unroll
+  for (int r = 0; r < SORT_R; ++r) {
+    const int n = n0 + r * 64;
+    key[r] = n < s.N ? key_at(s, src, n) : 0;
+    digit[r] = n < s.N ? key[r] >> s.shift & (bins - 1) : -1;
+  }
+  uint32_t rank[SORT_R];
+  rank_tile(digit, s.bits, wcnt, rank, nullptr);
+#pragma unroll
+  for (int r = 0; r < SORT_R; ++r) {
+    if (digit[r] < 0) continue;
+    const int n = n0 + r * 64;
+    const int32_t pos = s.first ? n : srcpos[n];
+    const uint32_t at = base[digit[r]] + before[digit[r]] + wcnt[w][digit[r]] + rank[r];
+    dst[at] = key[r];
+    if (s.last) dstrow[at] = row_at(g, (uint32_t)pos);
+    else dstpos[at] = pos;
+  }
+}
+
+// The whole sort of at most one tile in one workgroup.
+__global__ __launch_bounds__(SORT_T) void k_sort_small(SortGeo s, EmbedGeo g, int passes,
+                                                       const int32_t* __restrict__ ids,
+                                                       int32_t* __restrict__ dst,
+                                                       int64_t* __restrict__ dstrow) {
+  __shared__ uint32_t wcnt[SORT_W][1 << SORT_BITS];
+  __shared__ uint32_t base[1 << SORT_BITS];
+  __shared__ uint32_t buf[SORT_W];
+  __shared__ int32_t keys[SORT_TILE];
+  __shared__ uint16_t from[SORT_TILE];
+  const int t = threadIdx.x, lane = t & 63, w = t >> 6;
+  const int n0 = w * SORT_R * 64 + lane;
+  int32_t key[SORT_R];
+  int digit[SORT_R], pos[SORT_R];
+#pragma unroll
+  for (int r = 0; r < SORT_R; ++r) {
+    const int n = n0 + r * 64;
+    key[r] = n < s.N ? key_at(s, ids, n) : 0;
+    pos[r] = n;
+  }
+  for (int p = 0; p < passes; ++p) {
+    const int shift = p * s.bits, bins = 1 << s.bits;
+#pragma unroll
+    for (int r = 0; r < SORT_R; ++r)
+      digit[r] = n0 + r * 64 < s.N ? key[r] >> shift & (bins - 1) : -1;
+    uint32_t rank[SORT_R];
+    rank_tile(digit, s.bits, wcnt, rank, base);
+    scan_bins(base, bins, buf);
+#pragma unroll
+    for (int r = 0; r < SORT_R; ++r) {
+      if (digit[r] < 0) continue;
+      const uint32_t at = base[digit[r]] + wcnt[w][digit[r]] + rank[r];
+      keys[at] = key[r];
+      from[at] = (uint16_t)pos[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < SORT_R; ++r) {
+      const int n = n0 + r * 64;
+      if (n < s.N) {
+        key[r] = keys[n];
+        pos[r] = from[n];
+      }
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int r = 0; r < SORT_R; ++r) {
+    const int n = n0 + r * 64;
+    if (n < s.N) {
+      dst[n] = key[r];
+      dstrow[n] = row_at(g, (uint32_t)pos[r]);
+    }
+  }
+}
+
+// ---- sums ----------------------------------------------------------------------------------------
+constexpr int SUM_T = 256;
+constexpr int SUM_U = 8;       // rows in flight per group
+constexpr int FILL_ROWS = 64;  // gradient rows that a zeroing workgroup looks after
+
+struct SumGeo {
+  int64_t N;
+  int32_t piece;   // sorted positions of a group, a multiple of SUM_U
+  int32_t nblk;    // workgroups that add; the others zero
+  int32_t W;       // lanes of a group
+  int32_t slices;  // grid.y
+};
+
+// Sorted positions [a, b) of group k of workgroup blk.
+__device__ __forceinline__ int64_t piece_at(const SumGeo& s, int64_t blk, int k, int groups) {
+  const int64_t a = (blk * groups + k) * (int64_t)s.piece;
+  return a < s.N ? a : s.N;
+}
+
+template <int VEC, bool ADD>
+__device__ __forceinline__ void write_row(const EmbedGeo& g, float* dtable, int32_t v, int c,
+                                          const float* acc) {
+  float* o = dtable + (int64_t)v * g.E + c;
+  float x[VEC];
+  if (ADD) ldv<VEC>(o, x);
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) x[i] = ADD ? x[i] + g.scale * acc[i] : g.scale * acc[i];
+  stv<VEC>(o, x);
+}
+
+// Zeroes the rows among FILL_ROWS whose ids do not occur, of the workgroup's slice.
+template <int VEC, int W>
+__device__ __forceinline__ void zero_rows(const EmbedGeo& g, const SumGeo& s,
+                                          const int32_t* keys, float* dtable, int* present) {
+  const int v0 = ((int)blockIdx.x - s.nblk) * FILL_ROWS;
+  if (threadIdx.x < FILL_ROWS) {
+    const int v = v0 + threadIdx.x;
+    int64_t lo = 0, hi = s.N;  // first sorted position with a key >= v
+    while (lo < hi) {
+      const int64_t mid = (lo + hi) >> 1;
+      if (keys[mid] < v) lo = mid + 1;
+      else hi = mid;
+    }
+    present[threadIdx.x] = v >= g.V || (lo < s.N && keys[lo] == v);
+  }
+  __syncthreads();
+  const int c = ((int)blockIdx.y * W + threadIdx.x % W) * VEC;
+  const float zero[VEC] = {};
+  if (c >= g.E) return;
+  for (int r = threadIdx.x / W; r < FILL_ROWS; r += SUM_T / W)
+    if (!present[r]) stv<VEC>(dtable + (int64_t)(v0 + r) * g.E + c, zero);
+}
+
+// part: [nblk][2][E]: what a workgroup's positions add to a run that began in an earlier one, and
+// to a run that begins here and goes on in the next.
+template <class TO, int VEC, int W, bool ADD>
+__global__ __launch_bounds__(SUM_T) void k_embed_sum(EmbedGeo g, SumGeo s,
+                                                     const int32_t* __restrict__ keys,
+                                                     const int64_t* __restrict__ rows,
+                                                     const TO* __restrict__ dout,
+                                                     float* __restrict__ dtable,
+                                                     float* __restrict__ part) {
+  constexpr int K = SUM_T / W;  // groups
+  // per group: its share of a run that came in, and of one that goes out
+  __shared__ float edge[K][2][W * VEC];
+  __shared__ int32_t okey[K];   // key that goes out of the group, -1: none
+  __shared__ int32_t through[K];  // the key that came in goes out as well
+  __shared__ int present[FILL_ROWS];
+  if ((int)blockIdx.x >= s.nblk) {
+    zero_rows<VEC, W>(g, s, keys, dtable, present);
+    return;
+  }
+  const int k = threadIdx.x / W, lane = threadIdx.x % W;
+  const int c = ((int)blockIdx.y * W + lane) * VEC;
+  const bool live = c < g.E;
+  const int64_t a = piece_at(s, blockIdx.x, k, K), b = piece_at(s, blockIdx.x, k + 1, K);
+  float acc[VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
+  int32_t cur = -1;
+  const bool head = a > 0 && a < b && keys[a - 1] == keys[a];
+  bool came_in = head;  // the current run began in an earlier piece
+  const TO* d = dout + (live ? c : 0);
+  bool end = false;
+  for (int64_t t = a; t < b && !end; t += SUM_U) {
+    int32_t key[SUM_U];
+    float x[SUM_U][VEC];
+#pragma unroll
+    for (int i = 0; i < SUM_U; ++i) {
+      const int64_t n = t + i < b ? t + i : b - 1;
+      key[i] = t + i < b ? keys[n] : g.V;
+      ldv<VEC>(d + rows[n], x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < SUM_U; ++i) {
+      if (key[i] != cur) {
+        if (cur >= 0) {
+          if (came_in) {
+#pragma unroll
+            for (int j = 0; j < VEC; ++j) edge[k][0][lane * VEC + j] = acc[j];
+          } else if (live) {
+            write_row<VEC, ADD>(g, dtable, cur, c, acc);
+          }
+          came_in = false;
+        }
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
+        cur = key[i] < g.V ? key[i] : -1;
+      }
+      if (cur >= 0) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) acc[j] += x[i][j];
+      } else {
+        end = true;  // only absent ids follow
       }
     }
   }
+  // the last run: complete, or going on in the next piece
+  const bool goes_on = cur >= 0 && b < s.N && keys[b] == cur;
+  if (cur >= 0) {
+    if (came_in || goes_on) {
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) edge[k][came_in ? 0 : 1][lane * VEC + j] = acc[j];
+    } else if (live) {
+      write_row<VEC, ADD>(g, dtable, cur, c, acc);
+    }
+  }
+  if (lane == 0) {
+    okey[k] = goes_on && !came_in ? cur : -1;
+    through[k] = goes_on && came_in;
+  }
+  __syncthreads();
+  // join inside the workgroup: each group the run that leaves it first, group 0 also the run that
+  // came into the workgroup
+  for (int from = k == 0 ? -1 : k; from <= k; ++from) {
+    int32_t run;
+    int at;
+    if (from < 0) {
+      if (!head || keys[a] >= g.V) continue;
+      run = keys[a];
+      at = 0;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) acc[j] = edge[0][0][lane * VEC + j];
+    } else {
+      if (okey[k] < 0) continue;
+      run = okey[k];
+      at = k + 1;
+#pragma unroll
+      for (int j = 0; j < VEC; ++j) acc[j] = edge[k][1][lane * VEC + j];
+      if (at < K) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) acc[j] += edge[at][0][lane * VEC + j];
+      }
+    }
+    while (at < K && through[at]) {
+      if (++at < K) {
+#pragma unroll
+        for (int j = 0; j < VEC; ++j) acc[j] += edge[at][0][lane * VEC + j];
+      }
+    }
+    if (!live) continue;
+    if (from < 0) stv<VEC>(part + ((int64_t)blockIdx.x * 2 + 0) * g.E + c, acc);
+    else if (at == K) stv<VEC>(part + ((int64_t)blockIdx.x * 2 + 1) * g.E + c, acc);
+    else write_row<VEC, ADD>(g, dtable, run, c, acc);
+  }
+}
+
+// Runs that cross workgroups: the workgroup in which one begins adds the later ones' shares, its
+// groups every K-th of them, and then the groups' sums in order.
+template <int VEC, int W, bool ADD>
+__global__ __launch_bounds__(SUM_T) void k_embed_join(EmbedGeo g, SumGeo s,
+                                                      const int32_t* __restrict__ keys,
+                                                      const float* __restrict__ part,
+                                                      float* __restrict__ dtable) {
+  constexpr int K = SUM_T / W;
+  __shared__ float sums[K][W * VEC];
+  const int64_t a = piece_at(s, blockIdx.x, 0, K), b = piece_at(s, blockIdx.x, K, K);
+  if (b >= s.N) return;
+  const int32_t run = keys[b - 1];
+  if (run >= g.V || keys[b] != run || (a > 0 && keys[a - 1] == run)) return;
+  const int k = threadIdx.x / W, lane = threadIdx.x % W;
+  const int c = ((int)blockIdx.y * W + lane) * VEC;
+  const bool live = c < g.E;
+  float acc[VEC], x[4][VEC];
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
+  bool more = true;
+  for (int64_t j0 = blockIdx.x + 1 + k; more && j0 < s.nblk; j0 += 4 * K) {
+    bool in[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int64_t j = j0 + q * K, jj = j < s.nblk ? j : s.nblk - 1;
+      in[q] = j < s.nblk && keys[piece_at(s, jj, 0, K)] == run;
+      ldv<VEC>(part + (jj * 2) * g.E + (live ? c : 0), x[q]);
+    }
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (in[q]) {
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) acc[i] += x[q][i];
+      }
+    }
+    more = in[3];
+  }
+#pragma unroll
+  for (int i = 0; i < VEC; ++i) sums[k][lane * VEC + i] = acc[i];
+  __syncthreads();
+  if (k != 0 || !live) return;
+  ldv<VEC>(part + ((int64_t)blockIdx.x * 2 + 1) * g.E + c, acc);
+  for (int q = 0; q < K; ++q)
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) acc[i] += sums[q][lane * VEC + i];
+  write_row<VEC, ADD>(g, dtable, run, c, acc);
+}
+
+// ---- host side -----------------------------------------------------------------------------------
+
+int sort_passes(int32_t V, int* bits) {
+  int total = 0;
+  while (total < 31 && (V >> total) != 0) ++total;
+  const int passes = (total + SORT_BITS - 1) / SORT_BITS;
+  *bits = (total + passes - 1) / passes;
+  return passes;
+}
+
+// Lanes of a group: the row in vectors of VEC elements, at most a wave; a power of two >= 8.
+int group_width(int32_t E, int vec) {
+  int W = 8;
+  while (W < 64 && W * vec < E) W *= 2;
+  return W;
+}
+
+// Sorted positions per group: enough groups for 16 waves on each of 256 CUs, which hide the row
+// loads' latency; at least 16, so that the edges' share of the traffic stays small.
+SumGeo sum_geo(const EmbedGeo& g, int vec) {
+  SumGeo s;
+  s.N = g.N;
+  s.W = group_width(g.E, vec);
+  s.slices = (g.E + s.W * vec - 1) / (s.W * vec);
+  const double groups = 4096.0 * (64 / s.W) / s.slices;
+  int64_t piece = (int64_t)((double)g.N / (groups > 1.0 ? groups : 1.0)) + 1;
+  if (piece < 16) piece = 16;
+  piece = (piece + SUM_U - 1) / SUM_U * SUM_U;
+  s.piece = (int32_t)piece;
+  const int64_t per = piece * (SUM_T / s.W);
+  s.nblk = (int32_t)((g.N + per - 1) / per);
+  return s;
+}
+
+struct EmbedWs {
+  size_t key[2], pos[2], row, cnt, part, total;
+};
+EmbedWs embed_ws(const EmbedGeo& g) {
+  EmbedWs w;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    const size_t at = off;
+    off += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  int bits;
+  sort_passes(g.V, &bits);
+  const size_t nblk = (size_t)((g.N + SORT_TILE - 1) / SORT_TILE);
+  for (int i = 0; i < 2; ++i) w.key[i] = take((size_t)g.N * 4);
+  for (int i = 0; i < 2; ++i) w.pos[i] = take(nblk > 1 ? (size_t)g.N * 4 : 0);
+  w.row = take((size_t)g.N * 8);
+  w.cnt = take(nblk > 1 ? ((nblk + 1) << bits) * 4 : 0);
+  // the widest and the narrowest vectors bound the number of workgroups
+  size_t blocks = 0;
+  for (int vec = 1; vec <= 8; vec *= 2) {
+    const size_t n = (size_t)sum_geo(g, vec).nblk;
+    if (n > blocks) blocks = n;
+  }
+  w.part = take(blocks * 2 * (size_t)g.E * 4);
+  w.total = off > 0 ? off : 256;
+  return w;
+}
+
+bool fits(const void* p, size_t bytes) { return (uintptr_t)p % bytes == 0; }
+
+// Widest vector, in elements of at most 16 bytes of T, at which every row starts.
+template <class T>
+int vec_of(const EmbedGeo& g, const T* rows) {
+  int vec = 16 / (int)sizeof(T);
+  auto ok = [&](int v) {
+    if (g.E % v || !fits(rows, v * sizeof(T))) return false;
+    for (int i = 0; i < 3; ++i)
+      if (g.stride[i] % v) return false;
+    return true;
+  };
+  while (vec > 1 && !ok(vec)) vec /= 2;
+  return vec;
+}
+
+template <class TT, class TO, int VEC, bool ADD>
+hipError_t fwd_w(const EmbedGeo& g, const int32_t* ids, const TT* table, TO* out, hipStream_t s) {
+  const int W = group_width(g.E, VEC);
+  const int64_t per = (int64_t)(256 / W) * FWD_ROWS;
+  int64_t blocks = (g.N + per - 1) / per;
+  if (blocks > 65536) blocks = 65536;
+  const dim3 grid((unsigned)blocks, (unsigned)((g.E + W * VEC - 1) / (W * VEC)));
+#define RUN(X) case X: k_embed_fwd<TT, TO, VEC, X, ADD><<<grid, 256, 0, s>>>(g, ids, table, out); break;
+  switch (W) { RUN(8) RUN(16) RUN(32) RUN(64) }
+#undef RUN
+  return hipGetLastError();
+}
+
+template <class TO, int VEC, int W, bool ADD>
+hipError_t bwd_run(const EmbedGeo& g, const SumGeo& s, const int32_t* keys, const int64_t* rows,
+                   const TO* dout, float* dtable, float* part, hipStream_t st) {
+  const unsigned fill = ADD ? 0u : (unsigned)((g.V + FILL_ROWS - 1) / FILL_ROWS);
+  const dim3 grid((unsigned)s.nblk + fill, (unsigned)s.slices);
+  k_embed_sum<TO, VEC, W, ADD><<<grid, SUM_T, 0, st>>>(g, s, keys, rows, dout, dtable, part);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || s.nblk < 2) return e;
+  k_embed_join<VEC, W, ADD><<<dim3((unsigned)s.nblk, (unsigned)s.slices), SUM_T, 0, st>>>(
+      g, s, keys, part, dtable);
+  return hipGetLastError();
+}
+
+template <class TO, int VEC>
+hipError_t bwd_vec(const EmbedGeo& g, const int32_t* keys, const int64_t* rows, const TO* dout,
+                   float* dtable, float* part, int add, hipStream_t st) {
+  const SumGeo s = sum_geo(g, VEC);
+#define RUN(X)                                                                               \
+  case X:                                                                                    \
+    return add ? bwd_run<TO, VEC, X, true>(g, s, keys, rows, dout, dtable, part, st)         \
+               : bwd_run<TO, VEC, X, false>(g, s, keys, rows, dout, dtable, part, st);
+  switch (s.W) { RUN(8) RUN(16) RUN(32) RUN(64) }
+#undef RUN
+  return hipErrorInvalidValue;
 }
 
 }  // namespace
@@ -76,21 +713,74 @@ __global__ __launch_bounds__(256) void k_embed_bwd(EmbedGeo g, const int32_t* __
 template <class TT, class TO>
 hipError_t launch_embed_fwd(const EmbedGeo& g, const int32_t* ids, const TT* table, TO* out,
                             int accumulate, hipStream_t s) {
-  const unsigned blocks = (unsigned)(g.N < 65536 ? g.N : 65536);
-  if (accumulate) k_embed_fwd<TT, TO, true><<<blocks, 256, 0, s>>>(g, ids, table, out);
-  else k_embed_fwd<TT, TO, false><<<blocks, 256, 0, s>>>(g, ids, table, out);
-  return hipGetLastError();
+  // vectors of 4 or 8 elements: 16 bytes of the narrower type where both sides start on them
+  int vec = vec_of(g, out);
+  constexpr int most = sizeof(TT) < sizeof(TO) ? 16 / sizeof(TT) : 16 / sizeof(TO);
+  if (vec == 4 && most == 8 && sizeof(TO) == 4) {
+    bool ok = g.E % 8 == 0 && fits(table, 16);
+    if (ok) vec = 8;
+  }
+  while (vec > 1 && !fits(table, vec * sizeof(TT) < 16 ? vec * sizeof(TT) : 16)) vec /= 2;
+#define RUN(X)                                                                               \
+  case X:                                                                                    \
+    return accumulate ? fwd_w<TT, TO, X, true>(g, ids, table, out, s)                        \
+                      : fwd_w<TT, TO, X, false>(g, ids, table, out, s);
+  switch (vec) { RUN(1) RUN(2) RUN(4) RUN(8) }
+#undef RUN
+  return hipErrorInvalidValue;
 }
 
-size_t embed_bwd_bytes(const EmbedGeo&) { return 16; }
+size_t embed_bwd_bytes(const EmbedGeo& g) { return embed_ws(g).total; }
 
 template <class TO>
 hipError_t launch_embed_bwd(const EmbedGeo& g, const int32_t* ids, const TO* dout, float* dtable,
-                            int accumulate, void* ws, hipStream_t s) {
-  const unsigned blocks = (unsigned)(g.V < 65536 ? g.V : 65536);
-  if (accumulate) k_embed_bwd<TO, true><<<blocks, 256, 0, s>>>(g, ids, dout, dtable);
-  else k_embed_bwd<TO, false><<<blocks, 256, 0, s>>>(g, ids, dout, dtable);
-  return hipGetLastError();
+                            int accumulate, void* ws, hipStream_t st) {
+  const EmbedWs W = embed_ws(g);
+  char* w = (char*)ws;
+  SortGeo s;
+  s.N = (int32_t)g.N;
+  s.V = g.V;
+  s.nblk = (int32_t)((g.N + SORT_TILE - 1) / SORT_TILE);
+  const int passes = sort_passes(g.V, &s.bits);
+  int64_t* rows = (int64_t*)(w + W.row);
+  const int32_t* keys = ids;
+  hipError_t e = hipSuccess;
+  if (s.nblk == 1) {
+    s.shift = 0;
+    s.first = s.last = 1;
+    int32_t* dst = (int32_t*)(w + W.key[0]);
+    k_sort_small<<<1, SORT_T, 0, st>>>(s, g, passes, ids, dst, rows);
+    e = hipGetLastError();
+    keys = dst;
+  }
+  const int32_t* pos = nullptr;
+  uint32_t* cnt = (uint32_t*)(w + W.cnt);
+  for (int p = 0; s.nblk > 1 && p < passes && e == hipSuccess; ++p) {
+    s.shift = p * s.bits;
+    s.first = p == 0;
+    s.last = p == passes - 1;
+    int32_t* dst = (int32_t*)(w + W.key[p & 1]);
+    int32_t* dstpos = (int32_t*)(w + W.pos[p & 1]);
+    k_sort_count<<<s.nblk, SORT_T, 0, st>>>(s, keys, cnt);
+    if (s.nblk > SORT_FUSE) k_sort_scan<<<((1 << s.bits) + 3) / 4, 256, 0, st>>>(s, cnt);
+    k_sort_place<<<s.nblk, SORT_T, 0, st>>>(s, g, keys, pos, cnt, dst, dstpos, rows);
+    e = hipGetLastError();
+    keys = dst;
+    pos = dstpos;
+  }
+  if (e != hipSuccess) return e;
+  float* part = (float*)(w + W.part);
+  int vec = vec_of(g, dout);
+  while (vec > 1 && !fits(dtable, vec * 4 < 16 ? vec * 4 : 16)) vec /= 2;
+  switch (vec) {
+    case 1: return bwd_vec<TO, 1>(g, keys, rows, dout, dtable, part, accumulate, st);
+    case 2: return bwd_vec<TO, 2>(g, keys, rows, dout, dtable, part, accumulate, st);
+    case 4: return bwd_vec<TO, 4>(g, keys, rows, dout, dtable, part, accumulate, st);
+    case 8:
+      if constexpr (sizeof(TO) == 2)
+        return bwd_vec<TO, 8>(g, keys, rows, dout, dtable, part, accumulate, st);
+  }
+  return hipErrorInvalidValue;
 }
 
 #define FWD(TT, TO)                                                                            \

@@ -13,6 +13,7 @@ constexpr int DISTILL_KMAX = 256;    // most teacher entries of a row
 struct EmbedGeo {
   int64_t N;            // n0 n1 n2
   int64_t stride[3];
+  uint64_t m1, m2;      // floor(2^64 / n1) + 1 and of n2, 0 for 1
   int32_t n1, n2;
   int32_t E, V;
   float scale;

@@ -70,6 +70,8 @@ int embed_check(const tfm_embed* e, tfm::EmbedGeo& g) {
   g.N = (int64_t)rows;
   for (int i = 0; i < 3; ++i) g.stride[i] = e->stride[i];
   g.n1 = e->n[1]; g.n2 = e->n[2];
+  g.m1 = g.n1 > 1 ? ~uint64_t(0) / (uint64_t)g.n1 + 1 : 0;
+  g.m2 = g.n2 > 1 ? ~uint64_t(0) / (uint64_t)g.n2 + 1 : 0;
   g.E = e->E; g.V = e->V;
   g.scale = e->scale;
   return TFM_OK;
