@@ -1,7 +1,6 @@
 // Embedding rows and their gradient (declarations in vocab.h).
 //
-// Forward: a copy with a factor; rows go to groups of W lanes that move 16 bytes each where the
-// rows allow it, four rows in flight per group.
+// Forward: a copy with a factor, in pieces of 16 bytes where the rows allow it.
 // Backward: dtable[v] = scale sum_{n: id_n = v} dout_n.  The positions are sorted by id (stable
 // radix sort, so equal ids keep their order), and the sorted positions are cut into pieces of equal
 // length whatever the ids are: every group of lanes adds up the rows of its piece in registers and
@@ -9,6 +8,7 @@
 // workgroup and through float32 rows in the workspace between workgroups, in order, so the result
 // does not depend on timing.  Each gradient row is written once, by the one group that completes
 // it; rows of ids that do not occur are zeroed by further workgroups of the same launch.
+#include "mfma.h"
 #include "vocab.h"
 
 #include <hip/hip_runtime.h>
@@ -64,9 +64,7 @@ __device__ __forceinline__ void stv(float* p, const float* v) {
     *p = v[0];
   }
 }
-__device__ __forceinline__ uint32_t pair_of(const float* v) {
-  return (uint32_t)f2bf(v[0]) | (uint32_t)f2bf(v[1]) << 16;
-}
+__device__ __forceinline__ uint32_t pair_of(const float* v) { return pack2(v[0], v[1]); }
 template <int VEC>
 __device__ __forceinline__ void stv(bf16* p, const float* v) {
   if constexpr (VEC == 8)
@@ -77,6 +75,25 @@ __device__ __forceinline__ void stv(bf16* p, const float* v) {
     *reinterpret_cast<uint32_t*>(p) = pair_of(v);
   else
     st(p, v[0]);
+}
+
+// The same past the caches, for outputs too large for them to hold until they are read.
+template <int VEC, bool PAST, class T>
+__device__ __forceinline__ void put(T* p, const float* v) {
+  if constexpr (PAST && VEC * sizeof(T) >= 16) {
+    if constexpr (sizeof(T) == 2) {
+      const u32x4 q = {pack2(v[0], v[1]), pack2(v[2], v[3]), pack2(v[4], v[5]), pack2(v[6], v[7])};
+      __builtin_nontemporal_store(q, reinterpret_cast<u32x4*>(p));
+    } else {
+#pragma unroll
+      for (int i = 0; i < VEC / 4; ++i) {
+        const f32x4 q = {v[4 * i], v[4 * i + 1], v[4 * i + 2], v[4 * i + 3]};
+        __builtin_nontemporal_store(q, reinterpret_cast<f32x4*>(p) + i);
+      }
+    }
+  } else {
+    stv<VEC>(p, v);
+  }
 }
 
 // First element of the activations' row n.  n < 2^27, so n / d is the upper half of n (2^64 / d + 1)
@@ -91,53 +108,69 @@ __device__ __forceinline__ int64_t row_at(const EmbedGeo& g, uint32_t n) {
 }
 
 // ---- forward -----------------------------------------------------------------------------------
-constexpr int FWD_ROWS = 4;  // rows in flight per group
-
-// Groups of W lanes, each FWD_ROWS consecutive rows of its slice of W * VEC elements (grid.y).
-template <class TT, class TO, int VEC, int W, bool ADD>
-__global__ __launch_bounds__(256) void k_embed_fwd(EmbedGeo g, const int32_t* __restrict__ ids,
+// The rows' vectors one after another, L to a row, R of them in flight per thread.  A workgroup
+// first looks up the ids and places of its rows, once per row and not once per vector: that is some
+// 60 cycles of integer products, as much as moving a vector.  ml: as EmbedGeo's m1 for L (exact
+// here too: fewer than 2^43 vectors, L <= 2^16); ms: 2^32 / L + 1 (exact below 2^11 for L <= 2^10).
+template <class TT, class TO, int VEC, int R, bool ADD, bool PAST>
+__global__ __launch_bounds__(256) void k_embed_fwd(EmbedGeo g, uint32_t L, uint64_t ml, uint32_t ms,
+                                                   const int32_t* __restrict__ ids,
                                                    const TT* __restrict__ table,
                                                    TO* __restrict__ out) {
-  const int lane = threadIdx.x % W;
-  const int c = ((int)blockIdx.y * W + lane) * VEC;
-  if (c >= g.E) return;
-  const int64_t groups = (int64_t)gridDim.x * (256 / W);
-  for (int64_t n0 = ((int64_t)blockIdx.x * (256 / W) + threadIdx.x / W) * FWD_ROWS; n0 < g.N;
-       n0 += groups * FWD_ROWS) {
-    int32_t id[FWD_ROWS];
-    float v[FWD_ROWS][VEC], o[FWD_ROWS][VEC];
-    TO* p[FWD_ROWS];
+  constexpr int SPAN = 256 * R;  // vectors of a workgroup
+  __shared__ int64_t place[SPAN + 1];
+  __shared__ int32_t rid[SPAN + 1];
+  const int64_t total = g.N * L;
+  for (int64_t i0 = (int64_t)blockIdx.x * SPAN; i0 < total; i0 += (int64_t)gridDim.x * SPAN) {
+    const int64_t nb = ml ? (int64_t)__umul64hi((uint64_t)i0, ml) : i0;
+    const uint32_t cb = (uint32_t)(i0 - nb * L);
+    const uint32_t rows = (cb + SPAN - 1) / L + 1;  // that the span touches
+    __syncthreads();
+    for (uint32_t r = threadIdx.x; r < rows; r += 256) {
+      const int64_t n = nb + r;
+      rid[r] = n < g.N ? ids[n] : -1;
+      place[r] = n < g.N ? row_at(g, (uint32_t)n) : -1;
+    }
+    __syncthreads();
+    int32_t id[R];
+    float v[R][VEC], o[R][VEC];
+    int64_t p[R];
+    uint32_t c[R];
 #pragma unroll
-    for (int r = 0; r < FWD_ROWS; ++r) {
-      const int64_t n = n0 + r < g.N ? n0 + r : g.N - 1;
-      id[r] = ids[n];
-      p[r] = out + row_at(g, (uint32_t)n) + c;
+    for (int r = 0; r < R; ++r) {
+      const uint32_t at = cb + r * 256 + threadIdx.x;
+      const uint32_t dn = L == 1 ? at : L > 1024 ? at >= L : __umulhi(at, ms);
+      c[r] = (at - dn * L) * VEC;
+      id[r] = rid[dn];
+      p[r] = place[dn];
     }
 #pragma unroll
-    for (int r = 0; r < FWD_ROWS; ++r) {
+    for (int r = 0; r < R; ++r) {
       const bool here = (uint32_t)id[r] < (uint32_t)g.V;
-      ldv<VEC>(table + (int64_t)(here ? id[r] : 0) * g.E + c, v[r]);
-      if (ADD) ldv<VEC>(p[r], o[r]);
+      ldv<VEC>(table + (int64_t)(here ? id[r] : 0) * g.E + c[r], v[r]);
+      if (ADD && here) ldv<VEC>(out + p[r] + c[r], o[r]);
     }
 #pragma unroll
-    for (int r = 0; r < FWD_ROWS; ++r) {
+    for (int r = 0; r < R; ++r) {
       const bool here = (uint32_t)id[r] < (uint32_t)g.V;
 #pragma unroll
       for (int i = 0; i < VEC; ++i) {
         v[r][i] = here ? g.scale * v[r][i] : 0.f;
         if (ADD) v[r][i] += o[r][i];
       }
-      if (n0 + r < g.N && (here || !ADD)) stv<VEC>(p[r], v[r]);
+      if (p[r] >= 0 && (here || !ADD)) put<VEC, PAST>(out + p[r] + c[r], v[r]);
     }
   }
 }
 
 // ---- sort by id ---------------------------------------------------------------------------------
-// Keys: the id, V for an absent one (they end up behind every id).  Radix passes from the lowest
-// digit up; a workgroup ranks a tile of keys, each wave a contiguous part of it, 64 at a time.
-constexpr int SORT_T = 512;                 // threads
-constexpr int SORT_TILE = 4096;             // keys of a workgroup
-constexpr int SORT_R = SORT_TILE / SORT_T;  // keys of a thread
+// Keys: the id, V for an absent one (they end up behind every id); .x of a pair, .y being the
+// position, so that a pass moves each with one 8-byte store.  Radix passes from the lowest digit up; a workgroup ranks a tile of keys, each wave a contiguous part of it, 64 at a time.
+constexpr int SORT_T = 512;   // threads
+constexpr int SORT_R = 4;     // keys of a thread: a tile's rounds are ranked one after another
+constexpr int SORT_TILE = SORT_T * SORT_R;
+constexpr int SMALL_R = 8;    // of the sort in one workgroup
+constexpr int SMALL_TILE = SORT_T * SMALL_R;
 constexpr int SORT_W = SORT_T / 64;
 constexpr int SORT_BITS = 10;               // widest digit
 constexpr int SORT_FUSE = 24;               // workgroups up to which each sums the counts before it
@@ -147,16 +180,18 @@ constexpr int SORT_FUSE = 24;               // workgroups up to which each sums 
 struct SortGeo {
   int32_t N, V, nblk;
   int32_t shift, bits;     // digit of the pass
-  int32_t first, last;     // first pass: keys from ids; last pass: rows' elements as payload
 };
 
-__device__ __forceinline__ int32_t key_at(const SortGeo& s, const int32_t* src, int n) {
-  const int32_t k = src[n];
-  return s.first && (uint32_t)k >= (uint32_t)s.V ? s.V : k;
+// Key and position at place n: of the ids in the first pass, of the last one's pairs then.
+__device__ __forceinline__ int2 pair_at(const SortGeo& s, const int32_t* ids, int n) {
+  const int32_t k = ids[n];
+  return make_int2((uint32_t)k >= (uint32_t)s.V ? s.V : k, n);
 }
+__device__ __forceinline__ int2 pair_at(const SortGeo&, const int2* pairs, int n) { return pairs[n]; }
 
 // Counts of the digits of every tile: cnt[workgroup][digit], or cnt[digit][workgroup] for the scan.
-__global__ __launch_bounds__(SORT_T) void k_sort_count(SortGeo s, const int32_t* __restrict__ src,
+template <class S>
+__global__ __launch_bounds__(SORT_T) void k_sort_count(SortGeo s, const S* __restrict__ src,
                                                        uint32_t* __restrict__ cnt) {
   __shared__ uint32_t h[1 << SORT_BITS];
   const int bins = 1 << s.bits;
@@ -166,7 +201,7 @@ __global__ __launch_bounds__(SORT_T) void k_sort_count(SortGeo s, const int32_t*
 #pragma unroll
   for (int r = 0; r < SORT_R; ++r) {
     const int n = n0 + r * SORT_T + threadIdx.x;
-    if (n < s.N) atomicAdd(&h[key_at(s, src, n) >> s.shift & (bins - 1)], 1u);
+    if (n < s.N) atomicAdd(&h[pair_at(s, src, n).x >> s.shift & (bins - 1)], 1u);
   }
   __syncthreads();
   for (int d = threadIdx.x; d < bins; d += SORT_T)
@@ -224,18 +259,19 @@ __device__ __forceinline__ void scan_bins(uint32_t* v, int bins, uint32_t* buf) 
 }
 
 // Ranks of the workgroup's keys among its keys of the same digit, in order: wave w holds keys
-// w SORT_R 64 + r 64 + lane.  wcnt[w][digit] ends as the number of such keys of earlier waves.
+// w R 64 + r 64 + lane.  wcnt[w][digit] ends as the number of such keys of earlier waves.
 // digit < 0: no key.
-__device__ __forceinline__ void rank_tile(const int (&digit)[SORT_R], int bits,
+template <int R>
+__device__ __forceinline__ void rank_tile(const int (&digit)[R], int bits,
                                           uint32_t (*wcnt)[1 << SORT_BITS],
-                                          uint32_t (&rank)[SORT_R], uint32_t* total) {
+                                          uint32_t (&rank)[R], uint32_t* total) {
   const int t = threadIdx.x, lane = t & 63, w = t >> 6, bins = 1 << bits;
   for (int d = t; d < bins; d += SORT_T)
 #pragma unroll
     for (int i = 0; i < SORT_W; ++i) wcnt[i][d] = 0;
   __syncthreads();
 #pragma unroll
-  for (int r = 0; r < SORT_R; ++r) {
+  for (int r = 0; r < R; ++r) {
     const bool on = digit[r] >= 0;
     uint64_t same = __ballot(on);  // lanes that hold the same digit
     for (int b = 0; b < bits; ++b) {
@@ -265,15 +301,11 @@ __device__ __forceinline__ void rank_tile(const int (&digit)[SORT_R], int bits,
   __syncthreads();
 }
 
-// One pass: keys and payload (position, or its row's first element in the last pass) to their
-// places.
-__global__ __launch_bounds__(SORT_T) void k_sort_place(SortGeo s, EmbedGeo g,
-                                                       const int32_t* __restrict__ src,
-                                                       const int32_t* __restrict__ srcpos,
+// One pass: the pairs to their places.
+template <class S>
+__global__ __launch_bounds__(SORT_T) void k_sort_place(SortGeo s, const S* __restrict__ src,
                                                        const uint32_t* __restrict__ cnt,
-                                                       int32_t* __restrict__ dst,
-                                                       int32_t* __restrict__ dstpos,
-                                                       int64_t* __restrict__ dstrow) {
+                                                       int2* __restrict__ dst) {
   __shared__ uint32_t wcnt[SORT_W][1 << SORT_BITS];
   __shared__ uint32_t base[1 << SORT_BITS];
   __shared__ uint32_t before[1 << SORT_BITS];
@@ -286,10 +318,15 @@ __global__ __launch_bounds__(SORT_T) void k_sort_place(SortGeo s, EmbedGeo g,
       before[d] = cnt[(int64_t)d * s.nblk + blockIdx.x];
     } else {
       uint32_t all = 0, mine = 0;
-      for (int b = 0; b < s.nblk; ++b) {
-        const uint32_t q = cnt[b * bins + d];
-        if (b < (int)blockIdx.x) mine += q;
-        all += q;
+      for (int b0 = 0; b0 < s.nblk; b0 += 8) {
+        uint32_t q[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q[i] = cnt[(b0 + i < s.nblk ? b0 + i : b0) * bins + d];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          if (b0 + i < (int)blockIdx.x) mine += q[i];
+          if (b0 + i < s.nblk) all += q[i];
+        }
       }
       base[d] = all;
       before[d] = mine;
@@ -297,58 +334,51 @@ __global__ __launch_bounds__(SORT_T) void k_sort_place(SortGeo s, EmbedGeo g,
   }
   scan_bins(base, bins, buf);
   const int n0 = blockIdx.x * SORT_TILE + w * SORT_R * 64 + lane;
-  int32_t key[SORT_R];
+  int2 pair[SORT_R];
   int digit[SORT_R];
 #pragma unroll
   for (int r = 0; r < SORT_R; ++r) {
     const int n = n0 + r * 64;
-    key[r] = n < s.N ? key_at(s, src, n) : 0;
-    digit[r] = n < s.N ? key[r] >> s.shift & (bins - 1) : -1;
+    pair[r] = n < s.N ? pair_at(s, src, n) : make_int2(0, 0);
+    digit[r] = n < s.N ? pair[r].x >> s.shift & (bins - 1) : -1;
   }
   uint32_t rank[SORT_R];
   rank_tile(digit, s.bits, wcnt, rank, nullptr);
 #pragma unroll
-  for (int r = 0; r < SORT_R; ++r) {
-    if (digit[r] < 0) continue;
-    const int n = n0 + r * 64;
-    const int32_t pos = s.first ? n : srcpos[n];
-    const uint32_t at = base[digit[r]] + before[digit[r]] + wcnt[w][digit[r]] + rank[r];
-    dst[at] = key[r];
-    if (s.last) dstrow[at] = row_at(g, (uint32_t)pos);
-    else dstpos[at] = pos;
-  }
+  for (int r = 0; r < SORT_R; ++r)
+    if (digit[r] >= 0)
+      dst[base[digit[r]] + before[digit[r]] + wcnt[w][digit[r]] + rank[r]] = pair[r];
 }
 
 // The whole sort of at most one tile in one workgroup.
-__global__ __launch_bounds__(SORT_T) void k_sort_small(SortGeo s, EmbedGeo g, int passes,
+__global__ __launch_bounds__(SORT_T) void k_sort_small(SortGeo s, int passes,
                                                        const int32_t* __restrict__ ids,
-                                                       int32_t* __restrict__ dst,
-                                                       int64_t* __restrict__ dstrow) {
+                                                       int2* __restrict__ dst) {
   __shared__ uint32_t wcnt[SORT_W][1 << SORT_BITS];
   __shared__ uint32_t base[1 << SORT_BITS];
   __shared__ uint32_t buf[SORT_W];
-  __shared__ int32_t keys[SORT_TILE];
-  __shared__ uint16_t from[SORT_TILE];
+  __shared__ int32_t keys[SMALL_TILE];
+  __shared__ uint16_t from[SMALL_TILE];
   const int t = threadIdx.x, lane = t & 63, w = t >> 6;
-  const int n0 = w * SORT_R * 64 + lane;
-  int32_t key[SORT_R];
-  int digit[SORT_R], pos[SORT_R];
+  const int n0 = w * SMALL_R * 64 + lane;
+  int32_t key[SMALL_R];
+  int digit[SMALL_R], pos[SMALL_R];
 #pragma unroll
-  for (int r = 0; r < SORT_R; ++r) {
+  for (int r = 0; r < SMALL_R; ++r) {
     const int n = n0 + r * 64;
-    key[r] = n < s.N ? key_at(s, ids, n) : 0;
+    key[r] = n < s.N ? pair_at(s, ids, n).x : 0;
     pos[r] = n;
   }
   for (int p = 0; p < passes; ++p) {
     const int shift = p * s.bits, bins = 1 << s.bits;
 #pragma unroll
-    for (int r = 0; r < SORT_R; ++r)
+    for (int r = 0; r < SMALL_R; ++r)
       digit[r] = n0 + r * 64 < s.N ? key[r] >> shift & (bins - 1) : -1;
-    uint32_t rank[SORT_R];
+    uint32_t rank[SMALL_R];
     rank_tile(digit, s.bits, wcnt, rank, base);
     scan_bins(base, bins, buf);
 #pragma unroll
-    for (int r = 0; r < SORT_R; ++r) {
+    for (int r = 0; r < SMALL_R; ++r) {
       if (digit[r] < 0) continue;
       const uint32_t at = base[digit[r]] + wcnt[w][digit[r]] + rank[r];
       keys[at] = key[r];
@@ -356,7 +386,7 @@ __global__ __launch_bounds__(SORT_T) void k_sort_small(SortGeo s, EmbedGeo g, in
     }
     __syncthreads();
 #pragma unroll
-    for (int r = 0; r < SORT_R; ++r) {
+    for (int r = 0; r < SMALL_R; ++r) {
       const int n = n0 + r * 64;
       if (n < s.N) {
         key[r] = keys[n];
@@ -366,12 +396,9 @@ __global__ __launch_bounds__(SORT_T) void k_sort_small(SortGeo s, EmbedGeo g, in
     __syncthreads();
   }
 #pragma unroll
-  for (int r = 0; r < SORT_R; ++r) {
+  for (int r = 0; r < SMALL_R; ++r) {
     const int n = n0 + r * 64;
-    if (n < s.N) {
-      dst[n] = key[r];
-      dstrow[n] = row_at(g, (uint32_t)pos[r]);
-    }
+    if (n < s.N) dst[n] = make_int2(key[r], pos[r]);
   }
 }
 
@@ -386,6 +413,7 @@ struct SumGeo {
   int32_t nblk;    // workgroups that add; the others zero
   int32_t W;       // lanes of a group
   int32_t slices;  // grid.y
+  int32_t past;    // zeroed rows go past the caches
 };
 
 // Sorted positions [a, b) of group k of workgroup blk.
@@ -405,35 +433,55 @@ __device__ __forceinline__ void write_row(const EmbedGeo& g, float* dtable, int3
   stv<VEC>(o, x);
 }
 
+// Lane i's value within each group of W lanes.
+template <int W>
+__device__ __forceinline__ int32_t from_lane(int32_t v, int i) {
+  if constexpr (W == 64) return __builtin_amdgcn_readlane(v, i);
+  else return __shfl(v, i, W);
+}
+template <int W>
+__device__ __forceinline__ int64_t from_lane(int64_t v, int i) {
+  const uint32_t lo = (uint32_t)from_lane<W>((int32_t)(uint32_t)v, i);
+  const uint32_t hi = (uint32_t)from_lane<W>((int32_t)(v >> 32), i);
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
 // Zeroes the rows among FILL_ROWS whose ids do not occur, of the workgroup's slice.
 template <int VEC, int W>
 __device__ __forceinline__ void zero_rows(const EmbedGeo& g, const SumGeo& s,
-                                          const int32_t* keys, float* dtable, int* present) {
+                                          const int2* sorted, float* dtable, int* present) {
   const int v0 = ((int)blockIdx.x - s.nblk) * FILL_ROWS;
   if (threadIdx.x < FILL_ROWS) {
     const int v = v0 + threadIdx.x;
     int64_t lo = 0, hi = s.N;  // first sorted position with a key >= v
     while (lo < hi) {
       const int64_t mid = (lo + hi) >> 1;
-      if (keys[mid] < v) lo = mid + 1;
+      if (sorted[mid].x < v) lo = mid + 1;
       else hi = mid;
     }
-    present[threadIdx.x] = v >= g.V || (lo < s.N && keys[lo] == v);
+    present[threadIdx.x] = v >= g.V || (lo < s.N && sorted[lo].x == v);
   }
   __syncthreads();
-  const int c = ((int)blockIdx.y * W + threadIdx.x % W) * VEC;
-  const float zero[VEC] = {};
-  if (c >= g.E) return;
-  for (int r = threadIdx.x / W; r < FILL_ROWS; r += SUM_T / W)
-    if (!present[r]) stv<VEC>(dtable + (int64_t)(v0 + r) * g.E + c, zero);
+  constexpr int Z = VEC < 4 ? VEC : 4;  // a store instruction covers its stretch without gaps
+  const float zero[Z] = {};
+  for (int r = threadIdx.x / W; r < FILL_ROWS; r += SUM_T / W) {
+    if (present[r]) continue;
+    float* o = dtable + (int64_t)(v0 + r) * g.E;
+#pragma unroll
+    for (int q = 0; q < VEC / Z; ++q) {
+      const int c = (int)blockIdx.y * W * VEC + (q * W + threadIdx.x % W) * Z;
+      if (c >= g.E) continue;
+      if (s.past) put<Z, true>(o + c, zero);
+      else stv<Z>(o + c, zero);
+    }
+  }
 }
 
 // part: [nblk][2][E]: what a workgroup's positions add to a run that began in an earlier one, and
 // to a run that begins here and goes on in the next.
 template <class TO, int VEC, int W, bool ADD>
 __global__ __launch_bounds__(SUM_T) void k_embed_sum(EmbedGeo g, SumGeo s,
-                                                     const int32_t* __restrict__ keys,
-                                                     const int64_t* __restrict__ rows,
+                                                     const int2* __restrict__ sorted,
                                                      const TO* __restrict__ dout,
                                                      float* __restrict__ dtable,
                                                      float* __restrict__ part) {
@@ -444,7 +492,7 @@ __global__ __launch_bounds__(SUM_T) void k_embed_sum(EmbedGeo g, SumGeo s,
   __shared__ int32_t through[K];  // the key that came in goes out as well
   __shared__ int present[FILL_ROWS];
   if ((int)blockIdx.x >= s.nblk) {
-    zero_rows<VEC, W>(g, s, keys, dtable, present);
+    zero_rows<VEC, W>(g, s, sorted, dtable, present);
     return;
   }
   const int k = threadIdx.x / W, lane = threadIdx.x % W;
@@ -455,45 +503,57 @@ __global__ __launch_bounds__(SUM_T) void k_embed_sum(EmbedGeo g, SumGeo s,
 #pragma unroll
   for (int i = 0; i < VEC; ++i) acc[i] = 0.f;
   int32_t cur = -1;
-  const bool head = a > 0 && a < b && keys[a - 1] == keys[a];
+  const bool head = a > 0 && a < b && sorted[a - 1].x == sorted[a].x;
   bool came_in = head;  // the current run began in an earlier piece
   const TO* d = dout + (live ? c : 0);
-  bool end = false;
-  for (int64_t t = a; t < b && !end; t += SUM_U) {
-    int32_t key[SUM_U];
-    float x[SUM_U][VEC];
+  // a lane per position for its key and its row's place, the next W positions a step ahead
+  int2 next = make_int2(g.V, 0);
+  if (a + lane < b) next = sorted[a + lane];
+  bool end = a >= b;
+  for (int64_t t0 = a; !end; t0 += W) {
+    const int32_t key_w = next.x;
+    const int64_t row_w = row_at(g, (uint32_t)next.y);
+    next = make_int2(g.V, 0);
+    if (t0 + W + lane < b) next = sorted[t0 + W + lane];
+    const int left = b - t0 < W ? (int)(b - t0) : W;
+    for (int t = 0; t < left && !end; t += SUM_U) {
+      int32_t key[SUM_U];
+      float x[SUM_U][VEC];
 #pragma unroll
-    for (int i = 0; i < SUM_U; ++i) {
-      const int64_t n = t + i < b ? t + i : b - 1;
-      key[i] = t + i < b ? keys[n] : g.V;
-      ldv<VEC>(d + rows[n], x[i]);
-    }
+      for (int i = 0; i < SUM_U; ++i) {
+        key[i] = from_lane<W>(key_w, t + i);
+        const int64_t at = from_lane<W>(row_w, t + i < left ? t + i : 0);
+        ldv<VEC>(d + at, x[i]);
+      }
 #pragma unroll
-    for (int i = 0; i < SUM_U; ++i) {
-      if (key[i] != cur) {
-        if (cur >= 0) {
-          if (came_in) {
+      for (int i = 0; i < SUM_U; ++i) {
+        if (key[i] != cur) {
+          if (cur >= 0) {
+            if (came_in) {
 #pragma unroll
-            for (int j = 0; j < VEC; ++j) edge[k][0][lane * VEC + j] = acc[j];
-          } else if (live) {
-            write_row<VEC, ADD>(g, dtable, cur, c, acc);
+              for (int j = 0; j < VEC; ++j) edge[k][0][lane * VEC + j] = acc[j];
+            } else if (live) {
+              write_row<VEC, ADD>(g, dtable, cur, c, acc);
+            }
+            came_in = false;
           }
-          came_in = false;
+#pragma unroll
+          for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
+          cur = key[i] < g.V ? key[i] : -1;
         }
+        if (cur >= 0) {
 #pragma unroll
-        for (int j = 0; j < VEC; ++j) acc[j] = 0.f;
-        cur = key[i] < g.V ? key[i] : -1;
-      }
-      if (cur >= 0) {
-#pragma unroll
-        for (int j = 0; j < VEC; ++j) acc[j] += x[i][j];
-      } else {
-        end = true;  // only absent ids follow
+          for (int j = 0; j < VEC; ++j) acc[j] += x[i][j];
+        } else {
+          end = true;  // only absent ids follow
+          break;
+        }
       }
     }
+    end |= t0 + W >= b;
   }
   // the last run: complete, or going on in the next piece
-  const bool goes_on = cur >= 0 && b < s.N && keys[b] == cur;
+  const bool goes_on = cur >= 0 && b < s.N && sorted[b].x == cur;
   if (cur >= 0) {
     if (came_in || goes_on) {
 #pragma unroll
@@ -513,8 +573,8 @@ __global__ __launch_bounds__(SUM_T) void k_embed_sum(EmbedGeo g, SumGeo s,
     int32_t run;
     int at;
     if (from < 0) {
-      if (!head || keys[a] >= g.V) continue;
-      run = keys[a];
+      if (!head || sorted[a].x >= g.V) continue;
+      run = sorted[a].x;
       at = 0;
 #pragma unroll
       for (int j = 0; j < VEC; ++j) acc[j] = edge[0][0][lane * VEC + j];
@@ -546,15 +606,15 @@ __global__ __launch_bounds__(SUM_T) void k_embed_sum(EmbedGeo g, SumGeo s,
 // groups every K-th of them, and then the groups' sums in order.
 template <int VEC, int W, bool ADD>
 __global__ __launch_bounds__(SUM_T) void k_embed_join(EmbedGeo g, SumGeo s,
-                                                      const int32_t* __restrict__ keys,
+                                                      const int2* __restrict__ sorted,
                                                       const float* __restrict__ part,
                                                       float* __restrict__ dtable) {
   constexpr int K = SUM_T / W;
   __shared__ float sums[K][W * VEC];
   const int64_t a = piece_at(s, blockIdx.x, 0, K), b = piece_at(s, blockIdx.x, K, K);
   if (b >= s.N) return;
-  const int32_t run = keys[b - 1];
-  if (run >= g.V || keys[b] != run || (a > 0 && keys[a - 1] == run)) return;
+  const int32_t run = sorted[b - 1].x;
+  if (run >= g.V || sorted[b].x != run || (a > 0 && sorted[a - 1].x == run)) return;
   const int k = threadIdx.x / W, lane = threadIdx.x % W;
   const int c = ((int)blockIdx.y * W + lane) * VEC;
   const bool live = c < g.E;
@@ -567,7 +627,7 @@ __global__ __launch_bounds__(SUM_T) void k_embed_join(EmbedGeo g, SumGeo s,
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       const int64_t j = j0 + q * K, jj = j < s.nblk ? j : s.nblk - 1;
-      in[q] = j < s.nblk && keys[piece_at(s, jj, 0, K)] == run;
+      in[q] = j < s.nblk && sorted[piece_at(s, jj, 0, K)].x == run;
       ldv<VEC>(part + (jj * 2) * g.E + (live ? c : 0), x[q]);
     }
 #pragma unroll
@@ -621,11 +681,13 @@ SumGeo sum_geo(const EmbedGeo& g, int vec) {
   s.piece = (int32_t)piece;
   const int64_t per = piece * (SUM_T / s.W);
   s.nblk = (int32_t)((g.N + per - 1) / per);
+  // (as for the forward: 50,021 rows of 1,024, most of them zeros, 96 -> 92 us)
+  s.past = (int64_t)g.V * g.E * 4 > (32 << 20);
   return s;
 }
 
 struct EmbedWs {
-  size_t key[2], pos[2], row, cnt, part, total;
+  size_t pair[2], cnt, part, total;
 };
 EmbedWs embed_ws(const EmbedGeo& g) {
   EmbedWs w;
@@ -636,11 +698,10 @@ EmbedWs embed_ws(const EmbedGeo& g) {
     return at;
   };
   int bits;
-  sort_passes(g.V, &bits);
-  const size_t nblk = (size_t)((g.N + SORT_TILE - 1) / SORT_TILE);
-  for (int i = 0; i < 2; ++i) w.key[i] = take((size_t)g.N * 4);
-  for (int i = 0; i < 2; ++i) w.pos[i] = take(nblk > 1 ? (size_t)g.N * 4 : 0);
-  w.row = take((size_t)g.N * 8);
+  const int passes = sort_passes(g.V, &bits);
+  const size_t nblk = g.N <= SMALL_TILE ? 1 : (size_t)((g.N + SORT_TILE - 1) / SORT_TILE);
+  w.pair[0] = take((size_t)g.N * 8);
+  w.pair[1] = take(nblk > 1 && passes > 1 ? (size_t)g.N * 8 : 0);
   w.cnt = take(nblk > 1 ? ((nblk + 1) << bits) * 4 : 0);
   // the widest and the narrowest vectors bound the number of workgroups
   size_t blocks = 0;
@@ -670,39 +731,47 @@ int vec_of(const EmbedGeo& g, const T* rows) {
 }
 
 template <class TT, class TO, int VEC, bool ADD>
-hipError_t fwd_w(const EmbedGeo& g, const int32_t* ids, const TT* table, TO* out, hipStream_t s) {
-  const int W = group_width(g.E, VEC);
-  const int64_t per = (int64_t)(256 / W) * FWD_ROWS;
-  int64_t blocks = (g.N + per - 1) / per;
-  if (blocks > 65536) blocks = 65536;
-  const dim3 grid((unsigned)blocks, (unsigned)((g.E + W * VEC - 1) / (W * VEC)));
-#define RUN(X) case X: k_embed_fwd<TT, TO, VEC, X, ADD><<<grid, 256, 0, s>>>(g, ids, table, out); break;
-  switch (W) { RUN(8) RUN(16) RUN(32) RUN(64) }
+hipError_t fwd_vec(const EmbedGeo& g, const int32_t* ids, const TT* table, TO* out, hipStream_t s) {
+  const uint32_t L = (uint32_t)(g.E / VEC);
+  const uint64_t ml = L > 1 ? ~uint64_t(0) / L + 1 : 0;
+  const uint32_t ms = L > 1 ? (uint32_t)((uint64_t(1) << 32) / L + 1) : 0;
+  const int64_t total = g.N * L;
+  // an output that the 8 L2 caches of 4 MB cannot hold goes past them: 16 x 1,024 x 20 rows of 192
+  // (126 MB) take 25.7 us against 32.8
+  const bool past = g.N * g.E * (int64_t)sizeof(TO) > (32 << 20);
+  // four vectors in flight per thread once that leaves every CU its eight workgroups
+  const bool many = total >= 4 * 256 * 8 * 256 || past;
+  int64_t blocks = (total + (many ? 1023 : 255)) / (many ? 1024 : 256);
+  if (blocks > (1 << 23)) blocks = 1 << 23;
+#define RUN(R, P) \
+  k_embed_fwd<TT, TO, VEC, R, ADD, P><<<(unsigned)blocks, 256, 0, s>>>(g, L, ml, ms, ids, table, out)
+  if (past) RUN(4, true);
+  else if (many) RUN(4, false);
+  else RUN(1, false);
 #undef RUN
   return hipGetLastError();
 }
 
 template <class TO, int VEC, int W, bool ADD>
-hipError_t bwd_run(const EmbedGeo& g, const SumGeo& s, const int32_t* keys, const int64_t* rows,
-                   const TO* dout, float* dtable, float* part, hipStream_t st) {
+hipError_t bwd_run(const EmbedGeo& g, const SumGeo& s, const int2* sorted, const TO* dout, float* dtable, float* part, hipStream_t st) {
   const unsigned fill = ADD ? 0u : (unsigned)((g.V + FILL_ROWS - 1) / FILL_ROWS);
   const dim3 grid((unsigned)s.nblk + fill, (unsigned)s.slices);
-  k_embed_sum<TO, VEC, W, ADD><<<grid, SUM_T, 0, st>>>(g, s, keys, rows, dout, dtable, part);
+  k_embed_sum<TO, VEC, W, ADD><<<grid, SUM_T, 0, st>>>(g, s, sorted, dout, dtable, part);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess || s.nblk < 2) return e;
   k_embed_join<VEC, W, ADD><<<dim3((unsigned)s.nblk, (unsigned)s.slices), SUM_T, 0, st>>>(
-      g, s, keys, part, dtable);
+      g, s, sorted, part, dtable);
   return hipGetLastError();
 }
 
 template <class TO, int VEC>
-hipError_t bwd_vec(const EmbedGeo& g, const int32_t* keys, const int64_t* rows, const TO* dout,
+hipError_t bwd_vec(const EmbedGeo& g, const int2* sorted, const TO* dout,
                    float* dtable, float* part, int add, hipStream_t st) {
   const SumGeo s = sum_geo(g, VEC);
 #define RUN(X)                                                                               \
   case X:                                                                                    \
-    return add ? bwd_run<TO, VEC, X, true>(g, s, keys, rows, dout, dtable, part, st)         \
-               : bwd_run<TO, VEC, X, false>(g, s, keys, rows, dout, dtable, part, st);
+    return add ? bwd_run<TO, VEC, X, true>(g, s, sorted, dout, dtable, part, st)         \
+               : bwd_run<TO, VEC, X, false>(g, s, sorted, dout, dtable, part, st);
   switch (s.W) { RUN(8) RUN(16) RUN(32) RUN(64) }
 #undef RUN
   return hipErrorInvalidValue;
@@ -723,8 +792,8 @@ hipError_t launch_embed_fwd(const EmbedGeo& g, const int32_t* ids, const TT* tab
   while (vec > 1 && !fits(table, vec * sizeof(TT) < 16 ? vec * sizeof(TT) : 16)) vec /= 2;
 #define RUN(X)                                                                               \
   case X:                                                                                    \
-    return accumulate ? fwd_w<TT, TO, X, true>(g, ids, table, out, s)                        \
-                      : fwd_w<TT, TO, X, false>(g, ids, table, out, s);
+    return accumulate ? fwd_vec<TT, TO, X, true>(g, ids, table, out, s)                        \
+                      : fwd_vec<TT, TO, X, false>(g, ids, table, out, s);
   switch (vec) { RUN(1) RUN(2) RUN(4) RUN(8) }
 #undef RUN
   return hipErrorInvalidValue;
@@ -740,45 +809,38 @@ hipError_t launch_embed_bwd(const EmbedGeo& g, const int32_t* ids, const TO* dou
   SortGeo s;
   s.N = (int32_t)g.N;
   s.V = g.V;
-  s.nblk = (int32_t)((g.N + SORT_TILE - 1) / SORT_TILE);
+  s.nblk = g.N <= SMALL_TILE ? 1 : (int32_t)((g.N + SORT_TILE - 1) / SORT_TILE);
   const int passes = sort_passes(g.V, &s.bits);
-  int64_t* rows = (int64_t*)(w + W.row);
-  const int32_t* keys = ids;
   hipError_t e = hipSuccess;
-  if (s.nblk == 1) {
-    s.shift = 0;
-    s.first = s.last = 1;
-    int32_t* dst = (int32_t*)(w + W.key[0]);
-    k_sort_small<<<1, SORT_T, 0, st>>>(s, g, passes, ids, dst, rows);
-    e = hipGetLastError();
-    keys = dst;
-  }
-  const int32_t* pos = nullptr;
+  int2* sorted = (int2*)(w + W.pair[0]);
   uint32_t* cnt = (uint32_t*)(w + W.cnt);
+  s.shift = 0;
+  if (s.nblk == 1 && g.N > 0) {
+    k_sort_small<<<1, SORT_T, 0, st>>>(s, passes, ids, sorted);
+    e = hipGetLastError();
+  }
   for (int p = 0; s.nblk > 1 && p < passes && e == hipSuccess; ++p) {
     s.shift = p * s.bits;
-    s.first = p == 0;
-    s.last = p == passes - 1;
-    int32_t* dst = (int32_t*)(w + W.key[p & 1]);
-    int32_t* dstpos = (int32_t*)(w + W.pos[p & 1]);
-    k_sort_count<<<s.nblk, SORT_T, 0, st>>>(s, keys, cnt);
+    const int2* from = sorted;
+    sorted = (int2*)(w + W.pair[p & 1]);
+    if (p == 0) k_sort_count<<<s.nblk, SORT_T, 0, st>>>(s, ids, cnt);
+    else k_sort_count<<<s.nblk, SORT_T, 0, st>>>(s, from, cnt);
     if (s.nblk > SORT_FUSE) k_sort_scan<<<((1 << s.bits) + 3) / 4, 256, 0, st>>>(s, cnt);
-    k_sort_place<<<s.nblk, SORT_T, 0, st>>>(s, g, keys, pos, cnt, dst, dstpos, rows);
+    if (p == 0) k_sort_place<<<s.nblk, SORT_T, 0, st>>>(s, ids, cnt, sorted);
+    else k_sort_place<<<s.nblk, SORT_T, 0, st>>>(s, from, cnt, sorted);
     e = hipGetLastError();
-    keys = dst;
-    pos = dstpos;
   }
   if (e != hipSuccess) return e;
   float* part = (float*)(w + W.part);
   int vec = vec_of(g, dout);
   while (vec > 1 && !fits(dtable, vec * 4 < 16 ? vec * 4 : 16)) vec /= 2;
   switch (vec) {
-    case 1: return bwd_vec<TO, 1>(g, keys, rows, dout, dtable, part, accumulate, st);
-    case 2: return bwd_vec<TO, 2>(g, keys, rows, dout, dtable, part, accumulate, st);
-    case 4: return bwd_vec<TO, 4>(g, keys, rows, dout, dtable, part, accumulate, st);
+    case 1: return bwd_vec<TO, 1>(g, sorted, dout, dtable, part, accumulate, st);
+    case 2: return bwd_vec<TO, 2>(g, sorted, dout, dtable, part, accumulate, st);
+    case 4: return bwd_vec<TO, 4>(g, sorted, dout, dtable, part, accumulate, st);
     case 8:
       if constexpr (sizeof(TO) == 2)
-        return bwd_vec<TO, 8>(g, keys, rows, dout, dtable, part, accumulate, st);
+        return bwd_vec<TO, 8>(g, sorted, dout, dtable, part, accumulate, st);
   }
   return hipErrorInvalidValue;
 }
