@@ -70,7 +70,7 @@ def distill_row(s, idx, top, lse, label, tau, alpha, tail):
         lqt = _logsumexp(logq[out])
         D += rest * (np.log(rest) - lqt)
         grad[out] -= rest * np.exp(logq[out] - lqt)
-    loss, grad = alpha * tau * tau * D, alpha * tau * grad
+    loss, grad = alpha * tau * tau * D if alpha else 0.0, alpha * tau * grad
     if 0 <= label < V:
         l1 = s - _logsumexp(s)
         loss -= (1 - alpha) * l1[label]
