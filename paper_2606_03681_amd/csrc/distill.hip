@@ -10,8 +10,10 @@
 //
 // Rows of up to 1,024 classes go to groups of 8 to 64 lanes, longer ones to a workgroup each.
 // Bound by HBM (a read and a write of the logits) from some thousand classes on.
+#include "math64.h"
 #include "mfma.h"
 #include "vocab.h"
+#include "wave.h"
 
 #include <hip/hip_runtime.h>
 
@@ -20,29 +22,27 @@ namespace {
 
 constexpr float LOG2E = 1.44269504088896340736f;
 
-template <int W = 64, class V>
+template <int W, class V>
 __device__ __forceinline__ V group_sum(V v) {
 #pragma unroll
   for (int o = W / 2; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
-template <int W = 64>
+template <int W>
 __device__ __forceinline__ float group_max(float v) {
 #pragma unroll
   for (int o = W / 2; o > 0; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
   return v;
 }
 // Over the NW waves of a workgroup; every thread gets the result.  buf: NW entries.
-template <int NW, class V>
-__device__ __forceinline__ V block_sum(V v, V* buf) {
-  v = group_sum(v);
+template <int NW>
+__device__ __forceinline__ double block_sum(double v, double* buf) {
+  v = wave_sum(v);
   __syncthreads();
   if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
   __syncthreads();
-  V t = buf[0];
-#pragma unroll
-  for (int i = 1; i < NW; ++i) t += buf[i];
-  return t;
+  const int lane = threadIdx.x & 63;
+  return wave_sum(lane < NW ? buf[lane] : 0.0);
 }
 
 // Partial sums of the weights in 64 bits: workgroup b sums a contiguous share.
@@ -51,7 +51,13 @@ __global__ __launch_bounds__(256) void k_distill_weights(const float* __restrict
   __shared__ double buf[4];
   const int64_t a = blockIdx.x * share, b = a + share < N ? a + share : N;
   double acc = 0.0;
-  for (int64_t n = a + threadIdx.x; n < b; n += 256) acc += (double)w[n];
+  for (int64_t n = a + threadIdx.x; n < b; n += 1024) {
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = n + 256 * i < b ? w[n + 256 * i] : 0.f;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) acc += (double)v[i];
+  }
   acc = block_sum<4>(acc, buf);
   if (threadIdx.x == 0) part[blockIdx.x] = acc;
 }
@@ -61,18 +67,20 @@ __device__ __forceinline__ double weight_total(const DistillGeo& g) {
   if (!g.weights) return (double)g.N;
   double s = 0.0;
   for (int i = threadIdx.x & 63; i < g.nwsum; i += 64) s += g.wsum[i];
-  return group_sum(s);
+  return wave_sum(s);
 }
 
 __device__ __forceinline__ int row_classes(const DistillGeo& g, int64_t n) {
   return g.ncls ? min(max(g.ncls[n], 0), g.V) : g.V;
 }
 
-// The row's scalars from its sums, relative to its largest logit m:
+// The row's scalars from its sums:
 //   S_t, S_1    sums of exp((s - mt) / tau) and exp(s - mt) outside J
-//   T_t, T_1    sums of exp((s - m) / tau) and exp(s - m) over J (0 without a tail)
-//   E, G        sums over J of e_j and e_j (log e_j - (s_j - m) / tau), where p_j = e_j / E without
-//               a tail and e_j with one
+//   T_t, T_1    sums of exp((s - mj) / tau) and exp(s - mj) over J (unused without a tail)
+//   E, G        sums over J of e_j and e_j (log e_j - (s_j - mj) / tau), where p_j = e_j / E
+//               without a tail and e_j with one
+// m is the largest of all logits.  W lanes call it with the same values, W >= 8: each evaluates one
+// of the exponentials, of the logarithms and of the quotients.
 struct RowSums {
   double S_t, S_1, T_t, T_1, E, G;
 };
@@ -82,33 +90,51 @@ struct RowOut {
   double j_p, label;  //   - j_p e_j, and of the label: - label
   float c_t, c_1;     // gradient outside J: c_t exp((s - mt) / tau) + c_1 exp(s - mt)
 };
+template <int W>
+__device__ __forceinline__ double of_lane(double v, int i) {
+  if constexpr (W == 64) return from_lane(v, i);
+  else return __shfl(v, i, W);
+}
+template <int W>
 __device__ __forceinline__ RowOut row_scalars(const DistillGeo& g, const RowSums& r, float mt,
-                                              float m, double share, bool known, double s_label) {
+                                              float mj, float m, double share, bool known,
+                                              double s_label) {
+  const int lane = threadIdx.x % W;
   const double tau = g.tau, alpha = g.alpha, itau = 1.0 / tau;
-  const bool some = mt > -INFINITY;
-  const double back = some ? (double)mt - (double)m : 0.0;
-  const double bt = exp(back * itau), b1 = exp(back);
-  const double Zt = r.S_t * bt + r.T_t, Z1 = r.S_1 * b1 + r.T_1;
-  const double lZt = log(Zt);
+  const bool some = mt > -INFINITY, any = mj > -INFINITY;
+  // where mt and mj lie below m
+  const double back = some ? (double)mt - (double)m : 0.0, d = any ? (double)mj - (double)m : 0.0;
+  const double x = exp64((lane & 2 ? d : back) * (lane & 1 ? 1.0 : itau));
+  const double bt = of_lane<W>(x, 0), b1 = of_lane<W>(x, 1);
+  double Zt = r.S_t * bt, Z1 = r.S_1 * b1;
+  if (g.tail && any) {
+    Zt += r.T_t * of_lane<W>(x, 2);
+    Z1 += r.T_1 * of_lane<W>(x, 3);
+  }
   // the teacher's mass: P in the set, pt outside
-  const double norm = g.tail || r.E == 0.0 ? 1.0 : 1.0 / r.E;
-  double P = r.E * norm, pt = 0.0;
-  double D = r.G * norm + lZt * P;
-  if (!g.tail && r.E != 0.0) D -= log(r.E);
+  const double one_over = 1.0 / (lane == 0 ? Zt : lane == 1 ? r.E : lane == 2 ? r.S_t : Z1);
+  const double norm = g.tail || r.E == 0.0 ? 1.0 : of_lane<W>(one_over, 1);
+  const double P = r.E * norm;
+  double pt = 0.0;
   if (g.tail && some) {
     pt = 1.0 - P;
-    if (pt > 0.0) D += pt * (log(pt) - (back * itau + log(r.S_t) - lZt));
-    else if (pt <= 0.0) pt = 0.0;
+    if (pt <= 0.0) pt = 0.0;
   }
+  const double l = log64(lane == 0 ? Zt : lane == 1 ? r.E : lane == 2 ? pt : lane == 3 ? r.S_t : Z1);
+  const double lZt = of_lane<W>(l, 0);
+  double D = (r.G - r.E * d * itau) * norm + lZt * P;
+  if (!g.tail && r.E != 0.0) D -= of_lane<W>(l, 1);
+  const double lp = of_lane<W>(l, 2), lS = of_lane<W>(l, 3), lZ1 = of_lane<W>(l, 4);
+  if (!(pt == 0.0)) D += pt * (lp - (back * itau + lS - lZt));
   RowOut o;
   o.loss = alpha > 0.0 ? alpha * tau * tau * D : 0.0;
   const double cd = alpha * tau * share, cl = known ? (1.0 - alpha) * share : 0.0;
-  if (known) o.loss += (1.0 - alpha) * (log(Z1) - (s_label - (double)m));
-  o.j_q = cd * (P + pt) / Zt;
-  o.j_1 = cl / Z1;
+  if (known) o.loss += (1.0 - alpha) * (lZ1 - (s_label - (double)m));
+  o.j_q = cd * (P + pt) * of_lane<W>(one_over, 0);
+  o.j_1 = cl * of_lane<W>(one_over, 3);
   o.j_p = cd * norm;
   o.label = cl;
-  o.c_t = (float)(o.j_q * bt - (pt > 0.0 ? cd * pt / r.S_t : 0.0));
+  o.c_t = (float)(o.j_q * bt - (pt > 0.0 ? cd * pt * of_lane<W>(one_over, 2) : 0.0));
   o.c_1 = (float)(o.j_1 * b1);
   return o;
 }
@@ -185,13 +211,13 @@ __global__ __launch_bounds__(256) void k_distill_small(DistillGeo g, int64_t fir
       double lt;
       if (g.tail) {
         lt = (double)t[i] * itau - lse;
-        r.T_t += exp(y);
-        r.T_1 += exp(d);
+        r.T_t += exp64(y);
+        r.T_1 += exp64(d);
       } else {
         lt = tm > -INFINITY ? ((double)t[i] - (double)tm) * itau : -INFINITY;
       }
       if (t[i] != t[i]) lt = NAN;
-      e[i] = exp(lt);
+      e[i] = exp64(lt);
       r.E += e[i];
       if (!(e[i] == 0.0)) r.G += e[i] * (lt - y);
     }
@@ -212,7 +238,7 @@ __global__ __launch_bounds__(256) void k_distill_small(DistillGeo g, int64_t fir
     if (lane + W * i == y) sy = x[i];
   sy = __shfl(sy, known ? y % W : 0, W);
   const double share = wtot != 0.0 ? (double)wn / wtot : 0.0;
-  const RowOut o = row_scalars(g, r, mt, m, share, known, (double)sy);
+  const RowOut o = row_scalars<W>(g, r, mt, m, m, share, known, (double)sy);
   if (mine && lane == 0) g.row_loss[n] = left_out ? 0.f : (float)o.loss;
   if (dlogits && mine) {
     T* ds = dlogits + n * g.ld;
@@ -224,8 +250,8 @@ __global__ __launch_bounds__(256) void k_distill_small(DistillGeo g, int64_t fir
       if (!left_out && v < V) {
         if (in[i]) {
           const double dx = (double)x[i] - (double)m;
-          double q = o.j_q * exp(dx * itau) - o.j_p * e[i];
-          if (known) q += o.j_1 * exp(dx) - (v == y ? o.label : 0.0);
+          double q = o.j_q * exp64(dx * itau) - o.j_p * e[i];
+          if (known) q += o.j_1 * exp64(dx) - (v == y ? o.label : 0.0);
           d = (float)q;
         } else {
           d = o.c_t * exp2_hw((x[i] - mr) * c);
@@ -237,9 +263,15 @@ __global__ __launch_bounds__(256) void k_distill_small(DistillGeo g, int64_t fir
   }
 }
 
+// Most rows that are split, and the fewest classes.  The second launch and the hand-over take 4 us;
+// bf16, k = 64, split against whole: 1 x 16,384 15.1 / 14.1 us, 1 x 32,768 15.1 / 19.7, 64 x 32,768
+// 17.5 / 20.8, 64 x 131,072 24.8 / 31.1, 128 x 131,072 38.6 / 33.7.
+constexpr int64_t SPLIT_ROWS = 64;
+constexpr int32_t SPLIT_V = 24576;
+
 // ---- longer rows ---------------------------------------------------------------------------------
-// A row in pieces of 16 bytes on 16-byte boundaries; its first class may lie `skip` elements into
-// the first piece.
+// Pieces of 16 bytes on 16-byte boundaries; what a row has before the first and behind the last of
+// them (at most 14 classes) goes to a thread each.
 template <class T>
 struct Piece {
   static constexpr int E = 16 / sizeof(T);
@@ -250,234 +282,314 @@ struct Piece {
     else return __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
   }
 };
-
-// Classes e0 .. of a row of V; -inf where there are none.
-template <class T>
-__device__ __forceinline__ Piece<T> load_piece(const T* s, int e0, int V) {
-  Piece<T> p;
-  if (e0 >= 0 && e0 + Piece<T>::E <= V) {
-    p.u = *reinterpret_cast<const uint4*>(s + e0);
-  } else {
-    uint32_t w[4];
-#pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      if constexpr (sizeof(T) == 4) {
-        const int e = e0 + q;
-        w[q] = e >= 0 && e < V ? __float_as_uint(s[e]) : 0xff800000u;
-      } else {
-        const int e = e0 + 2 * q;
-        const uint32_t lo = e >= 0 && e < V ? s[e] : 0xff80u;
-        const uint32_t hi = e + 1 >= 0 && e + 1 < V ? s[e + 1] : 0xff80u;
-        w[q] = lo | hi << 16;
-      }
-    }
-    p.u = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-  return p;
+__device__ __forceinline__ void store_piece(float* p, const float* d) {
+  *reinterpret_cast<float4*>(p) = make_float4(d[0], d[1], d[2], d[3]);
 }
-template <class T>
-__device__ __forceinline__ void store_piece(T* ds, int e0, int V, bool whole, const float* d) {
-  constexpr int E = Piece<T>::E;
-  if (whole && e0 >= 0 && e0 + E <= V) {
-    if constexpr (sizeof(T) == 4)
-      *reinterpret_cast<float4*>(ds + e0) = make_float4(d[0], d[1], d[2], d[3]);
-    else
-      *reinterpret_cast<uint4*>(ds + e0) =
-          make_uint4(pack2(d[0], d[1]), pack2(d[2], d[3]), pack2(d[4], d[5]), pack2(d[6], d[7]));
-  } else {
-#pragma unroll
-    for (int j = 0; j < E; ++j)
-      if (e0 + j >= 0 && e0 + j < V) st(ds + e0 + j, d[j]);
-  }
+__device__ __forceinline__ void store_piece(bf16* p, const float* d) {
+  *reinterpret_cast<uint4*>(p) =
+      make_uint4(pack2(d[0], d[1]), pack2(d[2], d[3]), pack2(d[4], d[5]), pack2(d[6], d[7]));
 }
 
-// One workgroup of TH threads per row, I pieces per thread in registers (I = 0: read again for each
-// of the three passes: rows that the registers of a CU do not hold).  TWO: the label's softmax has
-// another temperature than the teacher's, a second exponential per class.
-template <class T, int TH, int I, bool TWO>
-__global__ __launch_bounds__(TH) void k_distill_rows(DistillGeo g, int64_t first, const T* logits,
-                                                     T* dlogits) {
+// What the two launches of a split row hand on (see k_distill_rows): of a part, and of J.
+struct PartSums {
+  double S_t, S_1;  // relative to mt
+  float mt, pad;
+};
+struct SetSums {
+  double E, G, T_t, T_1;
+  float mj, tm;
+  float s_label, pad;
+};
+struct SetEntry {
+  int32_t idx;  // -1: none
+  float s;      // its logit (the gradient may be written over the logits)
+};
+struct Split {
+  PartSums* part;   // [N][parts]
+  SetSums* set;     // [N]
+  SetEntry* entry;  // [N][k]
+  int32_t parts, len;
+};
+enum { WHOLE = 0, SUM = 1, APPLY = 2 };
+
+// TH threads, I pieces per thread in registers.  WHOLE: one workgroup per row.  Few long rows are
+// split into `parts` of `len` classes, a workgroup each, in two launches: SUM leaves every part's
+// sums (and one more workgroup the set's), APPLY joins them and writes the part's gradients.  I = 0: rows that
+// the registers of a CU do not hold, read again for each of the three passes, and (dlogits not
+// aligned as logits) rows written class by class.  TWO: the label's softmax has another temperature
+// than the teacher's, a second exponential per class.
+template <class T, int TH, int I, bool TWO, int STAGE>
+__global__ __launch_bounds__(TH, I == 32 ? 3 : 1) void k_distill_rows(DistillGeo g, Split sp,
+                                                                      int64_t first,
+                                                                      const T* logits, T* dlogits) {
   constexpr int E = Piece<T>::E, NW = TH / 64;
-  extern __shared__ uint32_t inside[];  // a bit per class from the first piece on: in J
-  __shared__ int32_t jidx[DISTILL_KMAX];
+  extern __shared__ uint32_t inside[];  // a bit per class, the first piece's from bit 0 on: in J
+  __shared__ alignas(16) int32_t jidx[DISTILL_KMAX];
   __shared__ float fbuf[3][NW];
   __shared__ double dbuf[6][NW];
   __shared__ RowOut row;
+  __shared__ float row_mt, row_m;
   __shared__ int again, label_in;
-  const int tid = threadIdx.x, lane = tid & 63, w = tid >> 6;
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
   const double itau = 1.0 / (double)g.tau;
   const float c = LOG2E / g.tau;
-  const int64_t n = first + blockIdx.x;
+  const int64_t n = first + (STAGE ? blockIdx.y : blockIdx.x);
   const T* s = logits + n * g.ld;
   T* ds = dlogits ? dlogits + n * g.ld : nullptr;
   const float wn = g.weights ? g.weights[n] : 1.f;
   const int V = row_classes(g, n);
-  const int skip = (int)((uintptr_t)s % 16 / sizeof(T));
-  const int np = (g.V + skip + E - 1) / E;
-  // in whole pieces too where they lie as the logits' do
-  const bool whole = ds && (uintptr_t)ds % 16 == (uintptr_t)s % 16;
-  float zero[E] = {};
-  if (wn == 0.f || V == 0) {
+  // this workgroup's classes [lo, hi)
+  const int part = STAGE ? (int)blockIdx.x : 0;
+  const int lo = STAGE ? min(part * sp.len, V) : 0, hi = STAGE ? min(lo + sp.len, V) : V;
+  // classes before the first piece
+  const int lead = min((int)(-(uintptr_t)(s + lo) % 16 / sizeof(T)), hi - lo);
+  const int np = (hi - lo - lead) / E;
+  // pieces lie at a uniform base plus a 32-bit offset (a 64-bit address each would cost registers)
+  const char* s0 = reinterpret_cast<const char*>(s + lo + lead);
+  char* ds0 = reinterpret_cast<char*>(ds + lo + lead);
+  const uint32_t off = tid * 16u;
+  // the class beside the pieces that this thread looks after, hi: none
+  const int odd = tid < lead ? lo + tid : min(lo + tid + np * E, hi);
+  // dlogits may lie otherwise than logits (I = 0 then)
+  const bool whole = I > 0 || (uintptr_t)ds % 16 == (uintptr_t)s % 16;
+  // zeros for the classes from v0 on
+  auto zero_from = [&](int v0) __attribute__((always_inline)) {
+    const int end = STAGE ? min((part + 1) * sp.len, g.V) : g.V;
     if (ds)
-      for (int v = tid; v < np; v += TH) store_piece(ds, v * E - skip, g.V, whole, zero);
-    if (tid == 0) g.row_loss[n] = 0.f;
+      for (int v = v0 + tid; v < end; v += TH) st(ds + v, 0.f);
+  };
+  if (wn == 0.f || V == 0) {
+    if (STAGE == SUM) return;
+    zero_from(STAGE ? part * sp.len : 0);
+    if (part == 0 && tid == 0) g.row_loss[n] = 0.f;
     return;
   }
-  // the teacher's entries first, the row behind them
+  // the teacher's entries
   int my = -1;
-  float tj = -INFINITY;
-  if (tid < g.k) {
-    my = g.idx[n * g.k + tid];
-    tj = g.top[n * g.k + tid];
-    if (my < 0 || my >= V) my = -1;
-  }
+  float tj = -INFINITY, sj = -INFINITY, sy = -INFINITY, mj, tm;
   const int y = g.labels ? g.labels[n] : -1;
   const bool known = y >= 0 && y < V;
-  const float sj = my >= 0 ? ld(s + my) : -INFINITY;
-  const float sy = known ? ld(s + y) : -INFINITY;
+  const float lse = g.tail ? g.lse[n] : 0.f;
+  if (tid < g.k) tj = g.top[n * g.k + tid];
+  if (STAGE == APPLY) {
+    if (tid < g.k) {
+      const SetEntry e = sp.entry[n * g.k + tid];
+      my = e.idx;
+      sj = e.s;
+    }
+    mj = sp.set[n].mj;
+    tm = sp.set[n].tm;
+    sy = sp.set[n].s_label;
+  } else {
+    if (tid < g.k) my = g.idx[n * g.k + tid];
+    if (my < 0 || my >= V) my = -1;
+    if (my >= 0) sj = ld(s + my);
+    if (known) sy = ld(s + y);
+  }
+  // bit of class v: shifted to where the first piece starts a word
+  const int shift = 32 - lead - lo;
+  for (int v = tid; v < (hi + shift + 31) / 32; v += TH) inside[v] = 0;
+  if (tid == 0) {
+    again = STAGE == SUM;  // (the set's workgroup has no bits to go by)
+    label_in = 0;
+  }
+  if (tid < DISTILL_KMAX) jidx[tid] = my;
+  __syncthreads();
+  if (my >= lo && my < hi) {
+    const uint32_t bit = 1u << ((my + shift) & 31);
+    if (atomicOr(&inside[(my + shift) >> 5], bit) & bit) again = 1;
+    if (my == y) label_in = 1;
+  }
+  __syncthreads();
+  // log e_j of this thread's entry (RowSums)
+  auto log_e = [&]() __attribute__((always_inline)) {
+    if (tj != tj) return (double)NAN;
+    if (g.tail) return (double)tj * itau - (double)lse;
+    return tm > -INFINITY ? ((double)tj - (double)tm) * itau : (double)-INFINITY;
+  };
+  if (STAGE == WHOLE || (STAGE == SUM && part == sp.parts)) {
+    if (again) {  // perhaps a repeated class: its first entry counts
+      bool earlier = false;
+      for (int j = 0; j < g.k; j += 16) {
+#pragma unroll
+        for (int q = 0; q < 16; q += 4) {
+          const int4 v = *reinterpret_cast<const int4*>(jidx + j + q);
+          earlier |= (v.x == my && j + q < tid) || (v.y == my && j + q + 1 < tid) ||
+                     (v.z == my && j + q + 2 < tid) || (v.w == my && j + q + 3 < tid);
+        }
+      }
+      if (earlier) my = -1;
+    }
+    // J's maxima, and its sums relative to them: done before the row arrives, so that their
+    // registers are free when it does
+    if (my < 0) tj = -INFINITY;
+    mj = wave_max(my >= 0 ? sj : -INFINITY);
+    tm = wave_max(tj);
+    if (lane == 0) {
+      fbuf[0][w] = mj;
+      fbuf[1][w] = tm;
+    }
+    __syncthreads();
+    mj = wave_max(lane < NW ? fbuf[0][lane] : -INFINITY);
+    tm = wave_max(lane < NW ? fbuf[1][lane] : -INFINITY);
+    double q[4] = {0.0, 0.0, 0.0, 0.0};
+    if (w * 64 < g.k) {  // the waves that hold entries
+      if (my >= 0) {
+        const double d = mj > -INFINITY ? (double)sj - (double)mj : (double)sj, lt = log_e();
+        q[0] = exp64(lt);
+        if (!(q[0] == 0.0)) q[1] = q[0] * (lt - d * itau);
+        q[2] = exp64(d * itau);
+        q[3] = TWO ? exp64(d) : q[2];
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) q[i] = wave_sum(q[i]);
+    }
+    if (lane == 0)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) dbuf[2 + i][w] = q[i];
+    if (STAGE == SUM) {
+      if (tid < g.k) sp.entry[n * g.k + tid] = {my, sj};
+      __syncthreads();
+      if (w == 0) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) q[i] = wave_sum(lane < NW ? dbuf[2 + i][lane] : 0.0);
+        if (lane == 0) sp.set[n] = {q[0], q[1], q[2], q[3], mj, tm, sy, 0.f};
+      }
+      return;
+    }
+  }
   Piece<T> x[I > 0 ? I : 1];
   if constexpr (I > 0) {
 #pragma unroll
     for (int i = 0; i < I; ++i)
-      if (i * TH + tid < np) x[i] = load_piece(s, (i * TH + tid) * E - skip, V);
+      if (i * TH + tid < np) x[i].u = *reinterpret_cast<const uint4*>(s0 + i * TH * 16 + off);
   }
+  const float xo = odd < hi ? ld(s + odd) : -INFINITY;
   auto each = [&](auto f) __attribute__((always_inline)) {
     if constexpr (I > 0) {
 #pragma unroll
       for (int i = 0; i < I; ++i)
-        if (i * TH + tid < np) f(x[i], i * TH + tid);
+        if (i * TH + tid < np) f(x[i], i * TH);
     } else {
-      for (int v = tid; v < np; v += TH) f(load_piece(s, v * E - skip, V), v);
+      for (int v0 = 0; v0 + tid < np; v0 += TH) {
+        x[0].u = *reinterpret_cast<const uint4*>(s0 + v0 * 16 + off);
+        f(x[0], v0);
+      }
     }
   };
-  for (int v = tid; v < (np * E + 31) / 32; v += TH) inside[v] = 0;
-  if (tid == 0) again = label_in = 0;
-  if (tid < DISTILL_KMAX) jidx[tid] = my;
-  __syncthreads();
-  if (my >= 0) {
-    const uint32_t bit = 1u << ((my + skip) & 31);
-    if (atomicOr(&inside[(my + skip) >> 5], bit) & bit) again = 1;
-    if (my == y) label_in = 1;
-  }
-  __syncthreads();
-  if (again) {  // a repeated class: its first entry counts
-    for (int j = 0; j < tid && my >= 0; ++j)
-      if (jidx[j] == my) my = -1;
-  }
-  if (my < 0) tj = -INFINITY;
-  // bits of piece v's classes that the sums leave out
-  auto out_of = [&](int v) __attribute__((always_inline)) -> uint32_t {
-    if (!g.tail) return 0u;
-    const uint32_t byte = reinterpret_cast<const uint8_t*>(inside)[v * E >> 3];
-    return E == 8 ? byte : byte >> (v & 1) * 4 & 15u;
-  };
-  // maxima: of the classes that are summed, of J's logits, of the teacher's
-  float mt = -INFINITY;
-  each([&](const Piece<T>& p, int v) __attribute__((always_inline)) {
-    const uint32_t o = out_of(v);
-    if (o == 0) {
+  float mt, m;
+  if (STAGE != APPLY) {
+    // f for every class that the sums do not leave out
+    auto each_summed = [&](auto f) __attribute__((always_inline)) {
+      each([&](const Piece<T>& p, int v0) __attribute__((always_inline)) {
+        uint32_t o = 0;
+        if (g.tail) {
+          o = reinterpret_cast<const uint8_t*>(inside + 1)[(v0 * E >> 3) + (tid * E >> 3)];
+          if (E == 4) o = o >> (tid & 1) * 4 & 15u;
+        }
+        if (o == 0) {
 #pragma unroll
-      for (int j = 0; j < E; ++j) mt = fmaxf(mt, p.get(j));
-    } else {
+          for (int j = 0; j < E; ++j) f(p.get(j));
+        } else {
 #pragma unroll
-      for (int j = 0; j < E; ++j) mt = fmaxf(mt, o >> j & 1 ? -INFINITY : p.get(j));
-    }
-  });
-  mt = group_max(mt);
-  const float mj = group_max(my >= 0 ? sj : -INFINITY), tj_m = group_max(tj);
-  if (lane == 0) {
-    fbuf[0][w] = mt;
-    fbuf[1][w] = mj;
-    fbuf[2][w] = tj_m;
-  }
-  __syncthreads();
-  // (a lane per wave's value: NW of them held at once would cost the registers of the row)
-  mt = group_max<NW>(fbuf[0][lane % NW]);
-  float m = group_max<NW>(fbuf[1][lane % NW]);
-  const float tm = group_max<NW>(fbuf[2][lane % NW]);
-  m = fmaxf(m, mt);
-  if (m == -INFINITY) {  // nothing to learn from
-    if (ds)
-      for (int v = tid; v < np; v += TH) store_piece(ds, v * E - skip, g.V, whole, zero);
-    if (tid == 0) g.row_loss[n] = 0.f;
-    return;
-  }
-  const float mr = mt > -INFINITY ? mt : 0.f;
-  // sums
-  float sum_t = 0.f, sum_1 = 0.f;
-  each([&](const Piece<T>& p, int v) __attribute__((always_inline)) {
-    const uint32_t o = out_of(v);
-#pragma unroll
-    for (int j = 0; j < E; ++j) {
-      const float d = (o >> j & 1 ? -INFINITY : p.get(j)) - mr;
+          for (int j = 0; j < E; ++j) f(o >> j & 1 ? -INFINITY : p.get(j));
+        }
+      });
+      if (odd < hi && !(g.tail && inside[(odd + shift) >> 5] >> ((odd + shift) & 31) & 1)) f(xo);
+    };
+    mt = -INFINITY;
+    each_summed([&](float v) __attribute__((always_inline)) { mt = fmaxf(mt, v); });
+    mt = wave_max(mt);
+    if (lane == 0) fbuf[2][w] = mt;
+    __syncthreads();
+    mt = wave_max(lane < NW ? fbuf[2][lane] : -INFINITY);
+    const float mr = mt > -INFINITY ? mt : 0.f;
+    float sum_t = 0.f, sum_1 = 0.f;
+    each_summed([&](float v) __attribute__((always_inline)) {
+      const float d = v - mr;
       sum_t += exp2_hw(d * c);
       if (TWO) sum_1 += exp2_hw(d * LOG2E);
+    });
+    const double S = wave_sum((double)sum_t), S1 = TWO ? wave_sum((double)sum_1) : S;
+    if (lane == 0) {
+      dbuf[0][w] = S;
+      dbuf[1][w] = S1;
     }
-  });
-  double e = 0.0, xj = 0.0, ex_t = 0.0, ex_1 = 0.0, G = 0.0;
-  if (w * 64 < g.k) {  // the waves that hold entries
-    if (my >= 0) {
-      const double d = (double)sj - (double)m;
-      xj = d * itau;
-      double lt;
-      if (g.tail) lt = (double)tj * itau - (double)g.lse[n];
-      else lt = tm > -INFINITY ? ((double)tj - (double)tm) * itau : -INFINITY;
-      if (tj != tj) lt = NAN;
-      e = exp(lt);
-      ex_t = exp(xj);
-      ex_1 = exp(d);
-      if (!(e == 0.0)) G = e * (lt - xj);
-    }
-    const double q[4] = {group_sum(e), group_sum(G), group_sum(ex_t), group_sum(ex_1)};
-    if (lane == 0)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) dbuf[2 + i][w] = q[i];
-  } else if (lane == 0) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) dbuf[2 + i][w] = 0.0;
+    __syncthreads();
   }
-  const double S = group_sum((double)sum_t), S1 = TWO ? group_sum((double)sum_1) : S;
-  if (lane == 0) {
-    dbuf[0][w] = S;
-    dbuf[1][w] = S1;
-  }
-  __syncthreads();
   if (w == 0) {
     double q[6];
 #pragma unroll
-    for (int i = 0; i < 6; ++i) q[i] = group_sum<NW>(dbuf[i][lane % NW]);
+    for (int i = 0; i < (STAGE == SUM ? 2 : 6); ++i)
+      if (STAGE != APPLY) q[i] = wave_sum(lane < NW ? dbuf[i][lane] : 0.0);
+    if (STAGE == SUM) {
+      if (lane == 0) sp.part[n * sp.parts + part] = {q[0], q[1], mt, 0.f};
+      return;
+    }
+    if (STAGE == APPLY) {  // the parts' sums relative to their largest logit
+      const bool on = lane < sp.parts;
+      const PartSums ps = sp.part[n * sp.parts + (on ? lane : 0)];
+      mt = wave_max(on ? ps.mt : -INFINITY);
+      const double d = ps.mt > -INFINITY ? (double)ps.mt - (double)mt : 0.0;
+      q[0] = wave_sum(on ? ps.S_t * exp64(d * itau) : 0.0);
+      q[1] = TWO ? wave_sum(on ? ps.S_1 * exp64(d) : 0.0) : q[0];
+      const SetSums ss = sp.set[n];
+      q[2] = ss.E; q[3] = ss.G; q[4] = ss.T_t; q[5] = ss.T_1;
+    }
+    m = fmaxf(mj, mt);
     const double wtot = weight_total(g);
-    const RowSums r = {q[0], q[1], g.tail ? q[4] : 0.0, g.tail ? q[5] : 0.0, q[2], q[3]};
-    const RowOut o = row_scalars(g, r, mt, m, wtot != 0.0 ? (double)wn / wtot : 0.0, known,
-                                 (double)sy);
+    const RowSums r = {q[0], q[1], q[4], q[5], q[2], q[3]};
+    const RowOut o = row_scalars<64>(g, r, mt, mj, m, wtot != 0.0 ? (double)wn / wtot : 0.0,
+                                     known, (double)sy);
     if (lane == 0) {
       row = o;
-      g.row_loss[n] = (float)o.loss;
+      row_mt = mt;
+      row_m = m;
+      if (part == 0) g.row_loss[n] = m == -INFINITY ? 0.f : (float)o.loss;
     }
   }
+  if (STAGE == SUM) return;
   __syncthreads();
-  if (ds) {
-    const float ct = TWO ? row.c_t : row.c_t + row.c_1, c1 = row.c_1;
-    each([&](const Piece<T>& p, int v) __attribute__((always_inline)) {
-      float d[E];
+  mt = row_mt;
+  m = row_m;
+  if (!ds) return;
+  if (m == -INFINITY) {  // nothing to learn from
+    zero_from(STAGE ? part * sp.len : 0);
+    return;
+  }
+  const float mr = mt > -INFINITY ? mt : 0.f;
+  const float ct = TWO ? row.c_t : row.c_t + row.c_1, c1 = row.c_1;
+  auto gradient = [&](float v) __attribute__((always_inline)) {
+    const float z = v - mr;
+    float d = ct * exp2_hw(z * c);
+    if (TWO) d += c1 * exp2_hw(z * LOG2E);
+    return d;
+  };
+  each([&](const Piece<T>& p, int v0) __attribute__((always_inline)) {
+    float d[E];
 #pragma unroll
-      for (int j = 0; j < E; ++j) {
-        const float z = p.get(j) - mr;
-        d[j] = ct * exp2_hw(z * c);
-        if (TWO) d[j] += c1 * exp2_hw(z * LOG2E);
-      }
-      store_piece(ds, v * E - skip, g.V, whole, d);
-    });
-    __syncthreads();
-    // then J's classes and the label's
-    if (my >= 0) {
-      const double q = row.j_q * ex_t + row.j_1 * ex_1 - row.j_p * e - (my == y ? row.label : 0.0);
-      st(ds + my, (float)q);
+    for (int j = 0; j < E; ++j) d[j] = gradient(p.get(j));
+    T* at = reinterpret_cast<T*>(ds0 + v0 * 16 + off);
+    if (whole) {
+      store_piece(at, d);
+    } else {
+#pragma unroll
+      for (int j = 0; j < E; ++j) st(at + j, d[j]);
     }
-    if (tid == 0 && known && !label_in) {
-      const double d = (double)sy - (double)mr;
-      st(ds + y, (float)((double)row.c_t * exp(d * itau) + (double)row.c_1 * exp(d) - row.label));
-    }
+  });
+  if (odd < hi) st(ds + odd, gradient(xo));
+  zero_from(STAGE ? max(part * sp.len, V) : V);
+  __syncthreads();
+  // then J's classes and the label's
+  if (my >= lo && my < hi) {
+    const double d = (double)sj - (double)m;
+    double q = row.j_q * exp64(d * itau) - row.j_p * exp64(log_e());
+    if (known) q += row.j_1 * exp64(d) - (my == y ? row.label : 0.0);
+    st(ds + my, (float)q);
+  }
+  if (tid == 0 && y >= lo && y < hi && !label_in) {
+    const double d = (double)sy - (double)mr;
+    st(ds + y, (float)((double)row.c_t * exp64(d * itau) + (double)row.c_1 * exp64(d) - row.label));
   }
 }
 
@@ -485,9 +597,17 @@ __global__ __launch_bounds__(TH) void k_distill_rows(DistillGeo g, int64_t first
 __global__ __launch_bounds__(1024) void k_distill_total(DistillGeo g, float* __restrict__ loss) {
   __shared__ double buf[16];
   double acc = 0.0;
-  for (int64_t n = threadIdx.x; n < g.N; n += 1024) {
-    const double w = g.weights ? (double)g.weights[n] : 1.0;
-    if (w != 0.0) acc += w * (double)g.row_loss[n];
+  for (int64_t n0 = threadIdx.x; n0 < g.N; n0 += 8192) {
+    float l[8], w[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t n = n0 + 1024 * i;
+      l[i] = n < g.N ? g.row_loss[n] : 0.f;
+      w[i] = n < g.N ? (g.weights ? g.weights[n] : 1.f) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (w[i] != 0.f) acc += (double)w[i] * (double)l[i];
   }
   acc = block_sum<16>(acc, buf);
   const double wtot = weight_total(g);
@@ -498,7 +618,7 @@ __global__ __launch_bounds__(1024) void k_distill_total(DistillGeo g, float* __r
 
 hipError_t launch_distill_weights(DistillGeo& g, hipStream_t s) {
   const int64_t share = (g.N + DISTILL_WPARTS - 1) / DISTILL_WPARTS;
-  const int64_t per = share < 4096 ? 4096 : share;
+  const int64_t per = share < 1024 ? 1024 : share;
   g.nwsum = (int32_t)((g.N + per - 1) / per);
   k_distill_weights<<<(unsigned)g.nwsum, 256, 0, s>>>(g.weights, g.N, per, g.wsum);
   return hipGetLastError();
@@ -518,21 +638,60 @@ hipError_t run_small(const DistillGeo& g, const T* logits, T* dlogits, hipStream
   return hipGetLastError();
 }
 
+size_t bit_bytes(int32_t classes) { return ((size_t)classes + 63) / 32 * 4; }
+
 template <class T, int TH, int I>
 hipError_t run_rows(const DistillGeo& g, const T* logits, T* dlogits, hipStream_t s) {
   constexpr int64_t most = MAX_THREADS / TH;
-  const size_t lds = ((size_t)g.V + 64) / 32 * 4;
+  const Split none = {};
   for (int64_t first = 0; first < g.N; first += most) {
     const unsigned blocks = (unsigned)(g.N - first < most ? g.N - first : most);
     if (g.labels && g.tau != 1.f)
-      k_distill_rows<T, TH, I, true><<<blocks, TH, lds, s>>>(g, first, logits, dlogits);
+      k_distill_rows<T, TH, I, true, WHOLE><<<blocks, TH, bit_bytes(g.V), s>>>(g, none, first, logits, dlogits);
     else
-      k_distill_rows<T, TH, I, false><<<blocks, TH, lds, s>>>(g, first, logits, dlogits);
+      k_distill_rows<T, TH, I, false, WHOLE><<<blocks, TH, bit_bytes(g.V), s>>>(g, none, first, logits, dlogits);
   }
   return hipGetLastError();
 }
 
+template <class T, int I>
+hipError_t run_split(const DistillGeo& g, const Split& sp, const T* logits, T* dlogits,
+                     hipStream_t s) {
+  const dim3 grid((unsigned)sp.parts, (unsigned)g.N), more((unsigned)sp.parts + 1, (unsigned)g.N);
+  const size_t lds = bit_bytes(sp.len);
+  if (g.labels && g.tau != 1.f) {
+    k_distill_rows<T, 256, I, true, SUM><<<more, 256, lds, s>>>(g, sp, 0, logits, dlogits);
+    k_distill_rows<T, 256, I, true, APPLY><<<grid, 256, lds, s>>>(g, sp, 0, logits, dlogits);
+  } else {
+    k_distill_rows<T, 256, I, false, SUM><<<more, 256, lds, s>>>(g, sp, 0, logits, dlogits);
+    k_distill_rows<T, 256, I, false, APPLY><<<grid, 256, lds, s>>>(g, sp, 0, logits, dlogits);
+  }
+  return hipGetLastError();
+}
+
+// Parts of a row of V classes (1: whole rows): rows that leave CUs idle are split once they are
+// long enough to pay for the second launch.  Two workgroups per CU then, of 2,048 classes at least.
+int split_parts(int64_t N, int32_t V, int32_t* len) {
+  *len = V;
+  if (N > SPLIT_ROWS || N < 1 || V < SPLIT_V) return 1;
+  int64_t parts = 512 / N;
+  if (parts > 64) parts = 64;
+  int64_t l = (V + parts - 1) / parts;
+  l = (l + 2047) / 2048 * 2048;
+  *len = (int32_t)l;
+  return (int)((V + l - 1) / l);
+}
+
+size_t align16(size_t x) { return (x + 15) / 16 * 16; }
+
 }  // namespace
+
+size_t distill_split_bytes(int64_t N, int32_t V, int32_t k) {
+  int32_t len;
+  const int parts = split_parts(N, V, &len);
+  if (parts == 1) return 0;
+  return (size_t)N * (parts * sizeof(PartSums) + sizeof(SetSums)) + align16(N * k * sizeof(SetEntry));
+}
 
 template <class T>
 hipError_t launch_distill_rows(const DistillGeo& g, const T* logits, T* dlogits, hipStream_t s) {
@@ -547,19 +706,33 @@ hipError_t launch_distill_rows(const DistillGeo& g, const T* logits, T* dlogits,
     if (g.V <= 512) return run_small<T, 64, 8>(g, logits, dlogits, s);
     return run_small<T, 64, 16>(g, logits, dlogits, s);
   }
-  // the fewest threads and registers that hold the row
   constexpr int E = Piece<T>::E;
-  // pieces: at the rows' alignment, or at the worst if it changes from row to row
-  const int skip = g.ld % E == 0 ? (int)((uintptr_t)logits % 16 / sizeof(T)) : E - 1;
-  const int np = (g.V + skip + E - 1) / E;
+  const bool whole = !dlogits || ((uintptr_t)dlogits - (uintptr_t)logits) % 16 == 0;
+  Split sp;
+  sp.parts = split_parts(g.N, g.V, &sp.len);
+  if (sp.parts > 1 && whole) {
+    sp.part = (PartSums*)g.split;
+    sp.set = (SetSums*)(sp.part + g.N * sp.parts);
+    sp.entry = (SetEntry*)(sp.set + g.N);
+    const int np = sp.len / E;
+    if (np <= 256) return run_split<T, 1>(g, sp, logits, dlogits, s);
+    if (np <= 512) return run_split<T, 2>(g, sp, logits, dlogits, s);
+    if (np <= 1024) return run_split<T, 4>(g, sp, logits, dlogits, s);
+    if (np <= 2048) return run_split<T, 8>(g, sp, logits, dlogits, s);
+    return run_split<T, 0>(g, sp, logits, dlogits, s);
+  }
+  // The fewest registers that hold the row, and few threads with many of them: more rows are in
+  // flight on a CU, one being read while another is summed or written (4,096 x 50,021 bf16: 256
+  // threads with 32 pieces, three rows, 224 us; 512 with 16, two, 244; 1,024 with 8, two, 270).
+  const int np = g.V / E;
+  if (!whole || np > 16384) return run_rows<T, 1024, 0>(g, logits, dlogits, s);
   if (np <= 256) return run_rows<T, 256, 1>(g, logits, dlogits, s);
   if (np <= 512) return run_rows<T, 256, 2>(g, logits, dlogits, s);
   if (np <= 1024) return run_rows<T, 256, 4>(g, logits, dlogits, s);
   if (np <= 2048) return run_rows<T, 256, 8>(g, logits, dlogits, s);
-  if (np <= 4096) return run_rows<T, 512, 8>(g, logits, dlogits, s);
-  if (np <= 8192) return run_rows<T, 1024, 8>(g, logits, dlogits, s);
-  if (np <= 16384) return run_rows<T, 1024, 16>(g, logits, dlogits, s);
-  return run_rows<T, 1024, 0>(g, logits, dlogits, s);
+  if (np <= 4096) return run_rows<T, 256, 16>(g, logits, dlogits, s);
+  if (np <= 8192) return run_rows<T, 256, 32>(g, logits, dlogits, s);
+  return run_rows<T, 1024, 16>(g, logits, dlogits, s);
 }
 template hipError_t launch_distill_rows<float>(const DistillGeo&, const float*, float*, hipStream_t);
 template hipError_t launch_distill_rows<bf16>(const DistillGeo&, const bf16*, bf16*, hipStream_t);

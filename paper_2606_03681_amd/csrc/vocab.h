@@ -40,7 +40,10 @@ struct DistillGeo {
   float* row_loss;       // caller's or scratch
   double* wsum;          // scratch: partial sums of the weights
   int32_t nwsum;         // their number
+  void* split;           // scratch of split rows
 };
+// Bytes of that scratch: few long rows are split over workgroups.
+size_t distill_split_bytes(int64_t N, int32_t V, int32_t k);
 
 constexpr int DISTILL_WPARTS = 256;  // most partial sums of the weights
 hipError_t launch_distill_weights(DistillGeo& g, hipStream_t s);

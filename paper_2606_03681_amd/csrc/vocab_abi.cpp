@@ -95,13 +95,14 @@ int rows_apart(const tfm_embed* e) {
 // ---- distillation ----------------------------------------------------------------------------
 
 struct DistillWs {
-  size_t wsum, row_loss, total;
+  size_t wsum, row_loss, split, total;
 };
 DistillWs distill_ws(const tfm_distill* d) {
   DistillWs w;
   w.wsum = 0;
   w.row_loss = sizeof(double) * tfm::DISTILL_WPARTS;
-  w.total = w.row_loss + ((size_t)d->N * 4 + 255) / 256 * 256;
+  w.split = w.row_loss + ((size_t)d->N * 4 + 255) / 256 * 256;
+  w.total = w.split + tfm::distill_split_bytes(d->N, d->V, d->k);
   return w;
 }
 
@@ -232,6 +233,7 @@ int tfm_distill_loss(const tfm_distill* d, const void* logits, const int32_t* to
   g.weights = weights; g.ncls = n_class;
   g.wsum = (double*)((char*)workspace + W.wsum);
   g.nwsum = 0;
+  g.split = (char*)workspace + W.split;
   g.row_loss = row_loss ? row_loss : (float*)((char*)workspace + W.row_loss);
   if (weights && d->N > 0) STEP("distill_weights/hbm", tfm::launch_distill_weights(g, st));
   if (d->N > 0) {

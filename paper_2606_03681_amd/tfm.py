@@ -411,15 +411,18 @@ def _tensors(call, *wanted):
     every tensor has its type and shape, lies side by side (shape None: not looked at) and all are
     on the current device."""
     import torch
+    device = None
     for name, t, dtype, shape in wanted:
         if t is None:
             continue
         if t.dtype != dtype:
             raise ValueError(f"{call}: {name} is {t.dtype}, {dtype} wanted")
-        if shape is not None and (tuple(t.shape) != tuple(shape) or not t.is_contiguous()):
+        if shape is not None and (t.shape != shape or not t.is_contiguous()):
             raise ValueError(f"{call}: {name} has shape {tuple(t.shape)} and strides {t.stride()}, "
                              f"{tuple(shape)} side by side wanted")
-        if not t.is_cuda or t.device.index != torch.cuda.current_device():
+        if device is None:
+            device = torch.cuda.current_device() if t.is_cuda else -1
+        if t.get_device() != device or device < 0:
             raise ValueError(f"{call}: {name} is on {t.device}, not on the current GPU")
 
 
@@ -444,10 +447,11 @@ def _logit_rows(call, d, name, t):
     """Rows of logits, ld elements apart."""
     if t is None:
         return name, t, None, None
-    if tuple(t.shape) != (d.N, d.V) or (d.V > 1 and d.N and t.stride(1) != 1) or \
-            (d.N > 1 and t.stride(0) != d.ld):
+    N, V = d.N, d.V
+    rows, step = t.stride() if t.dim() == 2 else (0, 0)
+    if t.shape != (N, V) or (V > 1 and N and step != 1) or (N > 1 and rows != d.ld):
         raise ValueError(f"{call}: {name} has shape {tuple(t.shape)} and strides {t.stride()}, "
-                         f"({d.N}, {d.V}) with rows {d.ld} apart wanted")
+                         f"({N}, {V}) with rows {d.ld} apart wanted")
     return name, t, _torch_dtype(d.dtype), None
 
 
