@@ -1,12 +1,28 @@
 // Sampling (declarations in vocab.h).
+//
+// A class's weight exp(x), x = (s - max) / tau <= 0, is an integer, exp(x) 2^S rounded, with S such
+// that a row's sum stays below 2^63: sums of integers have no order, so that neither the shape of a
+// reduction nor atomics can move a border between two classes.  The exponential is evaluated in 64
+// bits; at the full rate of 64-bit products that is about what reading the logits costs.
+//
+// Classes in falling order of (logit, -index) are kept from the front, so what is kept is told by
+// the last kept class alone.  top_k and top_p look for that class by histograms of counts or
+// weights, first over equal steps of x and then, inside the step that holds the border, over ever
+// finer ranges of the logit's bits, until the few classes left can be ranked against each other.
+// The draw then needs one sum over the kept classes in order of their indices.
+//
+// Rows of up to 64 classes go to groups of 8 to 64 lanes that rank all classes against each other;
+// longer ones to a workgroup each.  Its passes read the row again, from the caches: a pass has some
+// hundred cycles of arithmetic per 16 bytes, and few registers leave room for the waves that hide
+// the loads (the row held in registers took 250 of them at 32 classes per thread).
+#include "mfma.h"
 #include "vocab.h"
+#include "wave.h"
 
 #include <hip/hip_runtime.h>
 
 namespace tfm {
 namespace {
-
-typedef unsigned long long u64;
 
 // Logits as integers in the same order: 0 for what is never drawn (-inf and NaN).
 __device__ __forceinline__ uint32_t key_of(float x) {
@@ -18,164 +34,547 @@ __device__ __forceinline__ float of_key(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-template <class V, class F>
-__device__ __forceinline__ V block_all(V v, V* buf, F op) {
+// 1 / k! for the exponential's series, ln 2 in two parts (its first 40 bits, and the rest) and
+// 1 / ln 2: in scalar registers, where literals would each take two moves.
+struct ExpTable {
+  double c[13], ln2_hi, ln2_lo, inv_ln2;
+};
+__constant__ ExpTable EXP = {
+    {1.0, 1.0, 0.5, 1.0 / 6.0, 1.0 / 24.0, 1.0 / 120.0, 1.0 / 720.0, 1.0 / 5040.0, 1.0 / 40320.0,
+     1.0 / 362880.0, 1.0 / 3628800.0, 1.0 / 39916800.0, 1.0 / 479001600.0},
+    0x1.62e42fefa2000p-1, 0x1.9ef35793c7673p-41, 0x1.71547652b82fep+0};
+
+// A row's settings and scale.
+struct Row {
+  float max;
+  double itau, least;  // 1 / tau; log(min_p) or -inf
+  int S;
+  __device__ __forceinline__ double x(float s) const {
+    return s == max ? 0.0 : ((double)s - (double)max) * itau;
+  }
+  // exp(x) 2^S rounded, x <= 0: 2^n exp(r) by Taylor's series to r^12 / 12! (|r| <= ln 2 / 2: off
+  // by less than 2^-52), rounded by adding 2^52.
+  __device__ __forceinline__ uint64_t weight(double x) const {
+    if (!(x > -50.0)) return 0;
+    const double n = __builtin_rint(x * EXP.inv_ln2);
+    double r = __builtin_fma(n, -EXP.ln2_hi, x);
+    r = __builtin_fma(n, -EXP.ln2_lo, r);
+    double p = EXP.c[12];
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v = op(v, __shfl_xor(v, o));
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
-  __syncthreads();
-  return op(op(buf[0], buf[1]), op(buf[2], buf[3]));
+    for (int i = 11; i >= 0; --i) p = __builtin_fma(p, r, EXP.c[i]);
+    p = __builtin_amdgcn_ldexp(p, (int)n + S) + 0x1p52;
+    return (uint64_t)__double_as_longlong(p) & 0xfffffffffffffull;
+  }
+};
+
+struct Settings {
+  float tau, top_p, min_p, u;
+  int top_k;
+  bool greedy;  // the first class of the order is drawn whatever u says
+};
+__device__ __forceinline__ Settings settings_of(const SampleGeo& g, int64_t n) {
+  Settings o;
+  o.tau = g.temperature ? g.temperature[n] : 1.f;
+  o.top_k = g.top_k ? g.top_k[n] : 0;
+  o.top_p = g.top_p ? g.top_p[n] : 1.f;
+  o.min_p = g.min_p ? g.min_p[n] : 0.f;
+  o.u = g.u[n];
+  o.u = o.u > 0.f ? fminf(o.u, 0x1.fffffep-1f) : 0.f;
+  o.greedy = !(o.tau > 0.f) || o.top_k == 1 || o.top_p <= 0.f || o.min_p > 1.f;
+  return o;
+}
+__device__ __forceinline__ Row row_of(const Settings& o, float max, int S) {
+  return {max, 1.0 / (double)o.tau, o.min_p > 0.f ? log((double)o.min_p) : -(double)INFINITY, S};
+}
+__device__ __forceinline__ float logprob_of(const Row& r, float s, uint64_t mass) {
+  return (float)(r.x(s) - log((double)mass * __builtin_amdgcn_ldexp(1.0, -r.S)));
 }
 
-// One workgroup per row.
-template <class T>
-__global__ __launch_bounds__(256) void k_sample(SampleGeo g, const T* __restrict__ logits,
-                                                double one) {
-  __shared__ u64 buf[4];
-  __shared__ u64 scan_w[4];
-  __shared__ uint32_t scan_t[4];
-  __shared__ int found;
-  const int tid = threadIdx.x, lane = tid & 63, wv = tid >> 6;
-  auto add = [](u64 a, u64 b) { return a + b; };
-  auto mx = [](u64 a, u64 b) { return a > b ? a : b; };
-  auto mn = [](u64 a, u64 b) { return a < b ? a : b; };
-  for (int64_t n = blockIdx.x; n < g.N; n += gridDim.x) {
-    const T* s = logits + n * g.ld;
-    int V = g.V;
-    if (g.ncls) V = min(max(g.ncls[n], 0), g.V);
-    // the largest key and its lowest index in one number
-    u64 best = 0;
-    for (int v = tid; v < V; v += 256) {
-      const uint32_t k = key_of(ld(s + v));
-      if (k) best = mx(best, (u64)k << 32 | (uint32_t)~v);
-    }
-    best = block_all(best, buf, mx);
-    const uint32_t kmax = (uint32_t)(best >> 32);
-    const float tau = g.temperature ? g.temperature[n] : 1.f;
-    const int topk = g.top_k ? g.top_k[n] : 0;
-    const float topp = g.top_p ? g.top_p[n] : 1.f;
-    const float minp = g.min_p ? g.min_p[n] : 0.f;
-    if (kmax == 0 || !(tau > 0.f) || topk == 1 || topp <= 0.f || minp > 1.f) {
-      if (tid == 0) {
-        g.token[n] = kmax ? (int32_t)~(uint32_t)best : -1;
-        if (g.logprob) g.logprob[n] = kmax ? 0.f : -INFINITY;
-      }
-      __syncthreads();
-      continue;
-    }
-    const double top = (double)of_key(kmax), itau = 1.0 / (double)tau;
-    auto xof = [&](uint32_t k) { return k == kmax ? 0.0 : ((double)of_key(k) - top) * itau; };
-    auto weight = [&](uint32_t k) { return k ? (u64)(exp(xof(k)) * one + 0.5) : 0ull; };
-    // kept so far: keys above kt, and the first rt classes whose key is kt
-    uint32_t kt = 0x007fffffu;  // the key that -inf would have: below every logit's
-    u64 rt = ~0ull;
-    auto count_from = [&](uint32_t lo) {
-      u64 c = 0;
-      for (int v = tid; v < V; v += 256) c += key_of(ld(s + v)) >= lo;
-      return block_all(c, buf, add);
-    };
-    auto mass_from = [&](uint32_t lo) {
-      u64 c = 0;
-      for (int v = tid; v < V; v += 256) {
-        const uint32_t k = key_of(ld(s + v));
-        if (k >= lo) c += weight(k);
-      }
-      return block_all(c, buf, add);
-    };
-    if (topk > 0 && count_from(1) > (u64)topk) {
-      uint32_t lo = 1, hi = kmax;  // the largest key from which on at least topk classes lie
-      while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo + 1) / 2;
-        if (count_from(mid) >= (u64)topk) lo = mid;
-        else hi = mid - 1;
-      }
-      kt = lo;
-      rt = (u64)topk - (kt == kmax ? 0 : count_from(kt + 1));
-    }
-    if (topp < 1.f) {
-      const u64 above = kt == 0xffffffffu ? 0 : mass_from(kt + 1);
-      u64 ties = count_from(kt) - (kt == 0xffffffffu ? 0 : count_from(kt + 1));
-      if (ties > rt) ties = rt;
-      const double target = (double)topp * (double)(above + ties * weight(kt));
-      uint32_t lo = kt, hi = kmax;  // the smallest key above which less than the target lies
-      while (lo < hi) {
-        const uint32_t mid = lo + (hi - lo) / 2;
-        if ((double)mass_from(mid + 1) < target) hi = mid;
-        else lo = mid + 1;
-      }
-      const u64 before = lo == 0xffffffffu ? 0 : mass_from(lo + 1);
-      const u64 w = weight(lo);
-      u64 r = ~0ull;
-      if (w) {
-        const double q = (target - (double)before) / (double)w;
-        if (q < 2.0 * VOCAB_VMAX) {  // else every class with this key is kept
-          r = (u64)q;
-          while (r > 0 && !((double)(before + (r - 1) * w) < target)) --r;
-          while ((double)(before + r * w) < target) ++r;
-        }
-      }
-      if (lo > kt) { kt = lo; rt = r; }
-      else if (r < rt) rt = r;
-      if (rt == 0) rt = 1;
-    }
-    const double least = minp > 0.f ? log((double)minp) : -INFINITY;
-    // total of the kept classes
-    u64 mass = 0, ties = 0;
-    for (int v = tid; v < V; v += 256) {
-      const uint32_t k = key_of(ld(s + v));
-      if (k > kt && xof(k) >= least) mass += weight(k);
-      ties += k == kt;
-    }
-    mass = block_all(mass, buf, add);
-    ties = block_all(ties, buf, add);
-    if (ties > rt) ties = rt;
-    if (xof(kt) >= least) mass += ties * weight(kt);
-    float u = g.u[n];
-    u = u > 0.f ? fminf(u, 0x1.fffffep-1f) : 0.f;
-    const double goal = (double)u * (double)mass;
-    // walk in order of the classes
-    u64 run = 0, seen = 0;
-    if (tid == 0) found = -1;
-    int token = -1;
-    for (int v0 = 0; v0 < V && token < 0; v0 += 256) {
-      const int v = v0 + tid;
-      const uint32_t k = v < V ? key_of(ld(s + v)) : 0;
-      const bool tie = k == kt && k != 0;
-      const uint64_t tb = __ballot(tie);
-      __syncthreads();
-      if (lane == 0) scan_t[wv] = (uint32_t)__popcll(tb);
-      __syncthreads();
-      u64 rank = seen + __popcll(tb & ((1ull << lane) - 1));
-      for (int i = 0; i < wv; ++i) rank += scan_t[i];
-      const bool kept = k != 0 && xof(k) >= least && (k > kt || (tie && rank < rt));
-      const u64 w = kept ? weight(k) : 0;
-      u64 pre = w;
+// ---- rows of up to 64 classes -------------------------------------------------------------------
+template <int W, class V, class F>
+__device__ __forceinline__ V group_all(V v, F op) {
 #pragma unroll
-      for (int o = 1; o < 64; o <<= 1) {
-        const u64 q = __shfl_up(pre, o);
-        if (lane >= o) pre += q;
-      }
-      if (lane == 63) scan_w[wv] = pre;
-      __syncthreads();
-      u64 all = 0;
-      for (int i = 0; i < 4; ++i) {
-        if (i < wv) pre += scan_w[i];
-        all += scan_w[i];
-        seen += scan_t[i];
-      }
-      if (kept && (double)(run + pre) > goal && !((double)(run + pre - w) > goal)) found = v;
-      __syncthreads();
-      token = found;
-      run += all;
+  for (int o = W / 2; o > 0; o >>= 1) v = op(v, (V)__shfl_xor(v, o, W));
+  return v;
+}
+
+// W lanes per row, a class each.
+template <class T, int W>
+__global__ __launch_bounds__(256) void k_sample_small(SampleGeo g, int64_t first, int S,
+                                                      const T* __restrict__ logits) {
+  const int lane = threadIdx.x % W;
+  const int64_t at = first + (int64_t)blockIdx.x * (256 / W) + threadIdx.x / W;
+  const bool mine = at < g.N;
+  const int64_t n = mine ? at : g.N - 1;
+  const int V = g.ncls ? min(max(g.ncls[n], 0), g.V) : g.V;
+  const float s = lane < V ? ld(logits + n * g.ld + lane) : -INFINITY;
+  const uint32_t key = key_of(s);
+  const Settings o = settings_of(g, n);
+  const uint32_t kmax = group_all<W>(key, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+  const Row r = row_of(o, of_key(kmax), S);
+  const double x = key ? r.x(s) : -(double)INFINITY;
+  const uint64_t w = key && !o.greedy ? r.weight(x) : 0;
+  auto add = [](uint64_t a, uint64_t b) { return a + b; };
+  // classes before this one, and their weight
+  int ahead = 0;
+  uint64_t before = 0;
+  if (__any(o.greedy || o.top_k > 0 || o.top_p < 1.f || o.min_p > 0.f)) {
+    for (int j = 0; j < W; ++j) {
+      const uint32_t kj = __shfl(key, j, W);
+      const uint64_t wj = __shfl((unsigned long long)w, j, W);
+      const bool a = kj > key || (kj == key && j < lane);
+      ahead += a;
+      before += a ? wj : 0;
     }
+  }
+  bool kept = key != 0;
+  if (o.greedy) {
+    kept = kept && ahead == 0;
+  } else {
+    if (o.top_k > 0) kept = kept && ahead < o.top_k;
+    if (o.top_p < 1.f) {
+      const uint64_t mass = group_all<W>((unsigned long long)(kept ? w : 0), add);
+      kept = kept && (ahead == 0 || (double)before < (double)o.top_p * (double)mass);
+    }
+    if (o.min_p > 0.f) kept = kept && (ahead == 0 || x >= r.least);
+  }
+  const uint64_t share = kept ? (o.greedy ? 1 : w) : 0;
+  uint64_t run = share;
+#pragma unroll
+  for (int d = 1; d < W; d <<= 1) {
+    const uint64_t q = __shfl_up((unsigned long long)run, d, W);
+    if (lane >= d) run += q;
+  }
+  const uint64_t mass = __shfl((unsigned long long)run, W - 1, W);
+  const uint64_t hits = __ballot((double)run > (double)o.u * (double)mass);
+  const int base = (threadIdx.x & 63) - lane;
+  const uint64_t own = W == 64 ? hits : hits >> base & ((1ull << (W & 63)) - 1);
+  const int token = mass ? __ffsll((unsigned long long)own) - 1 : -1;
+  if (mine && lane == max(token, 0)) {
+    g.token[n] = token;
+    if (g.logprob)
+      g.logprob[n] = token < 0 ? -INFINITY : o.greedy ? 0.f : logprob_of(r, s, mass);
+  }
+}
+
+// ---- longer rows ---------------------------------------------------------------------------------
+constexpr int LIST = 512;   // classes that are ranked against each other
+constexpr int GROUPS = 256; // groups of threads whose maxima bound the top_k-th logit from below
+constexpr float STEPS_OVER = 32.f;  // x that the histogram's equal steps cover
+
+constexpr int CHUNKS = 128;        // most stretches of a row whose weights are summed
+constexpr int STRETCH = 8;         // pieces that a lane has of a stretch, at most
+
+// One workgroup of TH threads per row.
+template <class T, int TH>
+__global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S,
+                                               const T* __restrict__ logits) {
+  constexpr int E = 16 / sizeof(T), NW = TH / 64;
+  constexpr int LOG_BINS = TH == 256 ? 9 : 11, BINS = 1 << LOG_BINS;
+  __shared__ uint64_t hist[BINS];
+  __shared__ alignas(16) uint32_t lkey[LIST];
+  __shared__ int32_t lidx[LIST];
+  __shared__ uint64_t lw[LIST];
+  __shared__ uint64_t wbuf[NW];
+  __shared__ uint64_t chunk[CHUNKS];
+  __shared__ uint32_t count, key_lo, key_hi, out_key;
+  __shared__ int32_t out_idx, found_bin;
+  __shared__ uint64_t found_before;
+  const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
+  const int64_t n = first + blockIdx.x;
+  const T* s = logits + n * g.ld;
+  const int V = g.ncls ? min(max(g.ncls[n], 0), g.V) : g.V;
+  // classes before the first piece; pieces; the class beside them that this thread looks after
+  const int lead = min((int)(-(uintptr_t)s % 16 / sizeof(T)), V);
+  const int np = (V - lead) / E;
+  const char* s0 = reinterpret_cast<const char*>(s + lead);
+  const int odd = tid < lead ? tid : min(tid + np * E, V);
+  const float xo = odd < V ? ld(s + odd) : -INFINITY;
+  const Settings o = settings_of(g, n);
+  // The pieces in rounds of the workgroup, each wave a stretch of 64 C pieces of a round: C such
+  // that the rounds come out even.
+  const int rounds = (np + TH * STRETCH - 1) / (TH * STRETCH);
+  const int C = rounds ? (np + TH * rounds - 1) / (TH * rounds) : 0;
+  auto get = [](const uint4& u, int j) __attribute__((always_inline)) -> float {
+    const uint32_t v[4] = {u.x, u.y, u.z, u.w};
+    if constexpr (sizeof(T) == 4) return __uint_as_float(v[j]);
+    else return __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16);
+  };
+  auto load = [&](int v) __attribute__((always_inline)) {
+    return *reinterpret_cast<const uint4*>(s0 + (uint32_t)v * 16u);
+  };
+  // f(logit, class) for all of this thread's classes
+  auto each = [&](auto f) __attribute__((always_inline)) {
+    for (int r = 0; r < rounds; ++r) {
+      const int v0 = (r * NW + w) * 64 * C + lane;
+      for (int c = 0; c < C; ++c) {
+        const int v = v0 + c * 64;
+        if (v >= np) break;
+        const uint4 p = load(v);
+#pragma unroll
+        for (int j = 0; j < E; ++j) f(get(p, j), lead + v * E + j);
+      }
+    }
+    if (odd < V) f(xo, odd);
+  };
+  // the sum over the workgroup, for every thread
+  auto block_sum = [&](uint64_t v) __attribute__((always_inline)) -> uint64_t {
+    v = wave_sum(v);
+    __syncthreads();
+    if (lane == 0) wbuf[w] = v;
+    __syncthreads();
+    return wave_sum(lane < NW ? wbuf[lane] : (uint64_t)0);
+  };
+
+  float top = -INFINITY;
+  each([&](float v, int) __attribute__((always_inline)) { top = fmaxf(top, v); });
+  const float own_max = top;
+  top = wave_max(top);
+  if (lane == 0) wbuf[w] = __float_as_uint(top);
+  __syncthreads();
+  top = wave_max(lane < NW ? __uint_as_float((uint32_t)wbuf[lane]) : -INFINITY);
+  if (top == -INFINITY) {
     if (tid == 0) {
-      g.token[n] = token;
-      if (g.logprob)
-        g.logprob[n] = (float)(xof(key_of(ld(s + token))) - log((double)mass / one));
+      g.token[n] = -1;
+      if (g.logprob) g.logprob[n] = -INFINITY;
+    }
+    return;
+  }
+  if (o.greedy) {
+    uint32_t at = 0;  // the lowest class with the largest logit, complemented
+    each([&](float v, int c) __attribute__((always_inline)) { if (v == top) at = max(at, ~(uint32_t)c); });
+    at = wave_max(at);
+    __syncthreads();
+    if (lane == 0) wbuf[w] = at;
+    __syncthreads();
+    at = wave_max(lane < NW ? (uint32_t)wbuf[lane] : 0u);
+    if (tid == 0) {
+      g.token[n] = (int32_t)~at;
+      if (g.logprob) g.logprob[n] = 0.f;
+    }
+    return;
+  }
+  const Row r = row_of(o, top, S);
+  // the last kept class: its key and index; all at first
+  uint32_t last_key = 1;
+  int32_t last_idx = 0x7fffffff;
+  auto kept = [&](uint32_t k, int c) __attribute__((always_inline)) {
+    return k > last_key || (k == last_key && c <= last_idx);
+  };
+
+  // How far the border is searched: `want` classes (MASS = false), or the classes before which less
+  // than `goal` of weight lies.
+  uint64_t want = 0;
+  double goal = 0.0;
+  // bin of the histogram in which `carry` plus the bins up to it reach the border; -1: none does
+  auto cross = [&](auto mass, uint64_t carry) __attribute__((always_inline)) -> int {
+    constexpr bool MASS = decltype(mass)::value;
+    constexpr int PER = BINS / TH;
+    uint64_t v[PER], sum = 0;
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      v[i] = hist[tid * PER + i];
+      sum += v[i];
+    }
+    uint64_t run = wave_scan(sum, (uint64_t)0, [](uint64_t a, uint64_t b) { return a + b; });
+    if (lane == 63) wbuf[w] = run;
+    if (tid == 0) found_bin = -1;
+    __syncthreads();
+    run += carry - sum;
+    for (int i = 0; i < w; ++i) run += wbuf[i];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const uint64_t next = run + v[i];
+      const bool here = MASS ? (double)run < goal && !((double)next < goal)
+                             : run < want && next >= want;
+      if (here) {
+        found_bin = tid * PER + i;
+        found_before = run;
+      }
+      run = next;
     }
     __syncthreads();
+    return found_bin;
+  };
+  auto clear = [&]() __attribute__((always_inline)) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < BINS / TH; ++i) hist[i * TH + tid] = 0;
+    __syncthreads();
+  };
+  // classes for which in(key, class, logit), into the list as far as it goes; their number
+  auto gather = [&](auto in) __attribute__((always_inline)) -> uint32_t {
+    __syncthreads();
+    if (tid == 0) {
+      count = 0;
+      key_lo = 0xffffffffu;
+      key_hi = 0;
+    }
+    __syncthreads();
+    each([&](float v, int c) __attribute__((always_inline)) {
+      const uint32_t k = key_of(v);
+      if (k != 0 && in(k, c, v)) {
+        const uint32_t at = atomicAdd(&count, 1u);
+        if (at < LIST) {
+          lkey[at] = k;
+          lidx[at] = c;
+        }
+        atomicMin(&key_lo, k);
+        atomicMax(&key_hi, k);
+      }
+    });
+    __syncthreads();
+    return count;
+  };
+  // the border among the m classes of the list, `carry` lying before them
+  auto rank = [&](auto mass, uint32_t m, uint64_t carry) __attribute__((always_inline)) {
+    constexpr bool MASS = decltype(mass)::value;
+    if (MASS) {
+      for (uint32_t j = tid; j < m; j += TH) lw[j] = r.weight(r.x(of_key(lkey[j])));
+      __syncthreads();
+    }
+    for (uint32_t j = tid; j < m; j += TH) {
+      const uint32_t k = lkey[j];
+      const int c = lidx[j];
+      uint64_t run = carry;
+      for (uint32_t q = 0; q < m; ++q)
+        if (lkey[q] > k || (lkey[q] == k && lidx[q] < c)) run += MASS ? lw[q] : 1;
+      const uint64_t next = run + (MASS ? lw[j] : 1);
+      if (MASS ? (double)run < goal && !((double)next < goal) : run < want && next >= want) {
+        out_key = k;
+        out_idx = c;
+      }
+    }
+    __syncthreads();
+    last_key = out_key;
+    last_idx = out_idx;
+  };
+  // the border among the kept classes with keys in [lo, hi], `carry` lying before them
+  auto refine = [&](auto mass, uint32_t lo, uint32_t hi, uint32_t m, uint64_t carry)
+      __attribute__((always_inline)) {
+    constexpr bool MASS = decltype(mass)::value;
+    while (m > LIST && lo != hi) {
+      const int shift = max(0, 32 - __clz(hi - lo) - LOG_BINS);
+      clear();
+      each([&](float v, int c) __attribute__((always_inline)) {
+        const uint32_t k = key_of(v);
+        if (k >= lo && k <= hi && kept(k, c))
+          atomicAdd((unsigned long long*)&hist[(hi - k) >> shift], MASS ? r.weight(r.x(v)) : 1ull);
+      });
+      __syncthreads();
+      const int b = cross(mass, carry);
+      carry = found_before;
+      const uint32_t upper = hi - ((uint32_t)b << shift), wide = (1u << shift) - 1;
+      const uint32_t lower = max(lo, upper - min(wide, upper));
+      m = gather([&](uint32_t k, int c, float) { return k >= lower && k <= upper && kept(k, c); });
+      lo = key_lo;
+      hi = key_hi;
+    }
+    if (m > LIST) {
+      // one key more often than the list goes: how many of them, then the last one's index
+      if (MASS) {
+        const uint64_t each_w = r.weight(r.x(of_key(lo)));
+        uint64_t more = (uint64_t)((goal - (double)carry) / (double)each_w);
+        while (more > 0 && !((double)(carry + (more - 1) * each_w) < goal)) --more;
+        while ((double)(carry + more * each_w) < goal) ++more;
+        want = more;
+      } else {
+        want -= carry;
+      }
+      constexpr int SHIFT = 18 - LOG_BINS;  // (2^SHIFT <= LIST)
+      clear();
+      each([&](float v, int c) __attribute__((always_inline)) {
+        if (key_of(v) == lo && kept(lo, c)) atomicAdd((unsigned long long*)&hist[c >> SHIFT], 1ull);
+      });
+      __syncthreads();
+      const int b = cross(std::false_type(), 0);
+      carry = found_before;
+      m = gather([&](uint32_t k, int c, float) { return k == lo && c >> SHIFT == b && kept(k, c); });
+      rank(std::false_type(), m, carry);
+      return;
+    }
+    rank(mass, m, carry);
+  };
+  // step of x in which a logit lies
+  const float steps = fminf((float)BINS / STEPS_OVER * (float)r.itau, 3e38f);
+  auto step_of = [&](float v) __attribute__((always_inline)) {
+    return v == top ? 0 : (int)fminf((top - v) * steps, (float)(BINS - 1));
+  };
+  // by the histogram over x; false: nothing is cut off
+  auto search = [&](auto mass) __attribute__((always_inline)) {
+    constexpr bool MASS = decltype(mass)::value;
+    clear();
+    each([&](float v, int c) __attribute__((always_inline)) {
+      const uint32_t k = key_of(v);
+      if (k != 0 && kept(k, c))
+        atomicAdd((unsigned long long*)&hist[step_of(v)], MASS ? r.weight(r.x(v)) : 1ull);
+    });
+    __syncthreads();
+    if (MASS) {
+      uint64_t sum = 0;
+#pragma unroll
+      for (int i = 0; i < BINS / TH; ++i) sum += hist[i * TH + tid];
+      goal = (double)o.top_p * (double)block_sum(sum);
+      __syncthreads();
+    }
+    const int b = cross(mass, 0);
+    if (b < 0) return;
+    const uint64_t carry = found_before;
+    const uint32_t m = gather([&](uint32_t k, int c, float v) { return step_of(v) == b && kept(k, c); });
+    refine(mass, key_lo, key_hi, m, carry);
+  };
+
+  bool few = false;  // the kept classes fit the list
+  if (o.top_k > 0) {
+    want = (uint64_t)o.top_k;
+    bool done = false;
+    if (o.top_k <= GROUPS) {
+      // at least top_k classes reach the top_k-th largest of the groups' maxima, and few more
+      constexpr int PER = TH / GROUPS;
+      uint32_t k = key_of(own_max);
+#pragma unroll
+      for (int d = 1; d < PER; d <<= 1) k = max(k, (uint32_t)__shfl_xor(k, d));
+      __syncthreads();
+      if (tid % PER == 0) lkey[tid / PER] = k;
+      if (tid == 0) out_key = 0;
+      __syncthreads();
+      if (tid < GROUPS) {
+        const uint32_t mine = lkey[tid];
+        int ahead = 0;
+        for (int q = 0; q < GROUPS; q += 4) {
+          const uint4 v = *reinterpret_cast<const uint4*>(lkey + q);
+          ahead += (v.x > mine || (v.x == mine && q < tid)) + (v.y > mine || (v.y == mine && q + 1 < tid)) +
+                   (v.z > mine || (v.z == mine && q + 2 < tid)) + (v.w > mine || (v.w == mine && q + 3 < tid));
+        }
+        if (ahead == o.top_k - 1) out_key = mine;
+      }
+      __syncthreads();
+      const uint32_t least = out_key;
+      const uint32_t m = gather([&](uint32_t k, int, float) { return k >= least; });
+      if (m <= LIST) {
+        done = true;
+        if (m >= (uint32_t)o.top_k) rank(std::false_type(), m, 0);  // (else all drawable classes)
+        few = true;
+      }
+    }
+    if (!done) search(std::false_type());
   }
+  if (o.top_p < 1.f) {
+    if (few) {
+      const uint32_t m = gather([&](uint32_t k, int c, float) { return kept(k, c); });
+      uint64_t sum = 0;
+      for (uint32_t j = tid; j < m; j += TH) sum += r.weight(r.x(of_key(lkey[j])));
+      goal = (double)o.top_p * (double)block_sum(sum);
+      rank(std::true_type(), m, 0);
+    } else {
+      search(std::true_type());
+    }
+  }
+
+  // the kept classes' weights in order of their indices: the classes before the first piece, the
+  // pieces in rounds of the workgroup, the classes behind the last
+  auto share = [&](float v, int c) __attribute__((always_inline)) -> uint64_t {
+    const uint32_t k = key_of(v);
+    if (k == 0 || !kept(k, c)) return 0;
+    const double xx = r.x(v);
+    return xx >= r.least ? r.weight(xx) : 0;
+  };
+  const uint64_t odd_share = odd < V ? share(xo, odd) : 0;
+  auto add = [](uint64_t a, uint64_t b) { return a + b; };
+  for (int q = 0; q < rounds; ++q) {
+    const int v0 = (q * NW + w) * 64 * C + lane;
+    uint64_t sum = 0;
+    for (int c = 0; c < C; ++c) {
+      const int v = v0 + c * 64;
+      if (v >= np) break;
+      const uint4 p = load(v);
+#pragma unroll
+      for (int j = 0; j < E; ++j) sum += share(get(p, j), lead + v * E + j);
+    }
+    sum = wave_sum(sum);
+    if (lane == 0) chunk[q * NW + w] = sum;
+  }
+  __syncthreads();
+  if (w != 0) return;
+  // one wave draws: where the running sum passes u times the total, first among the stretches
+  const uint64_t beside = wave_scan(odd_share, (uint64_t)0, add);
+  const uint64_t lead_sum = wave_sum(tid < lead ? odd_share : (uint64_t)0);
+  const int chunks = rounds * NW;
+  const uint64_t c0 = 2 * lane < chunks ? chunk[2 * lane] : 0;
+  const uint64_t c1 = 2 * lane + 1 < chunks ? chunk[2 * lane + 1] : 0;
+  const uint64_t upto = wave_scan(c0 + c1, (uint64_t)0, add);
+  const uint64_t pieces = from_lane(upto, 63), mass = pieces + from_lane(beside, 63);
+  const double aim = (double)o.u * (double)mass;
+  auto passes = [&](uint64_t before, uint64_t own) __attribute__((always_inline)) {
+    return !((double)before > aim) && (double)(before + own) > aim;
+  };
+  int token = -1;
+  float logit = 0.f;
+  auto drawn = [&](bool hit, int c, float v) __attribute__((always_inline)) {
+    const uint64_t b = __ballot(hit);
+    if (b) {
+      const int l = __ffsll((unsigned long long)b) - 1;
+      token = (int)from_lane((uint32_t)c, l);
+      logit = from_lane(v, l);
+    }
+  };
+  drawn(odd < V && passes(beside - odd_share + (tid < lead ? (uint64_t)0 : pieces), odd_share), odd, xo);
+  uint64_t run = lead_sum + upto - c0 - c1;  // before this lane's first stretch
+  const bool in0 = passes(run, c0), in1 = passes(run + c0, c1);
+  const uint64_t hits = __ballot(in0 || in1);
+  if (hits) {
+    const int l = __ffsll((unsigned long long)hits) - 1;
+    const int at = (int)from_lane((uint32_t)(2 * lane + (in0 ? 0 : 1)), l);
+    run = from_lane(in0 ? run : run + c0, l);
+    for (int c = 0; c < C && token < 0; ++c) {
+      const int v = at * 64 * C + c * 64 + lane;
+      uint64_t q[E], sum = 0;
+      uint4 p = make_uint4(0, 0, 0, 0);
+      if (v < np) p = load(v);
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        q[j] = v < np ? share(get(p, j), lead + v * E + j) : 0;
+        sum += q[j];
+      }
+      const uint64_t to = wave_scan(sum, (uint64_t)0, add);
+      uint64_t before = run + to - sum;
+      bool hit = false;
+      int which = 0;
+      float z = 0.f;
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        if (passes(before, q[j])) {
+          hit = true;
+          which = lead + v * E + j;
+          z = get(p, j);
+        }
+        before += q[j];
+      }
+      drawn(hit, which, z);
+      run += from_lane(to, 63);
+    }
+  }
+  if (lane == 0) {
+    g.token[n] = token;
+    if (g.logprob) g.logprob[n] = logprob_of(r, logit, mass);
+  }
+}
+
+template <class T, int W>
+hipError_t run_small(const SampleGeo& g, int S, const T* logits, hipStream_t s) {
+  constexpr int64_t most = MAX_THREADS / 256;
+  for (int64_t first = 0; first < g.N; first += most * (256 / W)) {
+    const int64_t blocks = (g.N - first + 256 / W - 1) / (256 / W);
+    k_sample_small<T, W><<<(unsigned)(blocks < most ? blocks : most), 256, 0, s>>>(g, first, S, logits);
+  }
+  return hipGetLastError();
+}
+template <class T, int TH>
+hipError_t run_rows(const SampleGeo& g, int S, const T* logits, hipStream_t s) {
+  constexpr int64_t most = MAX_THREADS / TH;
+  for (int64_t first = 0; first < g.N; first += most)
+    k_sample<T, TH><<<(unsigned)(g.N - first < most ? g.N - first : most), TH, 0, s>>>(g, first, S, logits);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -184,10 +583,15 @@ template <class T>
 hipError_t launch_sample(const SampleGeo& g, const T* logits, hipStream_t s) {
   int bits = 0;
   while ((1 << bits) < g.V) ++bits;
-  const double one = ldexp(1.0, 62 - bits < 51 ? 62 - bits : 51);
-  const unsigned blocks = (unsigned)(g.N < 65536 ? g.N : 65536);
-  k_sample<T><<<blocks, 256, 0, s>>>(g, logits, one);
-  return hipGetLastError();
+  const int S = 62 - bits < 51 ? 62 - bits : 51;
+  if (g.V <= 8) return run_small<T, 8>(g, S, logits, s);
+  if (g.V <= 16) return run_small<T, 16>(g, S, logits, s);
+  if (g.V <= 32) return run_small<T, 32>(g, S, logits, s);
+  if (g.V <= 64) return run_small<T, 64>(g, S, logits, s);
+  // many threads to a row that has pieces for them, while there are CUs without a row
+  const int np = g.V / (16 / (int)sizeof(T));
+  if (np > 512 && g.N <= 512) return run_rows<T, 1024>(g, S, logits, s);
+  return run_rows<T, 256>(g, S, logits, s);
 }
 template hipError_t launch_sample<float>(const SampleGeo&, const float*, hipStream_t);
 template hipError_t launch_sample<bf16>(const SampleGeo&, const bf16*, hipStream_t);
