@@ -44,26 +44,29 @@ __constant__ ExpTable EXP = {
      1.0 / 362880.0, 1.0 / 3628800.0, 1.0 / 39916800.0, 1.0 / 479001600.0},
     0x1.62e42fefa2000p-1, 0x1.9ef35793c7673p-41, 0x1.71547652b82fep+0};
 
-// A row's settings and scale.
+// A row's largest logit and scale.
 struct Row {
   float max;
-  double itau, least;  // 1 / tau; log(min_p) or -inf
+  double itau;  // 1 / tau
+  double least; // x that stands for those below it: weight 0, or (largest logit +inf, where no
+                // other class can be drawn) x = 0
   int S;
   __device__ __forceinline__ double x(float s) const {
-    return s == max ? 0.0 : ((double)s - (double)max) * itau;
+    return __builtin_fmax(((double)s - (double)max) * itau, least);
   }
-  // exp(x) 2^S rounded, x <= 0: 2^n exp(r) by Taylor's series to r^12 / 12! (|r| <= ln 2 / 2: off
-  // by less than 2^-52), rounded by adding 2^52.
-  __device__ __forceinline__ uint64_t weight(double x) const {
-    if (!(x > -50.0)) return 0;
-    const double n = __builtin_rint(x * EXP.inv_ln2);
-    double r = __builtin_fma(n, -EXP.ln2_hi, x);
+  // exp(x) 2^S rounded: 2^n exp(r), n = round(x / ln 2), by Taylor's series to r^12 / 12! (|r| <=
+  // ln 2 / 2: off by less than 2^-52).  Both roundings to integers are additions of large numbers.
+  __device__ __forceinline__ uint64_t weight(float s) const {
+    const double v = x(s);
+    const double t = __builtin_fma(v, EXP.inv_ln2, 0x1.8p52), n = t - 0x1.8p52;
+    double r = __builtin_fma(n, -EXP.ln2_hi, v);
     r = __builtin_fma(n, -EXP.ln2_lo, r);
     double p = EXP.c[12];
 #pragma unroll
     for (int i = 11; i >= 0; --i) p = __builtin_fma(p, r, EXP.c[i]);
-    p = __builtin_amdgcn_ldexp(p, (int)n + S) + 0x1p52;
-    return (uint64_t)__double_as_longlong(p) & 0xfffffffffffffull;
+    const int32_t e = (int32_t)(uint32_t)(uint64_t)__double_as_longlong(t) + S + 1023;
+    const double scale = __longlong_as_double((long long)((uint64_t)(uint32_t)(e << 20) << 32));
+    return (uint64_t)__double_as_longlong(__builtin_fma(p, scale, 0x1p52)) & 0xfffffffffffffull;
   }
 };
 
@@ -84,10 +87,22 @@ __device__ __forceinline__ Settings settings_of(const SampleGeo& g, int64_t n) {
   return o;
 }
 __device__ __forceinline__ Row row_of(const Settings& o, float max, int S) {
-  return {max, 1.0 / (double)o.tau, o.min_p > 0.f ? log((double)o.min_p) : -(double)INFINITY, S};
+  return {max, 1.0 / (double)o.tau, max == INFINITY ? 0.0 : -60.0, S};
+}
+// The smallest logit whose x reaches log(min_p), min_p in (0, 1].
+__device__ __forceinline__ uint32_t min_p_key(const Settings& o, float top) {
+  const uint32_t kmax = key_of(top), lowest = 0x00800000u;  // (of -FLT_MAX)
+  if (top == INFINITY) return kmax;
+  const double least = log((double)o.min_p), itau = 1.0 / (double)o.tau;
+  auto reaches = [&](uint32_t k) { return ((double)of_key(k) - (double)top) * itau >= least; };
+  const double guess = (double)top + least * (double)o.tau;  // within a few steps
+  uint32_t k = guess > -3.4028234663852886e38 ? min(max(key_of((float)guess), lowest), kmax) : lowest;
+  while (k > lowest && reaches(k - 1)) --k;
+  while (k < kmax && !reaches(k)) ++k;
+  return k;
 }
 __device__ __forceinline__ float logprob_of(const Row& r, float s, uint64_t mass) {
-  return (float)(r.x(s) - log((double)mass * __builtin_amdgcn_ldexp(1.0, -r.S)));
+  return (float)((s == r.max ? 0.0 : r.x(s)) - log((double)mass * __builtin_amdgcn_ldexp(1.0, -r.S)));
 }
 
 // ---- rows of up to 64 classes -------------------------------------------------------------------
@@ -112,8 +127,8 @@ __global__ __launch_bounds__(256) void k_sample_small(SampleGeo g, int64_t first
   const Settings o = settings_of(g, n);
   const uint32_t kmax = group_all<W>(key, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
   const Row r = row_of(o, of_key(kmax), S);
-  const double x = key ? r.x(s) : -(double)INFINITY;
-  const uint64_t w = key && !o.greedy ? r.weight(x) : 0;
+  // (next to a largest logit of +inf no other class weighs anything)
+  const uint64_t w = key && !o.greedy && (r.max < INFINITY || key == kmax) ? r.weight(s) : 0;
   auto add = [](uint64_t a, uint64_t b) { return a + b; };
   // classes before this one, and their weight
   int ahead = 0;
@@ -136,7 +151,7 @@ __global__ __launch_bounds__(256) void k_sample_small(SampleGeo g, int64_t first
       const uint64_t mass = group_all<W>((unsigned long long)(kept ? w : 0), add);
       kept = kept && (ahead == 0 || (double)before < (double)o.top_p * (double)mass);
     }
-    if (o.min_p > 0.f) kept = kept && (ahead == 0 || x >= r.least);
+    if (o.min_p > 0.f) kept = kept && key >= min_p_key(o, r.max);
   }
   const uint64_t share = kept ? (o.greedy ? 1 : w) : 0;
   uint64_t run = share;
@@ -189,6 +204,7 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
   const int np = (V - lead) / E;
   const char* s0 = reinterpret_cast<const char*>(s + lead);
   const int odd = tid < lead ? tid : min(tid + np * E, V);
+  constexpr uint32_t NONE = sizeof(T) == 4 ? 0xff800000u : 0xff80ff80u;  // -inf
   const float xo = odd < V ? ld(s + odd) : -INFINITY;
   const Settings o = settings_of(g, n);
   // The pieces in rounds of the workgroup, each wave a stretch of 64 C pieces of a round: C such
@@ -203,19 +219,27 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
   auto load = [&](int v) __attribute__((always_inline)) {
     return *reinterpret_cast<const uint4*>(s0 + (uint32_t)v * 16u);
   };
-  // f(logit, class) for all of this thread's classes
+  // f(E logits, class of the first) for all of this wave's pieces, every lane active; -inf where
+  // there are no classes.  The classes beside the pieces come as one more piece.
   auto each = [&](auto f) __attribute__((always_inline)) {
+    float v[E];
     for (int r = 0; r < rounds; ++r) {
-      const int v0 = (r * NW + w) * 64 * C + lane;
-      for (int c = 0; c < C; ++c) {
-        const int v = v0 + c * 64;
-        if (v >= np) break;
-        const uint4 p = load(v);
+      const int first_piece = (r * NW + w) * 64 * C;
+      for (int c = 0; c < C && first_piece + c * 64 < np; ++c) {
+        const int at = first_piece + c * 64 + lane;
+        uint4 p = make_uint4(NONE, NONE, NONE, NONE);
+        if (at < np) p = load(at);
 #pragma unroll
-        for (int j = 0; j < E; ++j) f(get(p, j), lead + v * E + j);
+        for (int j = 0; j < E; ++j) v[j] = get(p, j);
+        f(v, lead + at * E);
       }
     }
-    if (odd < V) f(xo, odd);
+    if (w == 0) {
+      v[0] = xo;
+#pragma unroll
+      for (int j = 1; j < E; ++j) v[j] = -INFINITY;
+      f(v, odd);
+    }
   };
   // the sum over the workgroup, for every thread
   auto block_sum = [&](uint64_t v) __attribute__((always_inline)) -> uint64_t {
@@ -227,7 +251,10 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
   };
 
   float top = -INFINITY;
-  each([&](float v, int) __attribute__((always_inline)) { top = fmaxf(top, v); });
+  each([&](const float (&v)[E], int) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < E; ++j) top = fmaxf(top, v[j]);
+  });
   const float own_max = top;
   top = wave_max(top);
   if (lane == 0) wbuf[w] = __float_as_uint(top);
@@ -242,7 +269,11 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
   }
   if (o.greedy) {
     uint32_t at = 0;  // the lowest class with the largest logit, complemented
-    each([&](float v, int c) __attribute__((always_inline)) { if (v == top) at = max(at, ~(uint32_t)c); });
+    each([&](const float (&v)[E], int c) __attribute__((always_inline)) {
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (v[j] == top) at = max(at, ~(uint32_t)(c + j));
+    });
     at = wave_max(at);
     __syncthreads();
     if (lane == 0) wbuf[w] = at;
@@ -255,11 +286,11 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
     return;
   }
   const Row r = row_of(o, top, S);
-  // the last kept class: its key and index; all at first
-  uint32_t last_key = 1;
+  // the last kept class: its logit and index; every one that can be drawn at first
+  float last = top == INFINITY ? INFINITY : -3.402823466e38f;
   int32_t last_idx = 0x7fffffff;
-  auto kept = [&](uint32_t k, int c) __attribute__((always_inline)) {
-    return k > last_key || (k == last_key && c <= last_idx);
+  auto kept = [&](float v, int c) __attribute__((always_inline)) {
+    return v > last || (v == last && c <= last_idx);
   };
 
   // How far the border is searched: `want` classes (MASS = false), or the classes before which less
@@ -302,7 +333,7 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
     for (int i = 0; i < BINS / TH; ++i) hist[i * TH + tid] = 0;
     __syncthreads();
   };
-  // classes for which in(key, class, logit), into the list as far as it goes; their number
+  // classes for which in(logit, class), into the list as far as it goes; their number
   auto gather = [&](auto in) __attribute__((always_inline)) -> uint32_t {
     __syncthreads();
     if (tid == 0) {
@@ -311,18 +342,37 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
       key_hi = 0;
     }
     __syncthreads();
-    each([&](float v, int c) __attribute__((always_inline)) {
-      const uint32_t k = key_of(v);
-      if (k != 0 && in(k, c, v)) {
-        const uint32_t at = atomicAdd(&count, 1u);
-        if (at < LIST) {
-          lkey[at] = k;
-          lidx[at] = c;
+    uint32_t lo = 0xffffffffu, hi = 0;
+    each([&](const float (&v)[E], int c) __attribute__((always_inline)) {
+      uint32_t bits = 0;
+#pragma unroll
+      for (int j = 0; j < E; ++j) bits |= in(v[j], c + j) ? 1u << j : 0u;
+      if (__ballot(bits != 0) == 0) return;
+      // one place in the list per class, taken by the wave at once
+      const uint32_t mine = __popc(bits);
+      const uint32_t to = wave_scan(mine, 0u, [](uint32_t a, uint32_t b) { return a + b; });
+      uint32_t at = 0;
+      if (lane == 63) at = atomicAdd(&count, to);
+      at = from_lane(at, 63) + to - mine;
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (bits >> j & 1) {
+          const uint32_t k = key_of(v[j]);
+          lo = min(lo, k);
+          hi = max(hi, k);
+          if (at < LIST) {
+            lkey[at] = k;
+            lidx[at] = c + j;
+          }
+          ++at;
         }
-        atomicMin(&key_lo, k);
-        atomicMax(&key_hi, k);
-      }
     });
+    lo = ~wave_max(~lo);
+    hi = wave_max(hi);
+    if (lane == 0) {
+      atomicMin(&key_lo, lo);
+      atomicMax(&key_hi, hi);
+    }
     __syncthreads();
     return count;
   };
@@ -330,7 +380,7 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
   auto rank = [&](auto mass, uint32_t m, uint64_t carry) __attribute__((always_inline)) {
     constexpr bool MASS = decltype(mass)::value;
     if (MASS) {
-      for (uint32_t j = tid; j < m; j += TH) lw[j] = r.weight(r.x(of_key(lkey[j])));
+      for (uint32_t j = tid; j < m; j += TH) lw[j] = r.weight(of_key(lkey[j]));
       __syncthreads();
     }
     for (uint32_t j = tid; j < m; j += TH) {
@@ -346,8 +396,29 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
       }
     }
     __syncthreads();
-    last_key = out_key;
+    last = of_key(out_key);
     last_idx = out_idx;
+  };
+  // hist[bin(logit, class)] gets the weights, or numbers, of the kept classes for which in()
+  auto tally = [&](auto mass, auto in, auto bin) __attribute__((always_inline)) {
+    constexpr bool MASS = decltype(mass)::value;
+    clear();
+    each([&](const float (&v)[E], int c) __attribute__((always_inline)) {
+      bool on[E], any = false;
+#pragma unroll
+      for (int j = 0; j < E; ++j) {
+        on[j] = kept(v[j], c + j) && in(v[j], c + j);
+        any |= on[j];
+      }
+      if (__ballot(any) == 0) return;
+      uint64_t q[E];
+#pragma unroll
+      for (int j = 0; j < E; ++j) q[j] = MASS ? r.weight(v[j]) : 1;
+#pragma unroll
+      for (int j = 0; j < E; ++j)
+        if (on[j]) atomicAdd((unsigned long long*)&hist[bin(v[j], c + j)], (unsigned long long)q[j]);
+    });
+    __syncthreads();
   };
   // the border among the kept classes with keys in [lo, hi], `carry` lying before them
   auto refine = [&](auto mass, uint32_t lo, uint32_t hi, uint32_t m, uint64_t carry)
@@ -355,25 +426,22 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
     constexpr bool MASS = decltype(mass)::value;
     while (m > LIST && lo != hi) {
       const int shift = max(0, 32 - __clz(hi - lo) - LOG_BINS);
-      clear();
-      each([&](float v, int c) __attribute__((always_inline)) {
-        const uint32_t k = key_of(v);
-        if (k >= lo && k <= hi && kept(k, c))
-          atomicAdd((unsigned long long*)&hist[(hi - k) >> shift], MASS ? r.weight(r.x(v)) : 1ull);
-      });
-      __syncthreads();
+      const float f_lo = of_key(lo), f_hi = of_key(hi);
+      tally(mass, [&](float v, int) { return v >= f_lo && v <= f_hi; },
+            [&](float v, int) { return (hi - key_of(v)) >> shift; });
       const int b = cross(mass, carry);
       carry = found_before;
       const uint32_t upper = hi - ((uint32_t)b << shift), wide = (1u << shift) - 1;
       const uint32_t lower = max(lo, upper - min(wide, upper));
-      m = gather([&](uint32_t k, int c, float) { return k >= lower && k <= upper && kept(k, c); });
+      const float g_lo = of_key(lower), g_hi = of_key(upper);
+      m = gather([&](float v, int c) { return v >= g_lo && v <= g_hi && kept(v, c); });
       lo = key_lo;
       hi = key_hi;
     }
     if (m > LIST) {
       // one key more often than the list goes: how many of them, then the last one's index
       if (MASS) {
-        const uint64_t each_w = r.weight(r.x(of_key(lo)));
+        const uint64_t each_w = r.weight(of_key(lo));
         uint64_t more = (uint64_t)((goal - (double)carry) / (double)each_w);
         while (more > 0 && !((double)(carry + (more - 1) * each_w) < goal)) --more;
         while ((double)(carry + more * each_w) < goal) ++more;
@@ -382,14 +450,12 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
         want -= carry;
       }
       constexpr int SHIFT = 18 - LOG_BINS;  // (2^SHIFT <= LIST)
-      clear();
-      each([&](float v, int c) __attribute__((always_inline)) {
-        if (key_of(v) == lo && kept(lo, c)) atomicAdd((unsigned long long*)&hist[c >> SHIFT], 1ull);
-      });
-      __syncthreads();
+      const float tie = of_key(lo);
+      tally(std::false_type(), [&](float v, int) { return v == tie; },
+            [&](float, int c) { return c >> SHIFT; });
       const int b = cross(std::false_type(), 0);
       carry = found_before;
-      m = gather([&](uint32_t k, int c, float) { return k == lo && c >> SHIFT == b && kept(k, c); });
+      m = gather([&](float v, int c) { return v == tie && c >> SHIFT == b && kept(v, c); });
       rank(std::false_type(), m, carry);
       return;
     }
@@ -398,18 +464,12 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
   // step of x in which a logit lies
   const float steps = fminf((float)BINS / STEPS_OVER * (float)r.itau, 3e38f);
   auto step_of = [&](float v) __attribute__((always_inline)) {
-    return v == top ? 0 : (int)fminf((top - v) * steps, (float)(BINS - 1));
+    return (int)fminf((top - v) * steps, (float)(BINS - 1));
   };
   // by the histogram over x; false: nothing is cut off
   auto search = [&](auto mass) __attribute__((always_inline)) {
     constexpr bool MASS = decltype(mass)::value;
-    clear();
-    each([&](float v, int c) __attribute__((always_inline)) {
-      const uint32_t k = key_of(v);
-      if (k != 0 && kept(k, c))
-        atomicAdd((unsigned long long*)&hist[step_of(v)], MASS ? r.weight(r.x(v)) : 1ull);
-    });
-    __syncthreads();
+    tally(mass, [](float, int) { return true; }, [&](float v, int) { return step_of(v); });
     if (MASS) {
       uint64_t sum = 0;
 #pragma unroll
@@ -420,7 +480,7 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
     const int b = cross(mass, 0);
     if (b < 0) return;
     const uint64_t carry = found_before;
-    const uint32_t m = gather([&](uint32_t k, int c, float v) { return step_of(v) == b && kept(k, c); });
+    const uint32_t m = gather([&](float v, int c) { return step_of(v) == b && kept(v, c); });
     refine(mass, key_lo, key_hi, m, carry);
   };
 
@@ -449,8 +509,8 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
         if (ahead == o.top_k - 1) out_key = mine;
       }
       __syncthreads();
-      const uint32_t least = out_key;
-      const uint32_t m = gather([&](uint32_t k, int, float) { return k >= least; });
+      const float bound = out_key ? of_key(out_key) : -3.402823466e38f;
+      const uint32_t m = gather([&](float v, int c) { return v >= bound && kept(v, c); });
       if (m <= LIST) {
         done = true;
         if (m >= (uint32_t)o.top_k) rank(std::false_type(), m, 0);  // (else all drawable classes)
@@ -461,9 +521,9 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
   }
   if (o.top_p < 1.f) {
     if (few) {
-      const uint32_t m = gather([&](uint32_t k, int c, float) { return kept(k, c); });
+      const uint32_t m = gather(kept);
       uint64_t sum = 0;
-      for (uint32_t j = tid; j < m; j += TH) sum += r.weight(r.x(of_key(lkey[j])));
+      for (uint32_t j = tid; j < m; j += TH) sum += r.weight(of_key(lkey[j]));
       goal = (double)o.top_p * (double)block_sum(sum);
       rank(std::true_type(), m, 0);
     } else {
@@ -471,23 +531,33 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
     }
   }
 
+  if (o.min_p > 0.f) {
+    const float bound = of_key(min_p_key(o, top));
+    if (bound > last) {
+      last = bound;
+      last_idx = 0x7fffffff;
+    }
+  }
+
   // the kept classes' weights in order of their indices: the classes before the first piece, the
-  // pieces in rounds of the workgroup, the classes behind the last
+  // stretches, the classes behind the last piece
   auto share = [&](float v, int c) __attribute__((always_inline)) -> uint64_t {
-    const uint32_t k = key_of(v);
-    if (k == 0 || !kept(k, c)) return 0;
-    const double xx = r.x(v);
-    return xx >= r.least ? r.weight(xx) : 0;
+    const uint64_t q = r.weight(v);
+    return kept(v, c) ? q : 0;
   };
   const uint64_t odd_share = odd < V ? share(xo, odd) : 0;
   auto add = [](uint64_t a, uint64_t b) { return a + b; };
   for (int q = 0; q < rounds; ++q) {
-    const int v0 = (q * NW + w) * 64 * C + lane;
+    const int first_piece = (q * NW + w) * 64 * C;
     uint64_t sum = 0;
-    for (int c = 0; c < C; ++c) {
-      const int v = v0 + c * 64;
-      if (v >= np) break;
-      const uint4 p = load(v);
+    for (int c = 0; c < C && first_piece + c * 64 < np; ++c) {
+      const int v = first_piece + c * 64 + lane;
+      uint4 p = make_uint4(NONE, NONE, NONE, NONE);
+      if (v < np) p = load(v);
+      bool any = false;
+#pragma unroll
+      for (int j = 0; j < E; ++j) any |= kept(get(p, j), lead + v * E + j);
+      if (__ballot(any) == 0) continue;
 #pragma unroll
       for (int j = 0; j < E; ++j) sum += share(get(p, j), lead + v * E + j);
     }
