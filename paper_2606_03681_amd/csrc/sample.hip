@@ -15,6 +15,7 @@
 // longer ones to a workgroup each.  Its passes read the row again, from the caches: a pass has some
 // hundred cycles of arithmetic per 16 bytes, and few registers leave room for the waves that hide
 // the loads (the row held in registers took 250 of them at 32 classes per thread).
+#include "math64.h"
 #include "mfma.h"
 #include "vocab.h"
 #include "wave.h"
@@ -93,7 +94,7 @@ __device__ __forceinline__ Row row_of(const Settings& o, float max, int S) {
 __device__ __forceinline__ uint32_t min_p_key(const Settings& o, float top) {
   const uint32_t kmax = key_of(top), lowest = 0x00800000u;  // (of -FLT_MAX)
   if (top == INFINITY) return kmax;
-  const double least = log((double)o.min_p), itau = 1.0 / (double)o.tau;
+  const double least = log64((double)o.min_p), itau = 1.0 / (double)o.tau;
   auto reaches = [&](uint32_t k) { return ((double)of_key(k) - (double)top) * itau >= least; };
   const double guess = (double)top + least * (double)o.tau;  // within a few steps
   uint32_t k = guess > -3.4028234663852886e38 ? min(max(key_of((float)guess), lowest), kmax) : lowest;
@@ -102,7 +103,7 @@ __device__ __forceinline__ uint32_t min_p_key(const Settings& o, float top) {
   return k;
 }
 __device__ __forceinline__ float logprob_of(const Row& r, float s, uint64_t mass) {
-  return (float)((s == r.max ? 0.0 : r.x(s)) - log((double)mass * __builtin_amdgcn_ldexp(1.0, -r.S)));
+  return (float)((s == r.max ? 0.0 : r.x(s)) - log64((double)mass * __builtin_amdgcn_ldexp(1.0, -r.S)));
 }
 
 // ---- rows of up to 64 classes -------------------------------------------------------------------
@@ -175,26 +176,30 @@ __global__ __launch_bounds__(256) void k_sample_small(SampleGeo g, int64_t first
 // ---- longer rows ---------------------------------------------------------------------------------
 constexpr int LIST = 512;   // classes that are ranked against each other
 constexpr int GROUPS = 256; // groups of threads whose maxima bound the top_k-th logit from below
+                            // (four to a lane of one wave)
 constexpr float STEPS_OVER = 32.f;  // x that the histogram's equal steps cover
 
 constexpr int CHUNKS = 128;        // most stretches of a row whose weights are summed
 constexpr int STRETCH = 8;         // pieces that a lane has of a stretch, at most
 
-// One workgroup of TH threads per row.
+// One workgroup of TH threads per row.  With many rows per CU (TH = 256) more waves are worth some
+// spilled registers off the loops (8,192 x 5,000 float32, top_k and top_p: 187 us unbounded, 171 at
+// 6 waves per SIMD, 151 at 8; 1,024 x 50,021 bf16, top_p: 282, 280, 341).
 template <class T, int TH>
-__global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S,
-                                               const T* __restrict__ logits) {
+__global__ __launch_bounds__(TH, TH == 256 ? (sizeof(T) == 4 ? 8 : 6) : 1) void k_sample(
+    SampleGeo g, int64_t first, int S, const T* __restrict__ logits) {
   constexpr int E = 16 / sizeof(T), NW = TH / 64;
   constexpr int LOG_BINS = TH == 256 ? 9 : 11, BINS = 1 << LOG_BINS;
   __shared__ uint64_t hist[BINS];
-  __shared__ alignas(16) uint32_t lkey[LIST];
-  __shared__ int32_t lidx[LIST];
-  __shared__ uint64_t lw[LIST];
+  // classes as (key, ~index): larger is earlier in the order; and a part of them
+  __shared__ alignas(16) uint64_t list[LIST];
+  __shared__ uint64_t part_of[LIST];
+  __shared__ uint32_t part_count;
   __shared__ uint64_t wbuf[NW];
   __shared__ uint64_t chunk[CHUNKS];
-  __shared__ uint32_t count, key_lo, key_hi, out_key;
-  __shared__ int32_t out_idx, found_bin;
-  __shared__ uint64_t found_before;
+  __shared__ uint32_t count, key_lo, key_hi;
+  __shared__ int32_t found_bin;
+  __shared__ uint64_t found_before, found;
   const int tid = threadIdx.x, lane = tid & 63, w = wave_id();
   const int64_t n = first + blockIdx.x;
   const T* s = logits + n * g.ld;
@@ -251,10 +256,24 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
   };
 
   float top = -INFINITY;
-  each([&](const float (&v)[E], int) __attribute__((always_inline)) {
+  // (the row comes from HBM here: four loads in flight)
+  for (int r = 0; r < rounds; ++r) {
+    const int first_piece = (r * NW + w) * 64 * C + lane;
+    for (int c = 0; c < C; c += 4) {
+      uint4 p[4];
 #pragma unroll
-    for (int j = 0; j < E; ++j) top = fmaxf(top, v[j]);
-  });
+      for (int q = 0; q < 4; ++q) {
+        p[q] = make_uint4(NONE, NONE, NONE, NONE);
+        const int at = first_piece + (c + q) * 64;
+        if (c + q < C && at < np) p[q] = load(at);
+      }
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+#pragma unroll
+        for (int j = 0; j < E; ++j) top = fmaxf(top, get(p[q], j));
+    }
+  }
+  if (w == 0) top = fmaxf(top, xo);
   const float own_max = top;
   top = wave_max(top);
   if (lane == 0) wbuf[w] = __float_as_uint(top);
@@ -360,10 +379,7 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
           const uint32_t k = key_of(v[j]);
           lo = min(lo, k);
           hi = max(hi, k);
-          if (at < LIST) {
-            lkey[at] = k;
-            lidx[at] = c + j;
-          }
+          if (at < LIST) list[at] = (uint64_t)k << 32 | (uint32_t)~(c + j);
           ++at;
         }
     });
@@ -376,49 +392,89 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
     __syncthreads();
     return count;
   };
-  // the border among the m classes of the list, `carry` lying before them
-  auto rank = [&](auto mass, uint32_t m, uint64_t carry) __attribute__((always_inline)) {
+  // The border among the m classes of the list, `carry` lying before them (goal < 0: the list is all
+  // that is kept); false: it does not reach the border.  By histograms over ever finer ranges of
+  // (key, ~index), which no two classes share, until a wave can rank what is left.
+  auto rank = [&](auto mass, uint32_t m, uint64_t carry) __attribute__((always_inline)) -> bool {
     constexpr bool MASS = decltype(mass)::value;
-    if (MASS) {
-      for (uint32_t j = tid; j < m; j += TH) lw[j] = r.weight(of_key(lkey[j]));
-      __syncthreads();
+    uint64_t lo = (uint64_t)key_lo << 32, hi = (uint64_t)key_hi << 32 | 0xffffffffu;
+    if (MASS && goal < 0.0) {
+      uint64_t sum = 0;
+      for (uint32_t j = tid; j < m; j += TH) sum += r.weight(of_key((uint32_t)(list[j] >> 32)));
+      goal = (double)o.top_p * (double)block_sum(sum);
     }
-    for (uint32_t j = tid; j < m; j += TH) {
-      const uint32_t k = lkey[j];
-      const int c = lidx[j];
-      uint64_t run = carry;
-      for (uint32_t q = 0; q < m; ++q)
-        if (lkey[q] > k || (lkey[q] == k && lidx[q] < c)) run += MASS ? lw[q] : 1;
-      const uint64_t next = run + (MASS ? lw[j] : 1);
-      if (MASS ? (double)run < goal && !((double)next < goal) : run < want && next >= want) {
-        out_key = k;
-        out_idx = c;
+    uint64_t* from = list;
+    uint64_t* to = part_of;
+    while (m > 64) {
+      const int shift = max(0, 64 - __clzll((long long)(hi - lo)) - LOG_BINS);
+      clear();
+      for (uint32_t j = tid; j < m; j += TH) {
+        const uint64_t e = from[j];
+        atomicAdd((unsigned long long*)&hist[(hi - e) >> shift],
+                  MASS ? (unsigned long long)r.weight(of_key((uint32_t)(e >> 32))) : 1ull);
       }
+      if (tid == 0) part_count = 0;
+      __syncthreads();
+      const int b = cross(mass, carry);
+      if (b < 0) return false;
+      carry = found_before;
+      for (uint32_t j = tid; j < m; j += TH) {
+        const uint64_t e = from[j];
+        if ((int)((hi - e) >> shift) == b) to[atomicAdd(&part_count, 1u)] = e;
+      }
+      __syncthreads();
+      m = part_count;
+      hi -= (uint64_t)b << shift;
+      lo = hi - min((1ull << shift) - 1, (unsigned long long)hi);
+      uint64_t* const swap = from;
+      from = to;
+      to = swap;
+    }
+    if (tid == 0) found = 0;
+    __syncthreads();
+    if (w == 0) {
+      const uint64_t mine = lane < (int)m ? from[lane] : 0;
+      const uint64_t q = lane < (int)m ? (MASS ? r.weight(of_key((uint32_t)(mine >> 32))) : 1) : 0;
+      uint64_t before = carry;
+      for (uint32_t j = 0; j < m; ++j)
+        if (from_lane(mine, (int)j) > mine) before += from_lane(q, (int)j);
+      if (lane < (int)m && (MASS ? (double)before < goal && !((double)(before + q) < goal)
+                                 : before + 1 == want))
+        found = mine;
     }
     __syncthreads();
-    last = of_key(out_key);
-    last_idx = out_idx;
+    const uint64_t f = found;
+    if (f == 0) return false;
+    last = of_key((uint32_t)(f >> 32));
+    last_idx = (int32_t)~(uint32_t)f;
+    return true;
   };
-  // hist[bin(logit, class)] gets the weights, or numbers, of the kept classes for which in()
-  auto tally = [&](auto mass, auto in, auto bin) __attribute__((always_inline)) {
+  // hist[bin(logit, class)] gets the weights, or numbers, of the kept classes for which in(); the
+  // weight of the other kept classes that this thread meets is returned
+  auto tally = [&](auto mass, auto in, auto bin) __attribute__((always_inline)) -> uint64_t {
     constexpr bool MASS = decltype(mass)::value;
+    uint64_t rest = 0;
     clear();
     each([&](const float (&v)[E], int c) __attribute__((always_inline)) {
-      bool on[E], any = false;
+      bool keep[E], any = false;
 #pragma unroll
       for (int j = 0; j < E; ++j) {
-        on[j] = kept(v[j], c + j) && in(v[j], c + j);
-        any |= on[j];
+        keep[j] = kept(v[j], c + j);
+        any |= keep[j];
       }
       if (__ballot(any) == 0) return;
       uint64_t q[E];
 #pragma unroll
       for (int j = 0; j < E; ++j) q[j] = MASS ? r.weight(v[j]) : 1;
 #pragma unroll
-      for (int j = 0; j < E; ++j)
-        if (on[j]) atomicAdd((unsigned long long*)&hist[bin(v[j], c + j)], (unsigned long long)q[j]);
+      for (int j = 0; j < E; ++j) {
+        const bool on = keep[j] && in(v[j], c + j);
+        if (on) atomicAdd((unsigned long long*)&hist[bin(v[j], c + j)], (unsigned long long)q[j]);
+        if (MASS) rest += keep[j] && !on ? q[j] : 0;
+      }
     });
     __syncthreads();
+    return rest;
   };
   // the border among the kept classes with keys in [lo, hi], `carry` lying before them
   auto refine = [&](auto mass, uint32_t lo, uint32_t hi, uint32_t m, uint64_t carry)
@@ -466,71 +522,120 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
   auto step_of = [&](float v) __attribute__((always_inline)) {
     return (int)fminf((top - v) * steps, (float)(BINS - 1));
   };
-  // by the histogram over x; false: nothing is cut off
+  // by the histogram over x
   auto search = [&](auto mass) __attribute__((always_inline)) {
     constexpr bool MASS = decltype(mass)::value;
-    tally(mass, [](float, int) { return true; }, [&](float v, int) { return step_of(v); });
+    float from = -INFINITY;
     if (MASS) {
-      uint64_t sum = 0;
+      // Classes lighter than (1 - top_p) / V of the total hold less than 1 - top_p of it together:
+      // the border lies above them, and they only count for the total (an addition to LDS costs
+      // more than the weight).  The total is at least the threads' largest kept weights together
+      // (1 % more is taken off for the roundings here).
+      const uint64_t some = block_sum(kept(own_max, 0x7fffffff) ? r.weight(own_max) : 0);
+      const float part = (float)((1.0 - (double)o.top_p) * (double)some / V *
+                                 __builtin_amdgcn_ldexp(1.0, -S));
+      const double cut = (double)top + (double)o.tau * ((double)__logf(part) - 0.01);
+      from = (float)(cut - fabs(cut) * 0x1p-22);
+      if (!(from <= top)) from = -INFINITY;
+      __syncthreads();
+    }
+    const uint64_t rest = tally(mass, [&](float v, int) { return v >= from; },
+                                [&](float v, int) { return step_of(v); });
+    if (MASS) {
+      uint64_t sum = rest;
 #pragma unroll
       for (int i = 0; i < BINS / TH; ++i) sum += hist[i * TH + tid];
       goal = (double)o.top_p * (double)block_sum(sum);
       __syncthreads();
     }
     const int b = cross(mass, 0);
-    if (b < 0) return;
+    if (b < 0) return;  // (nothing is cut off)
     const uint64_t carry = found_before;
-    const uint32_t m = gather([&](float v, int c) { return step_of(v) == b && kept(v, c); });
+    const uint32_t m = gather([&](float v, int c) { return step_of(v) == b && kept(v, c) && v >= from; });
     refine(mass, key_lo, key_hi, m, carry);
+  };
+  // The kept classes that reach about the q-th largest of the groups' maxima, into the list: at
+  // least q and few more, unless there are fewer than q in all.
+  auto gather_top = [&](int q) __attribute__((always_inline)) -> uint32_t {
+    constexpr int PER = TH / GROUPS;
+    uint32_t* keys = reinterpret_cast<uint32_t*>(part_of);
+    uint32_t k = key_of(own_max);
+#pragma unroll
+    for (int d = 1; d < PER; d <<= 1) k = max(k, (uint32_t)__shfl_xor(k, d));
+    __syncthreads();
+    if (tid % PER == 0) keys[tid / PER] = k;
+    __syncthreads();
+    if (w == 0) {
+      // the upper 16 bits of the q-th largest, bit by bit
+      const uint4 four = reinterpret_cast<const uint4*>(keys)[lane];
+      uint32_t bound = 0;
+      for (uint32_t bit = 0x80000000u; bit >= 0x10000u; bit >>= 1) {
+        const uint32_t c = bound | bit;
+        const int reach = __popcll(__ballot(four.x >= c)) + __popcll(__ballot(four.y >= c)) +
+                          __popcll(__ballot(four.z >= c)) + __popcll(__ballot(four.w >= c));
+        if (reach >= q) bound = c;
+      }
+      if (lane == 0) found = bound;
+    }
+    __syncthreads();
+    const uint32_t f = (uint32_t)found;
+    const float bound = f >= 0x00800000u ? of_key(f) : -3.402823466e38f;
+    return gather([&](float v, int c) { return v >= bound && kept(v, c); });
+  };
+  // weights of the kept classes: of each stretch, and of the class beside the pieces
+  uint64_t odd_share = 0;
+  auto share = [&](float v, int c) __attribute__((always_inline)) -> uint64_t {
+    const uint64_t q = r.weight(v);
+    return kept(v, c) ? q : 0;
+  };
+  auto weigh = [&]() __attribute__((always_inline)) -> uint64_t {  // their sum, in this wave
+    uint64_t all = 0;
+    for (int q = 0; q < rounds; ++q) {
+      const int first_piece = (q * NW + w) * 64 * C;
+      uint64_t sum = 0;
+      for (int c = 0; c < C && first_piece + c * 64 < np; ++c) {
+        const int v = first_piece + c * 64 + lane;
+        uint4 p = make_uint4(NONE, NONE, NONE, NONE);
+        if (v < np) p = load(v);
+        bool any = false;
+#pragma unroll
+        for (int j = 0; j < E; ++j) any |= kept(get(p, j), lead + v * E + j);
+        if (__ballot(any) == 0) continue;
+#pragma unroll
+        for (int j = 0; j < E; ++j) sum += share(get(p, j), lead + v * E + j);
+      }
+      sum = wave_sum(sum);
+      if (lane == 0) chunk[q * NW + w] = sum;
+      all += sum;
+    }
+    if (w == 0) {
+      odd_share = odd < V ? share(xo, odd) : 0;
+      all += wave_sum(odd_share);
+    }
+    return all;
   };
 
   bool few = false;  // the kept classes fit the list
   if (o.top_k > 0) {
     want = (uint64_t)o.top_k;
-    bool done = false;
     if (o.top_k <= GROUPS) {
-      // at least top_k classes reach the top_k-th largest of the groups' maxima, and few more
-      constexpr int PER = TH / GROUPS;
-      uint32_t k = key_of(own_max);
-#pragma unroll
-      for (int d = 1; d < PER; d <<= 1) k = max(k, (uint32_t)__shfl_xor(k, d));
-      __syncthreads();
-      if (tid % PER == 0) lkey[tid / PER] = k;
-      if (tid == 0) out_key = 0;
-      __syncthreads();
-      if (tid < GROUPS) {
-        const uint32_t mine = lkey[tid];
-        int ahead = 0;
-        for (int q = 0; q < GROUPS; q += 4) {
-          const uint4 v = *reinterpret_cast<const uint4*>(lkey + q);
-          ahead += (v.x > mine || (v.x == mine && q < tid)) + (v.y > mine || (v.y == mine && q + 1 < tid)) +
-                   (v.z > mine || (v.z == mine && q + 2 < tid)) + (v.w > mine || (v.w == mine && q + 3 < tid));
-        }
-        if (ahead == o.top_k - 1) out_key = mine;
-      }
-      __syncthreads();
-      const float bound = out_key ? of_key(out_key) : -3.402823466e38f;
-      const uint32_t m = gather([&](float v, int c) { return v >= bound && kept(v, c); });
+      const uint32_t m = gather_top(o.top_k);
       if (m <= LIST) {
-        done = true;
-        if (m >= (uint32_t)o.top_k) rank(std::false_type(), m, 0);  // (else all drawable classes)
         few = true;
+        if (m >= (uint32_t)o.top_k) rank(std::false_type(), m, 0);  // (else all that can be drawn)
       }
     }
-    if (!done) search(std::false_type());
+    if (!few) search(std::false_type());
   }
   if (o.top_p < 1.f) {
     if (few) {
+      goal = -1.0;
       const uint32_t m = gather(kept);
-      uint64_t sum = 0;
-      for (uint32_t j = tid; j < m; j += TH) sum += r.weight(of_key(lkey[j]));
-      goal = (double)o.top_p * (double)block_sum(sum);
       rank(std::true_type(), m, 0);
     } else {
       search(std::true_type());
     }
   }
-
   if (o.min_p > 0.f) {
     const float bound = of_key(min_p_key(o, top));
     if (bound > last) {
@@ -539,31 +644,10 @@ __global__ __launch_bounds__(TH) void k_sample(SampleGeo g, int64_t first, int S
     }
   }
 
-  // the kept classes' weights in order of their indices: the classes before the first piece, the
-  // stretches, the classes behind the last piece
-  auto share = [&](float v, int c) __attribute__((always_inline)) -> uint64_t {
-    const uint64_t q = r.weight(v);
-    return kept(v, c) ? q : 0;
-  };
-  const uint64_t odd_share = odd < V ? share(xo, odd) : 0;
+  // The draw: the kept classes' weights in order of their indices, which is the classes before the
+  // first piece, the stretches, the classes behind the last piece.
+  weigh();
   auto add = [](uint64_t a, uint64_t b) { return a + b; };
-  for (int q = 0; q < rounds; ++q) {
-    const int first_piece = (q * NW + w) * 64 * C;
-    uint64_t sum = 0;
-    for (int c = 0; c < C && first_piece + c * 64 < np; ++c) {
-      const int v = first_piece + c * 64 + lane;
-      uint4 p = make_uint4(NONE, NONE, NONE, NONE);
-      if (v < np) p = load(v);
-      bool any = false;
-#pragma unroll
-      for (int j = 0; j < E; ++j) any |= kept(get(p, j), lead + v * E + j);
-      if (__ballot(any) == 0) continue;
-#pragma unroll
-      for (int j = 0; j < E; ++j) sum += share(get(p, j), lead + v * E + j);
-    }
-    sum = wave_sum(sum);
-    if (lane == 0) chunk[q * NW + w] = sum;
-  }
   __syncthreads();
   if (w != 0) return;
   // one wave draws: where the running sum passes u times the total, first among the stretches
