@@ -446,33 +446,36 @@ __device__ __forceinline__ int64_t from_lane(int64_t v, int i) {
   return (int64_t)((uint64_t)hi << 32 | lo);
 }
 
-// Zeroes the rows among FILL_ROWS whose ids do not occur, of the workgroup's slice.
+// Zeroes the rows whose ids do not occur, FILL_ROWS at a time, of the workgroup's slice.
 template <int VEC, int W>
 __device__ __forceinline__ void zero_rows(const EmbedGeo& g, const SumGeo& s,
                                           const int2* sorted, float* dtable, int* present) {
-  const int v0 = ((int)blockIdx.x - s.nblk) * FILL_ROWS;
-  if (threadIdx.x < FILL_ROWS) {
-    const int v = v0 + threadIdx.x;
-    int64_t lo = 0, hi = s.N;  // first sorted position with a key >= v
-    while (lo < hi) {
-      const int64_t mid = (lo + hi) >> 1;
-      if (sorted[mid].x < v) lo = mid + 1;
-      else hi = mid;
-    }
-    present[threadIdx.x] = v >= g.V || (lo < s.N && sorted[lo].x == v);
-  }
-  __syncthreads();
   constexpr int Z = VEC < 4 ? VEC : 4;  // a store instruction covers its stretch without gaps
   const float zero[Z] = {};
-  for (int r = threadIdx.x / W; r < FILL_ROWS; r += SUM_T / W) {
-    if (present[r]) continue;
-    float* o = dtable + (int64_t)(v0 + r) * g.E;
+  const int64_t step = (int64_t)((int)gridDim.x - s.nblk) * FILL_ROWS;
+  for (int64_t v0 = (int64_t)((int)blockIdx.x - s.nblk) * FILL_ROWS; v0 < g.V; v0 += step) {
+    __syncthreads();
+    if (threadIdx.x < FILL_ROWS) {
+      const int64_t v = v0 + threadIdx.x;
+      int64_t lo = 0, hi = s.N;  // first sorted position with a key >= v
+      while (lo < hi) {
+        const int64_t mid = (lo + hi) >> 1;
+        if (sorted[mid].x < v) lo = mid + 1;
+        else hi = mid;
+      }
+      present[threadIdx.x] = v >= g.V || (lo < s.N && sorted[lo].x == v);
+    }
+    __syncthreads();
+    for (int r = threadIdx.x / W; r < FILL_ROWS; r += SUM_T / W) {
+      if (present[r]) continue;
+      float* o = dtable + (v0 + r) * g.E;
 #pragma unroll
-    for (int q = 0; q < VEC / Z; ++q) {
-      const int c = (int)blockIdx.y * W * VEC + (q * W + threadIdx.x % W) * Z;
-      if (c >= g.E) continue;
-      if (s.past) put<Z, true>(o + c, zero);
-      else stv<Z>(o + c, zero);
+      for (int q = 0; q < VEC / Z; ++q) {
+        const int c = (int)blockIdx.y * W * VEC + (q * W + threadIdx.x % W) * Z;
+        if (c >= g.E) continue;
+        if (s.past) put<Z, true>(o + c, zero);
+        else stv<Z>(o + c, zero);
+      }
     }
   }
 }
@@ -754,7 +757,9 @@ hipError_t fwd_vec(const EmbedGeo& g, const int32_t* ids, const TT* table, TO* o
 
 template <class TO, int VEC, int W, bool ADD>
 hipError_t bwd_run(const EmbedGeo& g, const SumGeo& s, const int2* sorted, const TO* dout, float* dtable, float* part, hipStream_t st) {
-  const unsigned fill = ADD ? 0u : (unsigned)((g.V + FILL_ROWS - 1) / FILL_ROWS);
+  // (a launch holds fewer than 2^32 threads)
+  const int64_t most = MAX_THREADS / SUM_T / s.slices - s.nblk, want = (g.V + FILL_ROWS - 1) / FILL_ROWS;
+  const unsigned fill = ADD ? 0u : (unsigned)(want < most ? want : most);
   const dim3 grid((unsigned)s.nblk + fill, (unsigned)s.slices);
   k_embed_sum<TO, VEC, W, ADD><<<grid, SUM_T, 0, st>>>(g, s, sorted, dout, dtable, part);
   hipError_t e = hipGetLastError();
