@@ -48,10 +48,10 @@ extern "C" {
  *                   left as they were.
  *
  * Limits: every n >= 0 and their product at most 2^27; 1 <= V <= 2^24; 1 <= E <= 2^16; strides in
- * [0, 2^40], the last row at most 2^48 elements from the first.  The forward's rows must not overlap: in order of their strides, each axis longer
- * than one must step past all that the ones before it reach (the backward only reads its rows:
- * any strides, 0 for a broadcast gradient).  out and table (dtable, dout and workspace) must not
- * share memory. */
+ * [0, 2^40], the last row at most 2^48 elements from the first.  The forward's rows must not
+ * overlap: in order of their strides, each axis longer than one must step past all that the ones
+ * before it reach (the backward only reads its rows: any strides, 0 for a broadcast gradient).
+ * out and table (dtable, dout and workspace) must not share memory. */
 typedef struct {
   int32_t n[3];        /* shape of ids */
   int32_t E, V;        /* row width; table rows */
@@ -98,7 +98,8 @@ int tfm_embed_bwd(const tfm_embed* e, const int32_t* ids, const void* dout, floa
  * logits and dlogits: rows of V elements ld apart, the elements between rows untouched; dlogits
  * may be logits itself (in place) but must not overlap it otherwise.
  * Limits: 0 <= N <= 2^27, 1 <= V <= 2^18, 1 <= k <= 256, V <= ld <= 2^40, N ld <= 2^48,
- * temperature finite and > 0, 0 <= alpha <= 1. */
+ * temperature in [2^-20, 2^20] (D is held to about 2^-22, so the loss's error grows with tau^2),
+ * 0 <= alpha <= 1. */
 typedef struct {
   int32_t N, V, k;
   int32_t dtype; /* of logits and dlogits */

@@ -40,6 +40,7 @@ struct DistillGeo {
   float* row_loss;       // caller's or scratch
   double* wsum;          // scratch: partial sums of the weights
   int32_t nwsum;         // their number
+  double* lsum;          // scratch: partial sums of the weighted losses (as many at most)
   void* split;           // scratch of split rows
 };
 // Bytes of that scratch: few long rows are split over workgroups.

@@ -95,12 +95,13 @@ int rows_apart(const tfm_embed* e) {
 // ---- distillation ----------------------------------------------------------------------------
 
 struct DistillWs {
-  size_t wsum, row_loss, split, total;
+  size_t wsum, lsum, row_loss, split, total;
 };
 DistillWs distill_ws(const tfm_distill* d) {
   DistillWs w;
   w.wsum = 0;
-  w.row_loss = sizeof(double) * tfm::DISTILL_WPARTS;
+  w.lsum = w.wsum + sizeof(double) * tfm::DISTILL_WPARTS;
+  w.row_loss = w.lsum + sizeof(double) * tfm::DISTILL_WPARTS;
   w.split = w.row_loss + ((size_t)d->N * 4 + 255) / 256 * 256;
   w.total = w.split + tfm::distill_split_bytes(d->N, d->V, d->k);
   return w;
@@ -124,8 +125,8 @@ int distill_check(const tfm_distill* d) {
   if (d->k < 1 || d->k > tfm::DISTILL_KMAX)
     return fail(TFM_ERR_DIMS, "k=%d outside [1, %d]", d->k, tfm::DISTILL_KMAX);
   if (d->tail != 0 && d->tail != 1) return fail(TFM_ERR_DIMS, "tail=%d is not 0 or 1", d->tail);
-  if (!(std::isfinite(d->temperature) && d->temperature > 0.f))
-    return fail(TFM_ERR_DIMS, "temperature must be finite and > 0");
+  if (!(d->temperature >= 0x1p-20f && d->temperature <= 0x1p20f))
+    return fail(TFM_ERR_DIMS, "temperature outside [2^-20, 2^20]");
   if (!(d->alpha >= 0.f && d->alpha <= 1.f))
     return fail(TFM_ERR_DIMS, "alpha must lie in [0, 1]");
   return TFM_OK;
@@ -233,6 +234,7 @@ int tfm_distill_loss(const tfm_distill* d, const void* logits, const int32_t* to
   g.weights = weights; g.ncls = n_class;
   g.wsum = (double*)((char*)workspace + W.wsum);
   g.nwsum = 0;
+  g.lsum = (double*)((char*)workspace + W.lsum);
   g.split = (char*)workspace + W.split;
   g.row_loss = row_loss ? row_loss : (float*)((char*)workspace + W.row_loss);
   if (weights && d->N > 0) STEP("distill_weights/hbm", tfm::launch_distill_weights(g, st));

@@ -243,8 +243,9 @@ class TrainStep:
         d, e, N = self.dims, self.ends, self.distill.N
         top_idx, top_logit, top_lse = (tuple(teacher) + (None,))[:3]
         lab = labels.reshape(-1)[self.test_rows] if self.distill.alpha < 1 else None
-        tfm.decode_fwd(d, e, self.n_train, self.n_feat, self.Y, self.ends_params, self.logits,
-                       self.ends_ws)
+        if N:
+            tfm.decode_fwd(d, e, self.n_train, self.n_feat, self.Y, self.ends_params, self.logits,
+                           self.ends_ws)
         tfm.distill_loss(self.distill, self.logits[:N], top_idx, top_logit, top_lse, lab, None,
                          self.row_class, self.loss, None, self.dlogits[:N], self.distill_ws)
         tfm.decode_bwd(d, e, self.n_train, self.n_feat, self.Y, self.ends_params, self.dlogits,

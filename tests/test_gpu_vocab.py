@@ -733,3 +733,103 @@ def test_operators_on_a_side_stream_and_replayed_from_a_graph():
         run()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(outputs(), eager[2]))
+
+
+def test_operators_on_two_streams_at_once():
+    """Two sets of calls with buffers and workspaces of their own, running side by side."""
+    import torch
+    sets = [_chain(), _chain(N=20001, V=5000, E=64, W=30000)]
+    want = []
+    for run, change, outputs in sets:
+        change(5)
+        run()
+        want.append(outputs())
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for s, (run, _, _) in zip(streams, sets):
+            with torch.cuda.stream(s):
+                run()
+    torch.cuda.synchronize()
+    for (_, _, outputs), ref in zip(sets, want):
+        assert all(torch.equal(a, b) for a, b in zip(outputs(), ref))
+
+
+# ---------------------------------------------------------------------------------------------
+# Where one way of working passes into another
+# ---------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("N", [0, 1, 16384, 16385, 100003, 2200000])
+@pytest.mark.parametrize("weighted", [False, True])
+def test_distill_total_over_few_and_many_rows(N, weighted):
+    """The loss is the 64-bit weighted mean of the rows' own losses, rounded once."""
+    import torch
+    from paper_2606_03681_amd import tfm
+    V, k = 3, 2
+    g = torch.Generator(device="cuda").manual_seed(N + weighted)
+    z = torch.randn((N, V), generator=g, device="cuda")
+    idx = torch.randint(0, V, (N, k), generator=g, device="cuda").int()
+    top = torch.randn((N, k), generator=g, device="cuda")
+    w = torch.rand(N, generator=g, device="cuda") if weighted else None
+    if weighted:
+        w[::7] = 0
+    d = tfm.make_distill(N, V, k, V, "f32", 1.0, 1.0, 0)
+    ws = torch.full((tfm.distill_workspace_bytes(d),), 0xA5, dtype=torch.uint8, device="cuda")
+    rows, loss = torch.empty(N, device="cuda"), torch.empty(2, device="cuda")
+    tfm.distill_loss(d, z, idx, top, None, None, w, None, loss, rows, None, ws)
+    tfm.distill_loss(d, z, idx, top, None, None, w, None, loss[1:], None, None, ws)
+    wd = torch.ones(N, dtype=torch.float64) if w is None else w.double().cpu()
+    total = float(wd.sum())
+    ref = float((wd * rows.double().cpu()).sum()) / total if total else 0.0
+    assert abs(float(loss[0]) - ref) <= 2 * U * abs(ref)      # one rounding, and the reference's own
+    assert float(loss[1]) == float(loss[0])                   # rows in the workspace: the same
+    for n in {0, N // 2, N - 1} if N else ():
+        L, _ = ov.distill_row(z[n].double().cpu().numpy(), idx[n].cpu().numpy(),
+                              top[n].cpu().numpy(), None, -1, 1.0, 1.0, 0)
+        L = 0.0 if wd[n] == 0 else L
+        assert abs(float(rows[n]) - L) <= 1e3 * U * (abs(L) + 1)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V", [(64, 24575), (64, 24576), (65, 24576), (63, 24584), (64, 33001)])
+@pytest.mark.parametrize("tail,tau,alpha", [(0, 1.0, 1.0), (1, 3.0, 0.25)])
+def test_distill_around_split_rows(N, V, tail, tau, alpha, dtype):
+    s, t, idx, top = _distill_inputs(N, V, 16, dtype, N + V)
+    rng = np.random.default_rng(N * V)
+    lse = np.array([ov._logsumexp(r / tau) for r in t]).astype(np.float32) if tail else None
+    labels = rng.integers(-1, V, N).astype(np.int32)
+    w = (rng.random(N) < 0.9).astype(np.float32) * rng.uniform(0.5, 2.0, N).astype(np.float32)
+    ncls = rng.integers(V // 2, V + 1, N).astype(np.int32)
+    args = (idx, top, lse, labels, w, ncls, tau, alpha, tail)
+    _check_distill(_run_distill(s, dtype, *args), ov.distill_loss(s, *args), s, labels, w, ncls, tau,
+                   alpha, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [2049, 5000, 9001, 33000])
+def test_sample_row_is_the_same_in_few_and_many_rows(V, dtype):
+    """Few long rows and many of them run in workgroups of different sizes."""
+    import torch
+    from paper_2606_03681_amd import tfm
+    N = 1100
+    g = torch.Generator(device="cuda").manual_seed(V)
+    z = (3 * torch.randn((N, V), generator=g, device="cuda")).to(_torch(dtype))
+    u = torch.rand(N, generator=g, device="cuda")
+    t = 0.5 + torch.rand(N, generator=g, device="cuda")
+    k = torch.randint(0, 300, (N,), generator=g, device="cuda").int()
+    p = 0.5 + 0.6 * torch.rand(N, generator=g, device="cuda")
+    m = 0.02 * torch.rand(N, generator=g, device="cuda")
+
+    def draw(a, b):
+        n = b - a
+        token = torch.full((n,), -7, dtype=torch.int32, device="cuda")
+        lp = torch.empty(n, device="cuda")
+        tfm.sample(tfm.make_sampling(n, V, V, dtype), z[a:b], None, t[a:b], k[a:b], p[a:b], m[a:b],
+                   u[a:b], token, lp)
+        return token, lp
+
+    token, lp = draw(0, N)
+    assert bool((token >= 0).all())
+    for a, b in ((0, 1), (1, 513), (513, 1025), (1025, N)):
+        tt, ll = draw(a, b)
+        assert torch.equal(tt, token[a:b]) and torch.equal(ll, lp[a:b])

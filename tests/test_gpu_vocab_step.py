@@ -227,3 +227,20 @@ def test_draws_from_the_forward_only_path(name, T):
         assert int(token[n]) == t and abs(float(lp[n]) - l) <= 2.0 ** -24 * abs(l) + 1e-9
     greedy, _, _ = im.draw(x, lab, to_dev(u), cat_ids=cat, temperature=0.0)
     assert torch.equal(greedy.long(), logits.argmax(1))
+
+
+def test_training_step_without_unlabelled_rows():
+    """Every row labelled: no row to learn from, loss and gradients 0."""
+    import torch
+    from paper_2606_03681_amd.stack import TrainStep
+    w, e = ends_setup("d64-f32")
+    n_train = np.full_like(w.n_train, w.cfg["R"])
+    ids, table = _cats(w, e, 2, 7, 3)
+    ts = TrainStep(ends_dims(w), ends_struct(e), n_train, e.n_feat, e.n_class, w.params, e.params,
+                   e.table, cat_table=table, cat_cols=2, distill=dict(k=3, alpha=0.5, tail=1))
+    teacher = (torch.empty((0, 3), dtype=torch.int32, device="cuda"),
+               torch.empty((0, 3), device="cuda"), torch.empty(0, device="cuda"))
+    loss = ts.run(to_dev(e.x), to_dev(e.labels), cat_ids=to_dev(ids), teacher=teacher)
+    assert float(loss) == 0.0
+    for g in [ts.ends_grads, ts.cat_grad] + list(ts.stack.grads):
+        assert bool((g == 0).all())

@@ -200,3 +200,13 @@ def test_refusals_clean_under_sanitizers():
                          os.path.join("tests", "test_vocab_abi_cpu.py")])
     assert rc == 0, out[-6000:]
     assert "AddressSanitizer" not in out and "runtime error" not in out, out[-6000:]
+
+
+@pytest.mark.parametrize("tau", [1e-45, 4e-39, 2.0 ** -21, 1.01 * 2.0 ** 20, 1e30, 3e38])
+def test_distillation_temperatures_refused(tau):
+    """Temperatures at which 1 / tau or tau^2 D leaves float32's range or precision."""
+    assert tfm.distill_workspace_bytes(_distill(temperature=tau)) == 0
+    assert _loss(_distill(temperature=tau)) == -1
+    assert "temperature" in tfm.last_error()
+    for ok in (2.0 ** -20, 2.0 ** 20):
+        assert tfm.distill_workspace_bytes(_distill(temperature=ok)) > 0
