@@ -742,9 +742,14 @@ hipError_t launch_sample(const SampleGeo& g, const T* logits, hipStream_t s) {
   if (g.V <= 16) return run_small<T, 16>(g, S, logits, s);
   if (g.V <= 32) return run_small<T, 32>(g, S, logits, s);
   if (g.V <= 64) return run_small<T, 64>(g, S, logits, s);
-  // many threads to a row that has pieces for them, while there are CUs without a row
+  // many threads to a row that has pieces for them, while there are CUs without a row, or with one
+  // more turn where rows are long.  us with 1,024 threads / with 256, temperature alone and top-p:
+  //   1 x 5,000 float32   7.7 / 9.2, 16 / 20       64 x 131,072 bfloat16   50 / 83, 122 / 238
+  //   256 x 5,000         8.3 / 11,  17 / 22       512 x 131,072           113 / 127, 264 / 330
+  //   384 x 5,000         13 / 13,   29 / 26       512 x 12,000 float32    17 / 21, 42 / 50
+  //   1,024 x 5,000       22 / 17,   56 / 34       1,024 x 50,021 bf16     112 / 88, 260 / 206
   const int np = g.V / (16 / (int)sizeof(T));
-  if (np > 512 && g.N <= 512) return run_rows<T, 1024>(g, S, logits, s);
+  if (np > 512 && g.N <= (np > 2048 ? 512 : 256)) return run_rows<T, 1024>(g, S, logits, s);
   return run_rows<T, 256>(g, S, logits, s);
 }
 template hipError_t launch_sample<float>(const SampleGeo&, const float*, hipStream_t);
