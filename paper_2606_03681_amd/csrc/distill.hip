@@ -8,8 +8,13 @@
 // 256 entries, in 64 bits: the loss is a small difference of large logarithms where the student is
 // near the teacher, and the error of S cancels in it to first order only if all else is exact.
 //
-// Rows of up to 1,024 classes go to groups of 8 to 64 lanes, longer ones to a workgroup each.
-// Bound by HBM (a read and a write of the logits) from some thousand classes on.
+// Rows of up to 1,024 classes go to groups of 8 to 64 lanes, longer ones to a workgroup each; few
+// long rows are split over workgroups.  Bound by HBM (a read and a write of the logits) from some
+// thousand classes on: 8,192 x 5,000 float32 81 us (4.1 TB/s; a copy takes 69), 4,096 x 50,021
+// bfloat16 with a label's softmax at another temperature 227 us (3.6 TB/s; a copy 171: two
+// exponentials per class and pass are 164 us of issue beside it).  Short rows are bound by what a row
+// costs in 64 bits (2^21 x 10: 0.22 ns a row), few long ones by latency (7 x 131,072: 22 us in three
+// launches).
 #include "math64.h"
 #include "mfma.h"
 #include "vocab.h"
@@ -314,10 +319,10 @@ enum { WHOLE = 0, SUM = 1, APPLY = 2 };
 
 // TH threads, I pieces per thread in registers.  WHOLE: one workgroup per row.  Few long rows are
 // split into `parts` of `len` classes, a workgroup each, in two launches: SUM leaves every part's
-// sums (and one more workgroup the set's), APPLY joins them and writes the part's gradients.  I = 0: rows that
-// the registers of a CU do not hold, read again for each of the three passes, and (dlogits not
-// aligned as logits) rows written class by class.  TWO: the label's softmax has another temperature
-// than the teacher's, a second exponential per class.
+// sums (and one more workgroup the set's), APPLY joins them and writes the part's gradients.
+// I = 0: rows that the registers of a CU do not hold, read again for each of the three passes, and
+// (dlogits not aligned as logits) rows written class by class.  TWO: the label's softmax has another
+// temperature than the teacher's, a second exponential per class.
 template <class T, int TH, int I, bool TWO, int STAGE>
 __global__ __launch_bounds__(TH, I == 32 ? 3 : 1) void k_distill_rows(DistillGeo g, Split sp,
                                                                       int64_t first,

@@ -8,13 +8,26 @@
 // Classes in falling order of (logit, -index) are kept from the front, so what is kept is told by
 // the last kept class alone.  top_k and top_p look for that class by histograms of counts or
 // weights, first over equal steps of x and then, inside the step that holds the border, over ever
-// finer ranges of the logit's bits, until the few classes left can be ranked against each other.
-// The draw then needs one sum over the kept classes in order of their indices.
+// finer ranges of the logit's bits, until the few classes left (they are gathered in a list) can be
+// ranked against each other.  Classes too light to hold the border together stay out of the first
+// histogram, and where few classes can be kept at all they go straight into the list: an atomic on
+// LDS costs a wave some 115 cycles.  The draw then needs one sum over the kept classes in order of
+// their indices, of which chunks are kept so that only the drawn class's chunk is read again.
 //
 // Rows of up to 64 classes go to groups of 8 to 64 lanes that rank all classes against each other;
 // longer ones to a workgroup each.  Its passes read the row again, from the caches: a pass has some
 // hundred cycles of arithmetic per 16 bytes, and few registers leave room for the waves that hide
 // the loads (the row held in registers took 250 of them at 32 classes per thread).
+//
+// Bound by arithmetic: a weight is 19 instructions in 64 bits, some 80 cycles of a SIMD for 64
+// classes.  us by mode (largest class / temperature alone / top-k / top-p / both / min-p):
+//    64 x 131,072 bfloat16    13   49   55  141   68   54     (the row on one of 64 CUs)
+//     1 x  32,000 float32    5.4   17   22   41   31   14
+//  8,192 x  5,000 float32     42   80  123  155  149   76     (164 MB, a copy's rate: 34)
+//  4,096 x    300 float32      8   17   33   35   45   21
+// A series of the seventh degree behind a table of 32 roots of two in LDS has 14 instructions: 7 %
+// less for 1,024 threads, but 15 % more for 256 threads and bfloat16, which then spill; both have to
+// round alike, so that a row's draw does not depend on its batch.
 #include "math64.h"
 #include "mfma.h"
 #include "vocab.h"
@@ -35,36 +48,36 @@ __device__ __forceinline__ float of_key(uint32_t k) {
   return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
 }
 
-// 1 / k! for the exponential's series, ln 2 in two parts (its first 40 bits, and the rest) and
-// 1 / ln 2: in scalar registers, where literals would each take two moves.
-struct ExpTable {
-  double c[13], ln2_hi, ln2_lo, inv_ln2;
+// 2^f, |f| <= 1 / 2, by powers up to f^11: the Taylor series (ln 2)^k / k! to f^13, whose last two
+// powers are replaced by the Chebyshev polynomials' lower terms (T13 without its first is within
+// 2^-12 of x^13, T12 within 2^-11 of x^12, x = 2 f).  Off by less than 2^-57.  In scalar registers,
+// where literals would each take two moves.
+struct PowerTable {
+  double c[12];
 };
-__constant__ ExpTable EXP = {
-    {1.0, 1.0, 0.5, 1.0 / 6.0, 1.0 / 24.0, 1.0 / 120.0, 1.0 / 720.0, 1.0 / 5040.0, 1.0 / 40320.0,
-     1.0 / 362880.0, 1.0 / 3628800.0, 1.0 / 39916800.0, 1.0 / 479001600.0},
-    0x1.62e42fefa2000p-1, 0x1.9ef35793c7673p-41, 0x1.71547652b82fep+0};
+__constant__ PowerTable POWER = {
+    {1.0, 0x1.62e42fefa39efp-1, 0x1.ebfbdff82c5aep-3,
+     0x1.c6b08d704a0d1p-5, 0x1.3b2ab6fb9f1d3p-7, 0x1.5d87fe78a22b2p-10,
+     0x1.4309131120d4p-13, 0x1.ffcbfc75e5fb2p-17, 0x1.62bfc2f06930fp-20,
+     0x1.b524db5f98239p-24, 0x1.e6221f6484be9p-28, 0x1.ea03e67c9deafp-32}};
+constexpr double INV_LN2 = 0x1.71547652b82fep+0;
 
 // A row's largest logit and scale.
 struct Row {
   float max;
-  double itau;  // 1 / tau
-  double least; // x that stands for those below it: weight 0, or (largest logit +inf, where no
-                // other class can be drawn) x = 0
+  double iu;    // 1 / (tau ln 2): u = x / ln 2 = (s - max) iu
+  double least; // u that stands for those below it: weight 0, or (largest logit +inf, where no
+                // other class can be drawn) u = 0
   int S;
-  __device__ __forceinline__ double x(float s) const {
-    return __builtin_fmax(((double)s - (double)max) * itau, least);
-  }
-  // exp(x) 2^S rounded: 2^n exp(r), n = round(x / ln 2), by Taylor's series to r^12 / 12! (|r| <=
-  // ln 2 / 2: off by less than 2^-52).  Both roundings to integers are additions of large numbers.
+  // exp(x) 2^S rounded: 2^n 2^f, n = round(u), f = u - n.  Both roundings to integers are
+  // additions of large numbers.  Against the exact value the result is off by less than 0.75 of its
+  // steps of 2^-51 (20 million random x, tau = 1).
   __device__ __forceinline__ uint64_t weight(float s) const {
-    const double v = x(s);
-    const double t = __builtin_fma(v, EXP.inv_ln2, 0x1.8p52), n = t - 0x1.8p52;
-    double r = __builtin_fma(n, -EXP.ln2_hi, v);
-    r = __builtin_fma(n, -EXP.ln2_lo, r);
-    double p = EXP.c[12];
+    const double u = __builtin_fmax(((double)s - (double)max) * iu, least);
+    const double t = u + 0x1.8p52, f = u - (t - 0x1.8p52);
+    double p = POWER.c[11];
 #pragma unroll
-    for (int i = 11; i >= 0; --i) p = __builtin_fma(p, r, EXP.c[i]);
+    for (int i = 10; i >= 0; --i) p = __builtin_fma(p, f, POWER.c[i]);
     const int32_t e = (int32_t)(uint32_t)(uint64_t)__double_as_longlong(t) + S + 1023;
     const double scale = __longlong_as_double((long long)((uint64_t)(uint32_t)(e << 20) << 32));
     return (uint64_t)__double_as_longlong(__builtin_fma(p, scale, 0x1p52)) & 0xfffffffffffffull;
@@ -88,7 +101,7 @@ __device__ __forceinline__ Settings settings_of(const SampleGeo& g, int64_t n) {
   return o;
 }
 __device__ __forceinline__ Row row_of(const Settings& o, float max, int S) {
-  return {max, 1.0 / (double)o.tau, max == INFINITY ? 0.0 : -60.0, S};
+  return {max, INV_LN2 / (double)o.tau, max == INFINITY ? 0.0 : -86.0, S};
 }
 // The smallest logit whose x reaches log(min_p), min_p in (0, 1].
 __device__ __forceinline__ uint32_t min_p_key(const Settings& o, float top) {
@@ -103,7 +116,8 @@ __device__ __forceinline__ uint32_t min_p_key(const Settings& o, float top) {
   return k;
 }
 __device__ __forceinline__ float logprob_of(const Row& r, float s, uint64_t mass) {
-  return (float)((s == r.max ? 0.0 : r.x(s)) - log64((double)mass * __builtin_amdgcn_ldexp(1.0, -r.S)));
+  const double x = s == r.max ? 0.0 : ((double)s - (double)r.max) * r.iu * (LN2_HI + LN2_LO);
+  return (float)(x - log64((double)mass * __builtin_amdgcn_ldexp(1.0, -r.S)));
 }
 
 // ---- rows of up to 64 classes -------------------------------------------------------------------
@@ -518,7 +532,7 @@ __global__ __launch_bounds__(TH, TH == 256 ? (sizeof(T) == 4 ? 8 : 6) : 1) void 
     rank(mass, m, carry);
   };
   // step of x in which a logit lies
-  const float steps = fminf((float)BINS / STEPS_OVER * (float)r.itau, 3e38f);
+  const float steps = fminf((float)BINS / STEPS_OVER * (float)(r.iu * (LN2_HI + LN2_LO)), 3e38f);
   auto step_of = [&](float v) __attribute__((always_inline)) {
     return (int)fminf((top - v) * steps, (float)(BINS - 1));
   };
