@@ -22,14 +22,15 @@
 // Bound by arithmetic: a weight is 19 instructions in 64 bits, some 80 cycles of a SIMD for 64
 // classes.  us by mode (largest class / temperature alone / top-k / top-p / both / min-p):
 //    64 x 131,072 bfloat16    13   49   55  141   68   54     (the row on one of 64 CUs)
-//     1 x  32,000 float32    5.4   17   22   41   31   14
+//     1 x  32,000 float32    5.4   17   22   41   31   13
 //  8,192 x  5,000 float32     42   80  123  155  149   76     (164 MB, a copy's rate: 34)
-//  4,096 x    300 float32      8   17   33   35   45   21
+//  4,096 x    300 float32      8   17   33   35   45   20
 // A series of the seventh degree behind a table of 32 roots of two in LDS has 14 instructions: 7 %
 // less for 1,024 threads, but 15 % more for 256 threads and bfloat16, which then spill; both have to
 // round alike, so that a row's draw does not depend on its batch.
 #include "math64.h"
 #include "mfma.h"
+#include "order.h"
 #include "vocab.h"
 #include "wave.h"
 
@@ -37,16 +38,6 @@
 
 namespace tfm {
 namespace {
-
-// Logits as integers in the same order: 0 for what is never drawn (-inf and NaN).
-__device__ __forceinline__ uint32_t key_of(float x) {
-  if (!(x > -INFINITY)) return 0;
-  const uint32_t u = __float_as_uint(x + 0.f);  // -0 and 0 are equal
-  return u & 0x80000000u ? ~u : u | 0x80000000u;
-}
-__device__ __forceinline__ float of_key(uint32_t k) {
-  return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k);
-}
 
 // 2^f, |f| <= 1 / 2, by powers up to f^11: the Taylor series (ln 2)^k / k! to f^13, whose last two
 // powers are replaced by the Chebyshev polynomials' lower terms (T13 without its first is within
@@ -103,17 +94,9 @@ __device__ __forceinline__ Settings settings_of(const SampleGeo& g, int64_t n) {
 __device__ __forceinline__ Row row_of(const Settings& o, float max, int S) {
   return {max, INV_LN2 / (double)o.tau, max == INFINITY ? 0.0 : -86.0, S};
 }
-// The smallest logit whose x reaches log(min_p), min_p in (0, 1].
-__device__ __forceinline__ uint32_t min_p_key(const Settings& o, float top) {
-  const uint32_t kmax = key_of(top), lowest = 0x00800000u;  // (of -FLT_MAX)
-  if (top == INFINITY) return kmax;
-  const double least = log64((double)o.min_p), itau = 1.0 / (double)o.tau;
-  auto reaches = [&](uint32_t k) { return ((double)of_key(k) - (double)top) * itau >= least; };
-  const double guess = (double)top + least * (double)o.tau;  // within a few steps
-  uint32_t k = guess > -3.4028234663852886e38 ? min(max(key_of((float)guess), lowest), kmax) : lowest;
-  while (k > lowest && reaches(k - 1)) --k;
-  while (k < kmax && !reaches(k)) ++k;
-  return k;
+// Key of the smallest logit whose x reaches log(min_p), min_p in (0, 1].
+__device__ __forceinline__ uint32_t least_key(const Settings& o, float top) {
+  return min_p_key(log64((double)o.min_p), o.tau, top);
 }
 __device__ __forceinline__ float logprob_of(const Row& r, float s, uint64_t mass) {
   const double x = s == r.max ? 0.0 : ((double)s - (double)r.max) * r.iu * (LN2_HI + LN2_LO);
@@ -166,7 +149,7 @@ __global__ __launch_bounds__(256) void k_sample_small(SampleGeo g, int64_t first
       const uint64_t mass = group_all<W>((unsigned long long)(kept ? w : 0), add);
       kept = kept && (ahead == 0 || (double)before < (double)o.top_p * (double)mass);
     }
-    if (o.min_p > 0.f) kept = kept && key >= min_p_key(o, r.max);
+    if (o.min_p > 0.f) kept = kept && key >= least_key(o, r.max);
   }
   const uint64_t share = kept ? (o.greedy ? 1 : w) : 0;
   uint64_t run = share;
@@ -651,7 +634,7 @@ __global__ __launch_bounds__(TH, TH == 256 ? (sizeof(T) == 4 ? 8 : 6) : 1) void 
     }
   }
   if (o.min_p > 0.f) {
-    const float bound = of_key(min_p_key(o, top));
+    const float bound = of_key(least_key(o, top));
     if (bound > last) {
       last = bound;
       last_idx = 0x7fffffff;

@@ -833,3 +833,20 @@ def test_sample_row_is_the_same_in_few_and_many_rows(V, dtype):
     for a, b in ((0, 1), (1, 513), (513, 1025), (1025, N)):
         tt, ll = draw(a, b)
         assert torch.equal(tt, token[a:b]) and torch.equal(ll, lp[a:b])
+
+
+@pytest.mark.parametrize("V", [5, 64, 90, 1500, 5000, 70000])
+def test_sample_min_p_next_to_zero(V):
+    """Borders top + log(min_p) temperature that cancel to about 0, where float32 keys are densest:
+    the logits lie on both sides of the border, at least a thousandth of the largest away from it."""
+    top = [float.fromhex("0x1.485ff2p+0"), 2.384186e-07, math.log(10.0), 2 * math.log(4.0)]
+    tau = [float.fromhex("0x1.1d3904p-1"), 1.0, 1.0, 2.0]
+    min_p = [0.1, 0.99999976, 0.1, 0.25]
+    shares = np.array([1.0, 0.25, -0.25, 1e-3, -1e-3])
+    z = np.stack([t * shares[np.arange(V) % 5] for t in top for _ in range(4)])
+    z = z.astype(np.float32).astype(np.float64)
+    N = len(z)
+    u = np.random.default_rng(V).random(N)
+    kw = dict(temperature=np.repeat(tau, 4), min_p=np.repeat(min_p, 4))
+    _check_sample(z, "f32", u, **kw)
+    _check_sample(z, "f32", u, top_k=np.full(N, 4 * V // 5), **kw)
