@@ -90,10 +90,11 @@ int tfm_embed_bwd(const tfm_embed* e, const int32_t* ids, const void* dout, floa
  *   the weights sum to 0),  dlogits = the gradient of loss with respect to the logits (nullable:
  *   loss alone), 0 in [n_class[n], V).
  *
- * Rows of weight 0 and rows without a logit above -inf are left out: row_loss and dlogits are 0
- * whatever else they hold (the weight of the latter still counts).  A -inf logit has q = 0 and no
- * gradient but -p; a NaN or +inf logit, and a teacher's logit that is NaN or +inf, give that row a
- * loss that is not finite and undefined gradients.  Teacher's -inf logits have p = 0.
+ * Rows of weight 0, rows without a class and rows whose classes all have a logit of -inf are left
+ * out: row_loss and dlogits are 0 whatever else they hold (the weight of the latter two still
+ * counts).  A -inf logit has q = 0 and no gradient but -p; a NaN or +inf logit, and a teacher's
+ * logit that is NaN or +inf, give that row a loss that is not finite and undefined gradients
+ * (alpha == 0 without a label leaves L no term: 0).  Teacher's -inf logits have p = 0.
  *
  * logits and dlogits: rows of V elements ld apart, the elements between rows untouched; dlogits
  * may be logits itself (in place) but must not overlap it otherwise.

@@ -81,7 +81,8 @@ __device__ __forceinline__ int row_classes(const DistillGeo& g, int64_t n) {
 
 // The row's scalars from its sums:
 //   S_t, S_1    sums of exp((s - mt) / tau) and exp(s - mt) outside J
-//   T_t, T_1    sums of exp((s - mj) / tau) and exp(s - mj) over J (unused without a tail)
+//   T_t, T_1    sums of exp((s - mj) / tau) and exp(s - mj) over J (unused without a tail; 0, or NaN
+//               where J has a NaN, if no logit of J lies above -inf)
 //   E, G        sums over J of e_j and e_j (log e_j - (s_j - mj) / tau), where p_j = e_j / E
 //               without a tail and e_j with one
 // m is the largest of all logits.  W lanes call it with the same values, W >= 8: each evaluates one
@@ -95,6 +96,11 @@ struct RowOut {
   double j_p, label;  //   - j_p e_j, and of the label: - label
   float c_t, c_1;     // gradient outside J: c_t exp((s - mt) / tau) + c_1 exp(s - mt)
 };
+// The largest logit as a row goes on with it: -inf where all are -inf and the row is left out, but
+// not where the others are NaN, which the maxima pass over and the sums do not.
+__device__ __forceinline__ float row_max(float m, double S_t, double T_t) {
+  return m == -INFINITY && !(S_t + T_t == 0.0) ? 0.f : m;
+}
 template <int W>
 __device__ __forceinline__ double of_lane(double v, int i) {
   if constexpr (W == 64) return from_lane(v, i);
@@ -112,7 +118,7 @@ __device__ __forceinline__ RowOut row_scalars(const DistillGeo& g, const RowSums
   const double x = exp64((lane & 2 ? d : back) * (lane & 1 ? 1.0 : itau));
   const double bt = of_lane<W>(x, 0), b1 = of_lane<W>(x, 1);
   double Zt = r.S_t * bt, Z1 = r.S_1 * b1;
-  if (g.tail && any) {
+  if (g.tail) {
     Zt += r.T_t * of_lane<W>(x, 2);
     Z1 += r.T_1 * of_lane<W>(x, 3);
   }
@@ -198,7 +204,6 @@ __global__ __launch_bounds__(256) void k_distill_small(DistillGeo g, int64_t fir
   m = group_max<W>(m);
   mt = group_max<W>(mt);
   tm = group_max<W>(tm);
-  const bool left_out = wn == 0.f || m == -INFINITY;
   const float mr = mt > -INFINITY ? mt : 0.f;
   const double lse = g.tail ? (double)g.lse[n] : 0.0;
   float sum_t = 0.f, sum_1 = 0.f;
@@ -212,7 +217,7 @@ __global__ __launch_bounds__(256) void k_distill_small(DistillGeo g, int64_t fir
       sum_1 += exp2_hw((x[i] - mr) * LOG2E);
     }
     if (in[i]) {
-      const double d = (double)x[i] - (double)m, y = d * itau;
+      const double d = m > -INFINITY ? (double)x[i] - (double)m : (double)x[i], y = d * itau;
       double lt;
       if (g.tail) {
         lt = (double)t[i] * itau - lse;
@@ -235,6 +240,8 @@ __global__ __launch_bounds__(256) void k_distill_small(DistillGeo g, int64_t fir
     r.T_t = group_sum<W>(r.T_t);
     r.T_1 = group_sum<W>(r.T_1);
   }
+  m = row_max(m, r.S_t, r.T_t);
+  const bool left_out = wn == 0.f || m == -INFINITY;
   const int y = g.labels ? g.labels[n] : -1;
   const bool known = y >= 0 && y < V;
   float sy = -INFINITY;
@@ -541,7 +548,7 @@ __global__ __launch_bounds__(TH, I == 32 ? 3 : 1) void k_distill_rows(DistillGeo
       const SetSums ss = sp.set[n];
       q[2] = ss.E; q[3] = ss.G; q[4] = ss.T_t; q[5] = ss.T_1;
     }
-    m = fmaxf(mj, mt);
+    m = row_max(fmaxf(mj, mt), q[0], q[4]);
     const double wtot = weight_total(g);
     const RowSums r = {q[0], q[1], q[4], q[5], q[2], q[3]};
     const RowOut o = row_scalars<64>(g, r, mt, mj, m, wtot != 0.0 ? (double)wn / wtot : 0.0,

@@ -850,3 +850,51 @@ def test_sample_min_p_next_to_zero(V):
     kw = dict(temperature=np.repeat(tau, 4), min_p=np.repeat(min_p, 4))
     _check_sample(z, "f32", u, **kw)
     _check_sample(z, "f32", u, top_k=np.full(N, 4 * V // 5), **kw)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [3, 12, 64, 200, 1024, 3000, 70000])
+@pytest.mark.parametrize("tail", [0, 1])
+@pytest.mark.parametrize("alpha,tau", [(1.0, 1.0), (0.5, 2.0), (0.0, 1.0)])
+def test_distill_rows_of_nan(tail, V, dtype, alpha, tau):
+    """A logit that is NaN shows in the row's loss where nothing lies above -inf, and where the NaN
+    stands on an entry without weight; rows of -inf beside them are left out, the rest keeps its
+    values.  Split rows, whole ones, unaligned gradients and short rows."""
+    nan, inf = np.nan, np.inf
+    rng = np.random.default_rng(V + tail)
+    N, k = 8, 2
+    s = _rounded(rng.normal(size=(N, V)), dtype)
+    idx = np.stack([rng.permutation(V)[:k] for _ in range(N)]).astype(np.int32)
+    top = rng.normal(size=(N, k)).astype(np.float32)
+    lse = np.array([ov._logsumexp(r / tau) + 1 for r in top]).astype(np.float32) if tail else None
+    labels = idx[:, 0].copy()
+    s[0] = nan
+    s[1] = -inf
+    s[1, idx[1, 0]] = nan                          # on an entry and the label
+    s[2] = -inf
+    s[2, (set(range(V)) - set(idx[2].tolist())).pop()] = nan   # outside the entries
+    s[3] = -inf                                    # left out
+    s[4, idx[4, 1]] = nan                          # on an entry that weighs nothing
+    top[4, 1] = -inf
+    s[5, idx[5]] = nan                             # on all entries, which weigh nothing
+    top[5] = -inf
+    ncls = np.full(N, V, np.int32)
+    s[6] = nan
+    ncls[6] = 0                                    # no class: left out
+    args = (idx, top, lse, labels if alpha < 1 else None, None, ncls, tau, alpha, tail)
+    ref = ov.distill_loss(s[[3, 6, 7]], *[a[[3, 6, 7]] if isinstance(a, np.ndarray) else a
+                                         for a in args])
+    for kw in (dict(), dict(doffset=1), dict(inplace=True), dict(pad=1)):
+        loss, rows, grad = _run_distill(s, dtype, *args, **kw)
+        assert np.isnan(loss)
+        for n in (0, 1, 2, 4, 5):
+            assert np.isnan(rows[n]) and np.isnan(grad[n]).any(), (n, rows[n])
+        for n in (3, 6):
+            assert rows[n] == 0 and not grad[n].any(), n
+        R = (s[7].max() - s[7].min()) / min(tau, 1.0)
+        e = (4 * R + 32 + V / 64) * U
+        assert abs(rows[7] - ref[1][2]) <= 2 * e * (2 * alpha * tau * tau + 1) + U * abs(ref[1][2])
+        want = ref[2][2] * 3 / N
+        # terms of at most 1 in every class, as alpha tau times two distributions and two more
+        assert np.all(np.abs(grad[7] - want) <= 2 * e * (2 * alpha * tau + 2) / N +
+                      (B if dtype == "bf16" else U) * np.abs(want))
