@@ -189,8 +189,8 @@ __global__ __launch_bounds__(TH, TH == 256 ? (sizeof(T) == 4 ? 8 : 6) : 1) void 
   constexpr int LOG_BINS = TH == 256 ? 9 : 11, BINS = 1 << LOG_BINS;
   __shared__ uint64_t hist[BINS];
   // classes as (key, ~index): larger is earlier in the order; and a part of them
-  __shared__ alignas(16) uint64_t list[LIST];
-  __shared__ uint64_t part_of[LIST];
+  __shared__ uint64_t list[LIST];
+  __shared__ alignas(16) uint64_t part_of[LIST];
   __shared__ uint32_t part_count;
   __shared__ uint64_t wbuf[NW];
   __shared__ uint64_t chunk[CHUNKS];
@@ -555,6 +555,8 @@ __global__ __launch_bounds__(TH, TH == 256 ? (sizeof(T) == 4 ? 8 : 6) : 1) void 
   // least q and few more, unless there are fewer than q in all.
   auto gather_top = [&](int q) __attribute__((always_inline)) -> uint32_t {
     constexpr int PER = TH / GROUPS;
+    static_assert(__alignof__(part_of) >= alignof(uint4) && sizeof(part_of) >= 4 * GROUPS,
+                  "the keys are read as uint4");
     uint32_t* keys = reinterpret_cast<uint32_t*>(part_of);
     uint32_t k = key_of(own_max);
 #pragma unroll
