@@ -43,9 +43,9 @@ extern "C" {
  *                   were.
  *   tfm_embed_bwd   dtable[V][E] (float32) = scale times the sum, over the positions that hold the
  *                   id, of dout's rows, in the order of the positions up to how the sum is split
- *                   (a split that depends on the ids and sizes alone); rows of ids that do not
- *                   occur are 0; with accumulate != 0 it is added to dtable and those rows are
- *                   left as they were.
+ *                   (a split that depends on the ids, sizes and dtype alone, not on strides or
+ *                   where the buffers lie); rows of ids that do not occur are 0; with accumulate
+ *                   != 0 it is added to dtable and those rows are left as they were.
  *
  * Limits: every n >= 0 and their product at most 2^27; 1 <= V <= 2^24; 1 <= E <= 2^16; strides in
  * [0, 2^40], the last row at most 2^48 elements from the first.  The forward's rows must not

@@ -21,6 +21,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+
 namespace tfm {
 namespace {
 
@@ -101,6 +103,32 @@ __device__ __forceinline__ void put(T* p, const float* v) {
     }
   } else {
     stv<VEC>(p, v);
+  }
+}
+
+// Vectors that start at any element, which global loads and stores take as they come.
+template <int VEC>
+__device__ __forceinline__ void ld_any(const float* p, float* v) {
+  __builtin_memcpy(v, p, 4 * VEC);
+}
+template <int VEC>
+__device__ __forceinline__ void ld_any(const bf16* p, float* v) {
+  if constexpr (VEC == 1) {
+    v[0] = ld(p);
+  } else {
+    uint32_t u[VEC / 2];
+    __builtin_memcpy(u, p, 2 * VEC);
+#pragma unroll
+    for (int i = 0; i < VEC / 2; ++i) halves(u[i], v + 2 * i);
+  }
+}
+template <int VEC, bool PAST>
+__device__ __forceinline__ void st_any(float* p, const float* v) {
+  if constexpr (PAST && VEC == 4) {
+    typedef f32x4 f32x4_any __attribute__((aligned(4)));
+    __builtin_nontemporal_store(f32x4{v[0], v[1], v[2], v[3]}, reinterpret_cast<f32x4_any*>(p));
+  } else {
+    __builtin_memcpy(p, v, 4 * VEC);
   }
 }
 
@@ -438,10 +466,10 @@ __device__ __forceinline__ void write_row(const EmbedGeo& g, float* dtable, int3
                                           const float* acc) {
   float* o = dtable + (int64_t)v * g.E + c;
   float x[VEC];
-  if (ADD) ldv<VEC>(o, x);
+  if (ADD) ld_any<VEC>(o, x);
 #pragma unroll
   for (int i = 0; i < VEC; ++i) x[i] = ADD ? x[i] + g.scale * acc[i] : g.scale * acc[i];
-  stv<VEC>(o, x);
+  st_any<VEC, false>(o, x);
 }
 
 // Lane i's value within each group of W lanes.
@@ -484,8 +512,8 @@ __device__ __forceinline__ void zero_rows(const EmbedGeo& g, const SumGeo& s,
       for (int q = 0; q < VEC / Z; ++q) {
         const int c = (int)blockIdx.y * W * VEC + (q * W + threadIdx.x % W) * Z;
         if (c >= g.E) continue;
-        if (s.past) put<Z, true>(o + c, zero);
-        else stv<Z>(o + c, zero);
+        if (s.past) st_any<Z, true>(o + c, zero);
+        else st_any<Z, false>(o + c, zero);
       }
     }
   }
@@ -539,7 +567,7 @@ __global__ __launch_bounds__(SUM_T) void k_embed_sum(EmbedGeo g, SumGeo s,
       for (int i = 0; i < SUM_U; ++i) {
         key[i] = from_lane<W>(key_w, t + i);
         const int64_t at = from_lane<W>(row_w, t + i < left ? t + i : 0);
-        ldv<VEC>(d + at, x[i]);
+        ld_any<VEC>(d + at, x[i]);
       }
 #pragma unroll
       for (int i = 0; i < SUM_U; ++i) {
@@ -683,11 +711,21 @@ int group_width(int32_t E, int vec) {
   return W;
 }
 
+// Widest vector that rows of E elements divide into, of at most `most` elements.
+int row_vec(int32_t E, int most) {
+  while (E % most) most /= 2;
+  return most;
+}
+
+// How the sorted positions are cut into groups and workgroups, and so the order of every sum, goes by
+// N, E and the type of the rows (`most` elements to 16 bytes) alone: rows and gradients that start on
+// smaller boundaries are read and written in the same vectors.
 // Sorted positions per group: enough groups for 16 waves on each of 256 CUs, which hide the row
 // loads' latency; at least 16, so that the edges' share of the traffic stays small.
-SumGeo sum_geo(const EmbedGeo& g, int vec) {
+SumGeo sum_geo(const EmbedGeo& g, int most) {
   SumGeo s;
   s.N = g.N;
+  const int vec = row_vec(g.E, most);
   s.W = group_width(g.E, vec);
   s.slices = (g.E + s.W * vec - 1) / (s.W * vec);
   const double groups = 4096.0 * (64 / s.W) / s.slices;
@@ -719,12 +757,8 @@ EmbedWs embed_ws(const EmbedGeo& g) {
   w.pair[0] = take((size_t)g.N * 8);
   w.pair[1] = take(nblk > 1 && passes > 1 ? (size_t)g.N * 8 : 0);
   w.cnt = take(nblk > 1 ? ((nblk + 1) << bits) * 4 : 0);
-  // the widest and the narrowest vectors bound the number of workgroups
-  size_t blocks = 0;
-  for (int vec = 1; vec <= 8; vec *= 2) {
-    const size_t n = (size_t)sum_geo(g, vec).nblk;
-    if (n > blocks) blocks = n;
-  }
+  // rows of either type
+  const size_t blocks = (size_t)std::max(sum_geo(g, 4).nblk, sum_geo(g, 8).nblk);
   w.part = take(blocks * 2 * (size_t)g.E * 4);
   w.total = off > 0 ? off : 256;
   return w;
@@ -785,7 +819,7 @@ hipError_t bwd_run(const EmbedGeo& g, const SumGeo& s, const int2* sorted, const
 template <class TO, int VEC>
 hipError_t bwd_vec(const EmbedGeo& g, const int2* sorted, const TO* dout,
                    float* dtable, float* part, int add, hipStream_t st) {
-  const SumGeo s = sum_geo(g, VEC);
+  const SumGeo s = sum_geo(g, 16 / (int)sizeof(TO));
 #define RUN(X)                                                                               \
   case X:                                                                                    \
     return add ? bwd_run<TO, VEC, X, true>(g, s, sorted, dout, dtable, part, st)         \
@@ -850,9 +884,7 @@ hipError_t launch_embed_bwd(const EmbedGeo& g, const int32_t* ids, const TO* dou
   }
   if (e != hipSuccess) return e;
   float* part = (float*)(w + W.part);
-  int vec = vec_of(g, dout);
-  while (vec > 1 && !fits(dtable, vec * 4 < 16 ? vec * 4 : 16)) vec /= 2;
-  switch (vec) {
+  switch (row_vec(g.E, 16 / (int)sizeof(TO))) {
     case 1: return bwd_vec<TO, 1>(g, sorted, dout, dtable, part, accumulate, st);
     case 2: return bwd_vec<TO, 2>(g, sorted, dout, dtable, part, accumulate, st);
     case 4: return bwd_vec<TO, 4>(g, sorted, dout, dtable, part, accumulate, st);

@@ -898,3 +898,32 @@ def test_distill_rows_of_nan(tail, V, dtype, alpha, tau):
         # terms of at most 1 in every class, as alpha tau times two distributions and two more
         assert np.all(np.abs(grad[7] - want) <= 2 * e * (2 * alpha * tau + 2) / N +
                       (B if dtype == "bf16" else U) * np.abs(want))
+
+
+@pytest.mark.parametrize("rows", ["f32", "bf16"])
+@pytest.mark.parametrize("N,V,E", [(30001, 997, 192), (20000, 3, 64), (5000, 700, 100),
+                                   (9001, 300, 33), (3000, 50, 1032)])
+@pytest.mark.parametrize("add", [False, True])
+def test_embed_bwd_is_the_same_wherever_the_rows_lie(N, V, E, rows, add):
+    """Rows and a gradient on smaller boundaries than a vector's, and rows farther apart: the sums
+    keep their order, so the gradient is the same bit for bit."""
+    import torch
+    from paper_2606_03681_amd import tfm
+    g = torch.Generator(device="cuda").manual_seed(N)
+    ids = torch.randint(-1, V, (1, 1, N), generator=g, device="cuda").int()
+    ids[torch.rand(ids.shape, generator=g, device="cuda") < 0.4] = V // 2
+    src = torch.randn((N, E), generator=g, device="cuda").to(_torch(rows))
+    start = torch.randn((V, E), generator=g, device="cuda")
+    want = None
+    for pad, offset, at in ((0, 0, 0), (8, 0, 0), (4, 4, 2), (2, 2, 1), (1, 1, 3), (7, 3, 0), (0, 1, 1)):
+        buf = torch.zeros(offset + N * (E + pad) + 8, dtype=_torch(rows), device="cuda")
+        buf[offset:offset + N * (E + pad)].view(N, E + pad)[:, :E] = src
+        e = _shape((1, 1, N), (0, 0, E + pad), E, V, rows, "f32", 0.7)
+        whole = torch.full((at + V * E + 5,), 77.0, device="cuda")
+        dtable = whole[at:at + V * E].view(V, E)
+        dtable.copy_(start)
+        ws = torch.full((tfm.embed_workspace_bytes(e),), 0xA5, dtype=torch.uint8, device="cuda")
+        tfm.embed_bwd(e, ids, buf[offset:], dtable, add, ws)
+        want = dtable.clone() if want is None else want
+        assert torch.equal(dtable, want), (pad, offset, at)
+        assert bool((whole[:at] == 77.0).all()) and bool((whole[at + V * E:] == 77.0).all())
