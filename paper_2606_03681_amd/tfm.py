@@ -313,7 +313,7 @@ def thinking_rows_bwd(dims, n_train, cell_mask, T, dX, dtable, accumulate, works
 
 
 def _nbytes(t):
-    return t.numel() * t.element_size()
+    return 0 if t is None else t.numel() * t.element_size()
 
 
 def layer_fwd_context(dims, n_train, cell_mask, X, params, Y, kv_cache, workspace, stream=None):
@@ -409,14 +409,14 @@ def decode_bwd(dims, ends, n_train, n_feat, Y, params, dlogits, dY, grads, accum
 
 def _tensors(call, *wanted):
     """(name, tensor, type, shape) of a call's device tensors, None for one left out: raises unless
-    every tensor has its type and shape, lies side by side (shape None: not looked at) and all are
-    on the current device."""
+    every tensor has its type (None: any) and shape, lies side by side (shape None: not looked at)
+    and all are on the current device."""
     import torch
     device = None
     for name, t, dtype, shape in wanted:
         if t is None:
             continue
-        if t.dtype != dtype:
+        if dtype is not None and t.dtype != dtype:
             raise ValueError(f"{call}: {name} is {t.dtype}, {dtype} wanted")
         if shape is not None and (t.shape != shape or not t.is_contiguous()):
             raise ValueError(f"{call}: {name} has shape {tuple(t.shape)} and strides {t.stride()}, "
@@ -477,7 +477,7 @@ def embed_bwd(e, ids, dout, dtable, accumulate, workspace, stream=None):
     _tensors("embed_bwd", ("ids", ids, torch.int32, tuple(e.n)),
              _embed_rows("embed_bwd", e, "dout", dout),
              ("dtable", dtable, torch.float32, (e.V, e.E)),
-             ("workspace", workspace, workspace.dtype, None))
+             ("workspace", workspace, None, None))
     rc = lib().tfm_embed_bwd(ctypes.byref(e), _ptr(ids), _ptr(dout), _ptr(dtable),
                              int(bool(accumulate)), _ptr(workspace), _nbytes(workspace),
                              _stream(stream))
@@ -502,7 +502,7 @@ def distill_loss(d, logits, top_idx, top_logit, top_lse, labels, weights, n_clas
              ("top_lse", top_lse, f32, (d.N,)), ("labels", labels, i32, (d.N,)),
              ("weights", weights, f32, (d.N,)), ("n_class", n_class, i32, (d.N,)),
              ("loss", loss, f32, None), ("row_loss", row_loss, f32, (d.N,)),
-             ("workspace", workspace, workspace.dtype, None))
+             ("workspace", workspace, None, None))
     rc = lib().tfm_distill_loss(ctypes.byref(d), _ptr(logits), _ptr(top_idx), _ptr(top_logit),
                                 _ptr(top_lse), _ptr(labels), _ptr(weights), _ptr(n_class),
                                 _ptr(loss), _ptr(row_loss), _ptr(dlogits), _ptr(workspace),

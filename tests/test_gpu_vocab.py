@@ -927,3 +927,17 @@ def test_embed_bwd_is_the_same_wherever_the_rows_lie(N, V, E, rows, add):
         want = dtable.clone() if want is None else want
         assert torch.equal(dtable, want), (pad, offset, at)
         assert bool((whole[:at] == 77.0).all()) and bool((whole[at + V * E:] == 77.0).all())
+
+
+def test_missing_workspaces_refused():
+    import torch
+    from paper_2606_03681_amd import tfm
+    ids = torch.zeros((1, 1, 4), dtype=torch.int32, device="cuda")
+    rows, table = torch.zeros((4, 32), device="cuda"), torch.zeros((10, 32), device="cuda")
+    with pytest.raises(tfm.TfmError, match="workspace"):
+        tfm.embed_bwd(_shape((1, 1, 4), (0, 0, 32), 32, 10, "f32", "f32", 1.0), ids, rows, table,
+                      False, None)
+    z, one = torch.zeros((2, 8), device="cuda"), torch.zeros((2, 1), device="cuda")
+    with pytest.raises(tfm.TfmError, match="workspace"):
+        tfm.distill_loss(tfm.make_distill(2, 8, 1, 8, "f32"), z, one.int(), one, None, None, None,
+                         None, torch.zeros(1, device="cuda"), None, z, None)

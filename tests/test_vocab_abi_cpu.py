@@ -210,3 +210,21 @@ def test_distillation_temperatures_refused(tau):
     assert "temperature" in tfm.last_error()
     for ok in (2.0 ** -20, 2.0 ** 20):
         assert tfm.distill_workspace_bytes(_distill(temperature=ok)) > 0
+
+
+def test_binding_leaves_a_missing_workspace_to_the_library():
+    """No workspace: the library's own refusal (on the GPU for the calls that look at devices first,
+    as here), not an error on the way to it."""
+    import torch
+    e, ids = _embed(n=(1, 1, 4), stride=(0, 0, 32)), torch.zeros((1, 1, 4), dtype=torch.int32)
+    rows, table = torch.zeros((4, 32), dtype=torch.bfloat16), torch.zeros((10, 32))
+    with pytest.raises(ValueError, match="not on the current GPU"):
+        tfm.embed_bwd(e, ids, rows, table, False, None)
+    d = _distill(N=2, V=8, k=1, ld=8)
+    z, one = torch.zeros((2, 8), dtype=torch.bfloat16), torch.zeros((2, 1))
+    with pytest.raises(ValueError, match="not on the current GPU"):
+        tfm.distill_loss(d, z, one.int(), one, None, None, None, None, torch.zeros(1), None, z, None)
+    dims = tfm.make_dims(B=2, R=64, C=8, E=64, heads=4, H=128, dtype="f32")
+    with pytest.raises(tfm.TfmError, match="workspace"):
+        tfm.decode_bwd(dims, tfm.make_ends(1, [0], 8, 0, 128, 10, 0), [5, 6], [8, 8], FAKE, FAKE,
+                       FAKE, FAKE, FAKE, False, None, stream=0)
