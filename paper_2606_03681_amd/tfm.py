@@ -246,8 +246,12 @@ def _check(rc):
 def _stream(stream):
     if stream is None:
         import torch
-        # the handle itself, 0.3 us: torch.cuda.current_stream() takes 2.7 us to build a Stream
-        return torch._C._cuda_getCurrentRawStream(torch.cuda.current_device())
+        # the handle itself, 0.3 us: torch.cuda.current_stream() takes 2.7 us to build a Stream, but
+        # is the public way to it
+        raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+        if raw is None:
+            return torch.cuda.current_stream().cuda_stream
+        return raw(torch.cuda.current_device())
     return stream if isinstance(stream, int) else stream.cuda_stream
 
 

@@ -228,3 +228,17 @@ def test_binding_leaves_a_missing_workspace_to_the_library():
     with pytest.raises(tfm.TfmError, match="workspace"):
         tfm.decode_bwd(dims, tfm.make_ends(1, [0], 8, 0, 128, 10, 0), [5, 6], [8, 8], FAKE, FAKE,
                        FAKE, FAKE, FAKE, False, None, stream=0)
+
+
+def test_current_stream_with_and_without_the_raw_handle(monkeypatch):
+    """The binding takes the current stream's handle from whichever call torch has."""
+    import types
+
+    import torch
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 3)
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda: types.SimpleNamespace(cuda_stream=77))
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 100 + d, raising=False)
+    assert tfm._stream(None) == 103
+    monkeypatch.delattr(torch._C, "_cuda_getCurrentRawStream")
+    assert tfm._stream(None) == 77
+    assert tfm._stream(5) == 5 and tfm._stream(types.SimpleNamespace(cuda_stream=6)) == 6
