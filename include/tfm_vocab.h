@@ -15,7 +15,8 @@
  * Conventions: the caller owns every buffer and the library allocates nothing; calls are
  * asynchronous on `stream` (a hipStream_t, NULL = the null stream) of the current device and may
  * be captured into a graph; pointers are device pointers, aligned to their elements (workspaces to
- * 16 bytes); sums run in a fixed order (results are bitwise reproducible); on a negative return
+ * 16 bytes); sums run in a fixed order (the same call gives the same bits again; the last bits of a
+ * distillation may differ between buffers that lie otherwise to 16 bytes); on a negative return
  * (the codes of tfm_layer.h) nothing was launched and tfm_last_error() describes the error.  dtype
  * fields are tfm_dtype values.  Sums, softmax statistics and losses are held in 32 or 64 bits and
  * each bfloat16 output is rounded once.  Calls that run at the same time need workspaces of their
@@ -97,7 +98,8 @@ int tfm_embed_bwd(const tfm_embed* e, const int32_t* ids, const void* dout, floa
  * (alpha == 0 without a label leaves L no term: 0).  Teacher's -inf logits have p = 0.
  *
  * logits and dlogits: rows of V elements ld apart, the elements between rows untouched; dlogits
- * may be logits itself (in place) but must not overlap it otherwise.
+ * may be logits itself (in place) but must not overlap it otherwise (from the first element of the
+ * first row to the last of the last: rows that lie between the other's rows are refused too).
  * Limits: 0 <= N <= 2^27, 1 <= V <= 2^18, 1 <= k <= 256, V <= ld <= 2^40, N ld <= 2^48,
  * temperature in [2^-20, 2^20] (D is held to about 2^-22, so the loss's error grows with tau^2),
  * 0 <= alpha <= 1. */

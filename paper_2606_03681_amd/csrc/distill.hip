@@ -14,7 +14,7 @@
 // bfloat16 with a label's softmax at another temperature 227 us (3.6 TB/s; a copy 171: two
 // exponentials per class and pass are 164 us of issue beside it).  Short rows are bound by what a row
 // costs in 64 bits (2^21 x 10: 0.22 ns a row), few long ones by latency (7 x 131,072: 22 us in three
-// launches).
+// launches, the first of which waits for the one workgroup that has the teacher's entries).
 #include "math64.h"
 #include "mfma.h"
 #include "vocab.h"
@@ -151,7 +151,9 @@ __device__ __forceinline__ RowOut row_scalars(const DistillGeo& g, const RowSums
 }
 
 // ---- rows of up to 1,024 classes ----------------------------------------------------------------
-// W lanes to a row, class lane + W i in register i.
+// W lanes to a row, class lane + W i in register i.  Bound by its 64-bit arithmetic and element loads:
+// 65,536 x 300 float32 157 us (a copy 33), 32,768 x 1,000 206 (55).  Where one wave's registers end
+// the kernel for longer rows is the faster one: 32,768 x 1,024 206 us here, x 1,028 146 there.
 constexpr int SMALL_V = 1024;
 
 template <class T, int W, int I>
@@ -746,6 +748,9 @@ hipError_t launch_distill_rows(const DistillGeo& g, const T* logits, T* dlogits,
     if (np <= 2048) return run_split<T, 8>(g, sp, logits, dlogits, s);
     return run_split<T, 0>(g, sp, logits, dlogits, s);
   }
+  // Rows that the registers of a CU do not hold are read three times (512 rows: 65,536 float32 classes
+  // 62 us, 65,540 94; 131,072 bfloat16 73, 131,080 88), and so are those whose gradient lies otherwise
+  // to 16 bytes, which is then written element by element (8,192 x 5,000 float32 81 us, 263 so).
   // The fewest registers that hold the row, and few threads with many of them: more rows are in
   // flight on a CU, one being read while another is summed or written (4,096 x 50,021 bf16: 256
   // threads with 32 pieces, three rows, 224 us; 512 with 16, two, 244; 1,024 with 8, two, 270).

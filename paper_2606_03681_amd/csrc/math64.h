@@ -10,7 +10,7 @@ namespace tfm {
 constexpr double LN2_HI = 0x1.62e42fefa2000p-1, LN2_LO = 0x1.9ef35793c7673p-41;
 
 // exp(x) = 2^n exp(r), n = round(x / ln 2), |r| <= ln 2 / 2: Taylor's series to r^13 / 13!, whose
-// remainder is below 2^-58, by Horner's rule.  Relative error below 2^-51; NaN for NaN.
+// remainder is below 2^-57, by Horner's rule.  Relative error below 2^-51; NaN for NaN.
 __device__ __forceinline__ double exp64(double x) {
   if (x < -800.0) return 0.0;
   if (x > 800.0) return INFINITY;

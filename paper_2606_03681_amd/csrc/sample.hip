@@ -19,12 +19,19 @@
 // hundred cycles of arithmetic per 16 bytes, and few registers leave room for the waves that hide
 // the loads (the row held in registers took 250 of them at 32 classes per thread).
 //
-// Bound by arithmetic: a weight is 19 instructions in 64 bits, some 80 cycles of a SIMD for 64
-// classes.  us by mode (largest class / temperature alone / top-k / top-p / both / min-p):
+// What bounds it: a weight is 19 instructions in 64 bits, some 80 cycles of a SIMD for 64 classes, and
+// every class has one in the draw and another in the search for top_p: 21 us each of this chip over
+// 8,192 x 5,000.  Reading that row set from HBM takes 34 us and finding the largest class 42.  The
+// rest of a top-p call is reading the row four times through the caches, the histogram's atomics and,
+// with 256 threads, spilled registers.  Few rows leave CUs idle: a row stays in one workgroup.
+// us by mode (largest class / temperature alone / top-k / top-p / both / min-p):
 //    64 x 131,072 bfloat16    13   49   55  141   68   54     (the row on one of 64 CUs)
 //     1 x  32,000 float32    5.4   17   22   41   31   13
 //  8,192 x  5,000 float32     42   80  123  155  149   76     (164 MB, a copy's rate: 34)
 //  4,096 x    300 float32      8   17   33   35   45   20
+// Rows without a class that stands out (logits within 1/16) put all classes into few bins of the
+// histogram, whose atomics then wait for each other: top-p 286 us over 8,192 x 5,000 and 213 over
+// 64 x 131,072, the other modes as above.
 // A series of the seventh degree behind a table of 32 roots of two in LDS has 14 instructions: 7 %
 // less for 1,024 threads, but 15 % more for 256 threads and bfloat16, which then spill; both have to
 // round alike, so that a row's draw does not depend on its batch.
@@ -41,7 +48,8 @@ namespace {
 
 // 2^f, |f| <= 1 / 2, by powers up to f^11: the Taylor series (ln 2)^k / k! to f^13, whose last two
 // powers are replaced by the Chebyshev polynomials' lower terms (T13 without its first is within
-// 2^-12 of x^13, T12 within 2^-11 of x^12, x = 2 f).  Off by less than 2^-57.  In scalar registers,
+// 2^-12 of x^13, T12 within 2^-11 of x^12, x = 2 f).  Off by less than 2^-55.6, of which the degree is
+// 2^-56.9 and the rest the rounding of the coefficients.  In scalar registers,
 // where literals would each take two moves.
 struct PowerTable {
   double c[12];
