@@ -534,12 +534,13 @@ __global__ __launch_bounds__(TH, TH == 256 ? (sizeof(T) == 4 ? 8 : 6) : 1) void 
     if (MASS) {
       // Classes lighter than (1 - top_p) / V of the total hold less than 1 - top_p of it together:
       // the border lies above them, and they only count for the total (an addition to LDS costs
-      // more than the weight).  The total is at least the threads' largest kept weights together
-      // (1 % more is taken off for the roundings here).
+      // more than the weight).  The total is at least the threads' largest kept weights together.
+      // That share is 4 steps of the weights or more (V <= 2^18, 1 - top_p >= 2^-24), which roundings
+      // raise by 0.75: below exp(-0.21) of it none passes it.
       const uint64_t some = block_sum(kept(own_max, 0x7fffffff) ? r.weight(own_max) : 0);
       const float part = (float)((1.0 - (double)o.top_p) * (double)some / V *
                                  __builtin_amdgcn_ldexp(1.0, -S));
-      const double cut = (double)top + (double)o.tau * ((double)__logf(part) - 0.01);
+      const double cut = (double)top + (double)o.tau * ((double)__logf(part) - 0.22);
       from = (float)(cut - fabs(cut) * 0x1p-22);
       if (!(from <= top)) from = -INFINITY;
       __syncthreads();

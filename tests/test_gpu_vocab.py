@@ -941,3 +941,15 @@ def test_missing_workspaces_refused():
     with pytest.raises(tfm.TfmError, match="workspace"):
         tfm.distill_loss(tfm.make_distill(2, 8, 1, 8, "f32"), z, one.int(), one, None, None, None,
                          None, torch.zeros(1, device="cuda"), None, z, None)
+
+
+def test_sample_top_p_next_to_one_over_a_flat_tail():
+    """Two heavy classes and 262,142 light ones of 4.53 steps of 2^-44 each, which round to 5, while
+    top_p = 1 - 2^-24 leaves out 4.6 steps per class: by either count the last heavy class is drawn
+    where u reaches it, and no light one although all of them together may not be left out."""
+    V = 1 << 18
+    z = np.full((2, V), np.log(4.53) - 44 * np.log(2.0))
+    z[:, 0], z[:, 4096] = 0.0, np.log(0.15)       # (of two threads)
+    z = z.astype(np.float32).astype(np.float64)
+    p = np.full(2, 1 - 2.0 ** -24)
+    _check_sample(z, "f32", np.array([1 - 2.0 ** -24, 0.5]), top_p=p)
