@@ -11,7 +11,7 @@
 //
 // Both are bound by HBM where the rows are many: 327,680 ids into rows of 192 bfloat16 elements take
 // 26 us forward (as a copy of the 127 MB; the 0.4 MB table is read from the caches) and 54 us
-// backward (floor 26.6), of which the sums are 30 (4.2 TB/s), the sort 20 and the join 5: the sort
+// backward (floor 26.6), of which the sums are 29 (4.4 TB/s), the sort 20 and the join 5: the sort
 // moves little, but is three launches of a few dependent steps each.  40,000 ids into 50,021 rows of
 // 1,024 elements backward: 92 us (floor 60), the sums 64 of it (4.5 TB/s).  16 rows of 2,048 forward:
 // 3 us in the kernel, 11 with the host's call.  Sums by floating-point atomics would not be
