@@ -1,8 +1,8 @@
 /*
  * tfm_vocab.h — C ABI of the operators over discrete values at the two ends of the stack on
  * MI355X (gfx950): category or token ids in (an embedding table and its gradient), a teacher's
- * top logits as training signal (distillation), classes drawn from logits out (sampling).  They
- * stand beside the encoders and the decoder of tfm_ends.h:
+ * top logits as training signal (distillation), logits adjusted by what a row has said and may say,
+ * classes drawn from logits out (sampling).  They stand beside the encoders and the decoder of tfm_ends.h:
  *
  *     X      = encode(x) + embed(ids)         tfm_encode_fwd, tfm_embed_fwd (accumulate)
  *     logits = decode(blocks(X))              tfm_layer_fwd per block, tfm_decode_fwd
@@ -10,7 +10,7 @@
  *     dY, decoder grads                       tfm_decode_bwd
  *     dX, block grads                         tfm_layer_bwd per block
  *     encoder grads, dtable                   tfm_encode_bwd, tfm_embed_bwd
- *     answers                                 tfm_sample
+ *     answers                                 tfm_adjust_logits, tfm_sample
  *
  * Conventions: the caller owns every buffer and the library allocates nothing; calls are
  * asynchronous on `stream` (a hipStream_t, NULL = the null stream) of the current device and may
@@ -118,6 +118,40 @@ int tfm_distill_loss(const tfm_distill* d, const void* logits, const int32_t* to
                      const float* top_logit, const float* top_lse, const int32_t* labels,
                      const float* weights, const int32_t* n_class, float* loss, float* row_loss,
                      void* dlogits, void* workspace, size_t workspace_bytes, void* stream);
+
+/* ---- adjusted logits ----------------------------------------------------------------------------
+ * out[n][v] for the logits s[0 .. V) of row n, of which the classes [0, n_class[n]) count (nullable
+ * as above), step by step:
+ *
+ *   x = s_v
+ *   c = the number of j < n_history[n] with history[n][j] == v       (n_history null: n_hist)
+ *   c > 0:  x = x / r where x > 0, else x r, with r = repetition[n]  (null, <= 0 or NaN: 1)
+ *           x = x - (presence[n] + frequency[n] c)                   (null: 0)
+ *   x = x + bias[n][j], j the first entry with bias_idx[n][j] == v, if there is one
+ *   x = -inf where bit v % 32 of allowed[n][v / 32] is 0 (allowed null: all bits 1), whatever x was
+ *   x = -inf where v >= n_class[n]
+ *
+ * in float32, each step rounded once, and a bfloat16 output once more.  Entries of history and
+ * bias_idx outside [0, V) are absent; n_history is cut to [0, n_hist].  A NaN logit that is allowed
+ * stays one.  Rows of logits, out, history (n_hist entries), bias_idx and bias (n_bias entries each)
+ * and allowed (ceil(V / 32) words) lie ld elements of their own apart; ld_history, ld_bias and
+ * ld_allowed may be 0, one row for all.  out may be logits itself (with ld_out == ld: in place) but
+ * must not overlap it otherwise, nor anything else that the call reads; the elements between rows are
+ * left as they were.
+ * Limits: N, V, ld, ld_out as for tfm_sample; 0 <= n_hist, n_bias <= 2^27; ld_history, ld_bias and
+ * ld_allowed 0 or at least a row, at most 2^40, and the last row at most 2^48 elements from the first. */
+typedef struct {
+  int32_t N, V;
+  int32_t dtype;          /* of logits and out */
+  int32_t n_hist, n_bias; /* entries of a row of history and of bias_idx, 0: none */
+  int64_t ld, ld_out;
+  int64_t ld_history, ld_bias, ld_allowed;
+} tfm_adjust;
+
+int tfm_adjust_logits(const tfm_adjust* a, const void* logits, const int32_t* n_class,
+                      const int32_t* history, const int32_t* n_history, const float* repetition,
+                      const float* presence, const float* frequency, const int32_t* bias_idx,
+                      const float* bias, const uint32_t* allowed, void* out, void* stream);
 
 /* ---- sampling ---------------------------------------------------------------------------------
  * Draws one class per row from the logits s[0 .. V), of which the classes [0, n_class[n]) count

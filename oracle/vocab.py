@@ -1,5 +1,5 @@
 """Float64 CPU oracle of the operators over discrete values: embedding rows and their gradient,
-distillation from a teacher's top logits, sampling with temperature, top-k, top-p and min-p.
+distillation from a teacher's top logits, adjusted logits, sampling with temperature, top-k, top-p and min-p.
 
 TEST INFRASTRUCTURE ONLY, like the rest of this package.  Each function is the definition written
 out for one row (or one id) after another; nothing is shared with the GPU package.
@@ -96,6 +96,37 @@ def distill_loss(s, idx, top, lse, labels, weights, n_class, tau, alpha, tail):
     with np.errstate(invalid="ignore"):
         loss = (w * rows)[w != 0].sum() / total if total != 0 else 0.0
     return loss, rows, grad
+
+
+# ---- adjusted logits ---------------------------------------------------------------------------
+
+def adjust_row(s, n_class=None, history=(), repetition=1.0, presence=0.0, frequency=0.0,
+               bias_idx=(), bias=(), allowed=None):
+    """The logits of one row after penalties, biases and the mask (see include/tfm_vocab.h), and what
+    the roundings of its steps are relative to: the sum of the magnitudes that a class went through."""
+    x = np.array(s, dtype=np.float64)
+    V = len(x)
+    size = np.zeros(V)
+    r = repetition if repetition > 0 else 1.0
+    for v in range(V):
+        c = sum(1 for t in history if t == v)
+        if c:
+            x[v] = x[v] / r if x[v] > 0 else x[v] * r
+            size[v] += abs(x[v])
+            less = presence + frequency * c
+            size[v] += 2 * abs(frequency * c) + abs(presence)
+            x[v] = x[v] - less
+            size[v] += abs(x[v])
+        for i, b in zip(bias_idx, bias):
+            if i == v:
+                x[v] = x[v] + b
+                size[v] += abs(x[v])
+                break
+        if allowed is not None and not (int(allowed[v // 32]) >> (v % 32)) & 1:
+            x[v] = -np.inf
+        if n_class is not None and v >= n_class:
+            x[v] = -np.inf
+    return x, size
 
 
 # ---- sampling ----------------------------------------------------------------------------------

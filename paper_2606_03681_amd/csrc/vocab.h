@@ -1,5 +1,5 @@
 // Kernels of the operators over discrete values (include/tfm_vocab.h): embedding rows and their
-// gradient, distillation from a teacher's top logits, sampling.
+// gradient, distillation from a teacher's top logits, adjusted logits, sampling.
 #pragma once
 
 #include "common.h"
@@ -51,6 +51,22 @@ hipError_t launch_distill_weights(DistillGeo& g, hipStream_t s);
 template <class T>
 hipError_t launch_distill_rows(const DistillGeo& g, const T* logits, T* dlogits, hipStream_t s);
 hipError_t launch_distill_total(const DistillGeo& g, float* loss, hipStream_t s);
+
+struct AdjustGeo {
+  int64_t N, ld, ld_out, ld_history, ld_bias, ld_allowed;
+  int32_t V, n_hist, n_bias;
+  const int32_t* ncls;      // nullable, as are all but bias_idx and bias where n_bias > 0
+  const int32_t* history;
+  const int32_t* n_history;
+  const float* repetition;
+  const float* presence;
+  const float* frequency;
+  const int32_t* bias_idx;
+  const float* bias;
+  const uint32_t* allowed;
+};
+template <class T>
+hipError_t launch_adjust(const AdjustGeo& g, const T* logits, T* out, hipStream_t s);
 
 struct SampleGeo {
   int64_t N, ld;

@@ -1,5 +1,5 @@
 // Host side of the C ABI declared in include/tfm_vocab.h: argument validation, workspace layouts
-// and launch sequences of the embedding, the distillation loss and the sampler.
+// and launch sequences of the embedding, the distillation loss, the adjusted logits and the sampler.
 #include "tfm_vocab.h"
 
 #include <hip/hip_runtime.h>
@@ -132,6 +132,37 @@ int distill_check(const tfm_distill* d) {
   return TFM_OK;
 }
 
+// ---- adjusted logits ---------------------------------------------------------------------------
+
+// Rows of `width` elements ld apart, 0: one for all.
+int side_rows(const char* name, int64_t N, int64_t width, int64_t ld) {
+  if (ld != 0 && (ld < width || ld > kMaxStride))
+    return fail(TFM_ERR_DIMS, "%s=%lld is neither 0 nor in [%lld, 2^40]", name, (long long)ld,
+                (long long)width);
+  if (N > 1 && (double)(N - 1) * (double)ld > kMaxReach)
+    return fail(TFM_ERR_DIMS, "%s: the rows reach over more than 2^48 elements", name);
+  return TFM_OK;
+}
+
+int adjust_check(const tfm_adjust* a) {
+  if (!a) return fail(TFM_ERR_POINTER, "the adjustment's description is null");
+  int rc = logits_check(a->N, a->V, a->dtype, a->ld);
+  if (!rc) rc = logits_check(a->N, a->V, a->dtype, a->ld_out);
+  if (rc) return rc;
+  if (a->n_hist < 0 || a->n_hist > kMaxRows || a->n_bias < 0 || a->n_bias > kMaxRows)
+    return fail(TFM_ERR_DIMS, "n_hist=%d or n_bias=%d outside [0, 2^27]", a->n_hist, a->n_bias);
+  rc = side_rows("ld_history", a->N, a->n_hist, a->ld_history);
+  if (!rc) rc = side_rows("ld_bias", a->N, a->n_bias, a->ld_bias);
+  if (!rc) rc = side_rows("ld_allowed", a->N, (a->V + 31) / 32, a->ld_allowed);
+  return rc;
+}
+
+// Whether [p, p + bytes) and [q, q + more) share memory.
+bool overlap(const void* p, double bytes, const void* q, double more) {
+  return p && q && (double)(uintptr_t)p < (double)(uintptr_t)q + more &&
+         (double)(uintptr_t)q < (double)(uintptr_t)p + bytes;
+}
+
 }  // namespace
 
 extern "C" {
@@ -245,6 +276,54 @@ int tfm_distill_loss(const tfm_distill* d, const void* logits, const int32_t* to
       STEP("distill_rows/hbm", tfm::launch_distill_rows(g, (const float*)logits, (float*)dlogits, st));
   }
   STEP("distill_loss/hbm", tfm::launch_distill_total(g, loss, st));
+  return TFM_OK;
+}
+
+int tfm_adjust_logits(const tfm_adjust* a, const void* logits, const int32_t* n_class,
+                      const int32_t* history, const int32_t* n_history, const float* repetition,
+                      const float* presence, const float* frequency, const int32_t* bias_idx,
+                      const float* bias, const uint32_t* allowed, void* out, void* stream) {
+  int rc = adjust_check(a);
+  if (rc) return rc;
+  if (a->N == 0) return TFM_OK;
+  const size_t es = elem(a->dtype);
+  if (!aligned(logits, es) || !aligned(out, es))
+    return fail(TFM_ERR_POINTER, "logits and out must be non-null and aligned to their elements");
+  if (a->n_hist > 0 && !aligned(history, 4))
+    return fail(TFM_ERR_POINTER, "history must be non-null and 4-byte aligned where n_hist > 0");
+  if (a->n_bias > 0 && (!aligned(bias_idx, 4) || !aligned(bias, 4)))
+    return fail(TFM_ERR_POINTER, "bias_idx and bias must be non-null and 4-byte aligned where "
+                                 "n_bias > 0");
+  if (!aligned_or_null(n_class, 4) || !aligned_or_null(n_history, 4) ||
+      !aligned_or_null(repetition, 4) || !aligned_or_null(presence, 4) ||
+      !aligned_or_null(frequency, 4) || !aligned_or_null(allowed, 4))
+    return fail(TFM_ERR_POINTER, "n_class, n_history, repetition, presence, frequency and allowed "
+                                 "must be 4-byte aligned");
+  const double last = a->N - 1, wide = (last * a->ld + a->V) * es, room = (last * a->ld_out + a->V) * es;
+  if (!(logits == out && a->ld == a->ld_out) && overlap(logits, wide, out, room))
+    return fail(TFM_ERR_POINTER, "out overlaps logits without being logits, rows as far apart");
+  struct { const char* name; const void* p; double bytes; } others[] = {
+      {"n_class", n_class, 4. * a->N}, {"n_history", n_history, 4. * a->N},
+      {"repetition", repetition, 4. * a->N}, {"presence", presence, 4. * a->N},
+      {"frequency", frequency, 4. * a->N},
+      {"history", a->n_hist ? history : nullptr, 4. * (last * a->ld_history + a->n_hist)},
+      {"bias_idx", a->n_bias ? bias_idx : nullptr, 4. * (last * a->ld_bias + a->n_bias)},
+      {"bias", a->n_bias ? bias : nullptr, 4. * (last * a->ld_bias + a->n_bias)},
+      {"allowed", allowed, 4. * (last * a->ld_allowed + (a->V + 31) / 32)}};
+  for (const auto& o : others)
+    if (overlap(o.p, o.bytes, out, room)) return fail(TFM_ERR_POINTER, "out overlaps %s", o.name);
+  hipStream_t st = (hipStream_t)stream;
+  tfm::AdjustGeo g;
+  g.N = a->N; g.ld = a->ld; g.ld_out = a->ld_out;
+  g.ld_history = a->ld_history; g.ld_bias = a->ld_bias; g.ld_allowed = a->ld_allowed;
+  g.V = a->V; g.n_hist = a->n_hist; g.n_bias = a->n_bias;
+  g.ncls = n_class; g.history = a->n_hist ? history : nullptr; g.n_history = n_history;
+  g.repetition = repetition; g.presence = presence; g.frequency = frequency;
+  g.bias_idx = bias_idx; g.bias = bias; g.allowed = allowed;
+  if (a->dtype == TFM_BF16)
+    STEP("adjust_logits/hbm", tfm::launch_adjust(g, (const tfm::bf16*)logits, (tfm::bf16*)out, st));
+  else
+    STEP("adjust_logits/hbm", tfm::launch_adjust(g, (const float*)logits, (float*)out, st));
   return TFM_OK;
 }
 

@@ -1,5 +1,5 @@
 """Thin ctypes binding of libtfmlayer.so (C ABI in include/tfm_layer.h, include/tfm_ends.h,
-include/tfm_vocab.h and include/tfm_optim.h).
+include/tfm_vocab.h, include/tfm_cache.h and include/tfm_optim.h).
 
 Argument marshalling only: every step of the layer runs in the library's HIP kernels.  torch
 supplies device memory and the stream.  There is no fallback: if the library is missing, every
@@ -32,6 +32,8 @@ EXPORTS = ("tfm_layer_param_count", "tfm_layer_saved_bytes", "tfm_layer_workspac
            "tfm_encode_bwd", "tfm_decode_fwd", "tfm_decode_loss", "tfm_decode_bwd",
            "tfm_embed_workspace_bytes", "tfm_embed_fwd", "tfm_embed_bwd",
            "tfm_distill_workspace_bytes", "tfm_distill_loss", "tfm_sample",
+           "tfm_adjust_logits", "tfm_cache8_bytes", "tfm_cache8_append",
+           "tfm_cache8_attend_workspace_bytes", "tfm_cache8_attend",
            "tfm_clip_workspace_bytes",
            "tfm_clip_scale", "tfm_sfadamw_step", "tfm_muon_workspace_bytes", "tfm_muon_step")
 
@@ -113,6 +115,60 @@ def make_sampling(N, V, ld, dtype):
     return tfm_sampling(int(N), int(V), int(_DTYPES.get(dtype, dtype)), int(ld))
 
 
+class tfm_adjust(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("N", "V", "dtype", "n_hist", "n_bias")] + \
+        [(n, ctypes.c_int64) for n in ("ld", "ld_out", "ld_history", "ld_bias", "ld_allowed")]
+
+
+def make_adjust(N, V, ld, dtype, n_hist=0, n_bias=0, ld_out=None, ld_history=None, ld_bias=None,
+                ld_allowed=None):
+    """Elements between the rows of each array: ld_out like ld, the others side by side if None."""
+    V, n_hist, n_bias = int(V), int(n_hist), int(n_bias)
+    return tfm_adjust(int(N), V, int(_DTYPES.get(dtype, dtype)), n_hist, n_bias, int(ld),
+                      int(ld if ld_out is None else ld_out),
+                      n_hist if ld_history is None else int(ld_history),
+                      n_bias if ld_bias is None else int(ld_bias),
+                      (V + 31) // 32 if ld_allowed is None else int(ld_allowed))
+
+
+class tfm_cache8(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("heads", "d", "page", "n_pages")]
+
+
+def make_cache8(heads, d, page, n_pages):
+    return tfm_cache8(int(heads), int(d), int(page), int(n_pages))
+
+
+class tfm_cache8_rows(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "L", "max_pages", "dtype")] + \
+        [(n, ctypes.c_int64 * 3) for n in ("stride_k", "stride_v")]
+
+
+def make_cache8_rows(B, L, max_pages, dtype, stride_k, stride_v):
+    """stride_k, stride_v: elements between sequences, rows and heads."""
+    if len(stride_k) != 3 or len(stride_v) != 3:
+        raise ValueError(f"need three strides each, got {stride_k} and {stride_v}")
+    return tfm_cache8_rows(int(B), int(L), int(max_pages), int(_DTYPES.get(dtype, dtype)),
+                           tuple(map(int, stride_k)), tuple(map(int, stride_v)))
+
+
+class tfm_cache8_query(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("B", "L", "max_pages", "max_len", "heads", "causal",
+                                               "dtype")] + [("scale", ctypes.c_float)] + \
+        [(n, ctypes.c_int64 * 3) for n in ("stride_q", "stride_out")]
+
+
+def make_cache8_query(B, L, heads, max_pages, dtype, stride_q, stride_out, scale, causal=False,
+                      max_len=0):
+    """stride_q, stride_out: elements between sequences, rows and heads; max_len: no sequence is
+    longer (0: not said)."""
+    if len(stride_q) != 3 or len(stride_out) != 3:
+        raise ValueError(f"need three strides each, got {stride_q} and {stride_out}")
+    return tfm_cache8_query(int(B), int(L), int(max_pages), int(max_len), int(heads),
+                            int(bool(causal)), int(_DTYPES.get(dtype, dtype)), float(scale),
+                            tuple(map(int, stride_q)), tuple(map(int, stride_out)))
+
+
 def lib():
     """Loads the library (once).  Raises if it has not been built."""
     global _lib
@@ -173,6 +229,18 @@ def lib():
         L.tfm_distill_loss.argtypes = [P(tfm_distill)] + [vp] * 11 + [sz, vp]
         L.tfm_sample.restype = i32
         L.tfm_sample.argtypes = [P(tfm_sampling)] + [vp] * 10
+        L.tfm_adjust_logits.restype = i32
+        L.tfm_adjust_logits.argtypes = [P(tfm_adjust)] + [vp] * 12
+        C8 = P(tfm_cache8)
+        L.tfm_cache8_bytes.restype = sz
+        L.tfm_cache8_bytes.argtypes = [C8]
+        L.tfm_cache8_append.restype = i32
+        L.tfm_cache8_append.argtypes = [C8, P(tfm_cache8_rows)] + [vp] * 6 + [sz, vp]
+        L.tfm_cache8_attend_workspace_bytes.restype = sz
+        L.tfm_cache8_attend_workspace_bytes.argtypes = [C8, P(tfm_cache8_query)]
+        L.tfm_cache8_attend.restype = i32
+        L.tfm_cache8_attend.argtypes = [C8, P(tfm_cache8_query)] + [vp] * 5 + [sz] + [vp] * 3 + \
+            [sz, vp]
         i64, f32 = ctypes.c_int64, ctypes.c_float
         L.tfm_clip_workspace_bytes.restype = sz
         L.tfm_clip_workspace_bytes.argtypes = [i32, P(i64)]
@@ -436,25 +504,43 @@ def _torch_dtype(dtype):
     return torch.bfloat16 if dtype == TFM_BF16 else torch.float32
 
 
-def _embed_rows(call, e, name, t):
-    """The activations of an embedding call: from their first row on, room for the last."""
-    (a, b, c), (x, y, z) = e.n, e.stride
+def _strided_rows(call, name, t, dtype, shape, stride, width):
+    """Rows of `width` elements along three axes: from the first row on, room for the last."""
+    (a, b, c), (x, y, z) = shape, stride
     n, reach = a * b * c, (a - 1) * x + (b - 1) * y + (c - 1) * z
     room = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
-    if n and reach + e.E > room:
-        raise ValueError(f"{call}: {name} has room for {room} elements, {reach + e.E} wanted")
-    return name, t, _torch_dtype(e.dtype), None
+    if n and reach + width > room:
+        raise ValueError(f"{call}: {name} has room for {room} elements, {reach + width} wanted")
+    return name, t, dtype, None
 
 
-def _logit_rows(call, d, name, t):
+def _embed_rows(call, e, name, t):
+    """The activations of an embedding call."""
+    return _strided_rows(call, name, t, _torch_dtype(e.dtype), e.n, e.stride, e.E)
+
+
+def _side_rows(call, a, name, t, dtype, width, ld):
+    """Rows of what goes with a row of logits, ld elements apart: room for the last."""
+    if t is not None and a.N and width:
+        room = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
+        if (a.N - 1) * ld + width > room:
+            raise ValueError(f"{call}: {name} has room for {room} elements, "
+                             f"{(a.N - 1) * ld + width} wanted")
+        if t.stride(-1) != 1 and t.shape[-1] > 1:
+            raise ValueError(f"{call}: the rows of {name} are {t.stride(-1)} elements a step")
+    return name, t, dtype, None
+
+
+def _logit_rows(call, d, name, t, ld=None):
     """Rows of logits, ld elements apart."""
     if t is None:
         return name, t, None, None
     N, V = d.N, d.V
+    ld = d.ld if ld is None else ld
     rows, step = t.stride() if t.dim() == 2 else (0, 0)
-    if t.shape != (N, V) or (V > 1 and N and step != 1) or (N > 1 and rows != d.ld):
+    if t.shape != (N, V) or (V > 1 and N and step != 1) or (N > 1 and rows != ld):
         raise ValueError(f"{call}: {name} has shape {tuple(t.shape)} and strides {t.stride()}, "
-                         f"({N}, {V}) with rows {d.ld} apart wanted")
+                         f"({N}, {V}) with rows {ld} apart wanted")
     return name, t, _torch_dtype(d.dtype), None
 
 
@@ -528,6 +614,82 @@ def sample(s, logits, n_class, temperature, top_k, top_p, min_p, u, token, logpr
     rc = lib().tfm_sample(ctypes.byref(s), _ptr(logits), _ptr(n_class), _ptr(temperature),
                           _ptr(top_k), _ptr(top_p), _ptr(min_p), _ptr(u), _ptr(token),
                           _ptr(logprob), _stream(stream))
+    _check(rc)
+
+
+def adjust_logits(a, logits, n_class, history, n_history, repetition, presence, frequency,
+                  bias_idx, bias, allowed, out, stream=None):
+    """tfm_adjust_logits.  logits, out: device [N, V], rows a.ld and a.ld_out apart (out may be
+    logits); n_class, n_history int32 [N], repetition, presence, frequency float32 [N], each or None;
+    history int32, bias_idx int32, bias float32 and allowed int32 (bits): first elements of rows
+    a.ld_history, a.ld_bias and a.ld_allowed apart, each or None."""
+    import torch
+    i32, f32, N = torch.int32, torch.float32, (a.N,)
+    call = "adjust_logits"
+    _tensors(call, _logit_rows(call, a, "logits", logits),
+             _logit_rows(call, a, "out", out, a.ld_out), ("n_class", n_class, i32, N),
+             _side_rows(call, a, "history", history, i32, a.n_hist, a.ld_history),
+             ("n_history", n_history, i32, N), ("repetition", repetition, f32, N),
+             ("presence", presence, f32, N), ("frequency", frequency, f32, N),
+             _side_rows(call, a, "bias_idx", bias_idx, i32, a.n_bias, a.ld_bias),
+             _side_rows(call, a, "bias", bias, f32, a.n_bias, a.ld_bias),
+             _side_rows(call, a, "allowed", allowed, i32, (a.V + 31) // 32, a.ld_allowed))
+    rc = lib().tfm_adjust_logits(ctypes.byref(a), _ptr(logits), _ptr(n_class), _ptr(history),
+                                 _ptr(n_history), _ptr(repetition), _ptr(presence),
+                                 _ptr(frequency), _ptr(bias_idx), _ptr(bias), _ptr(allowed),
+                                 _ptr(out), _stream(stream))
+    _check(rc)
+
+
+def cache8_bytes(c):
+    return lib().tfm_cache8_bytes(ctypes.byref(c))
+
+
+def cache8_views(c, pool):
+    """The keys [n_pages, heads, page, d], values [n_pages, heads, d, page] (e4m3 codes) and powers
+    [n_pages, heads, 2] (bytes e of 2^(e - 127)) of a pool, as views of it."""
+    import torch
+    n, h, d, p = c.n_pages, c.heads, c.d, c.page
+    half, f8 = n * h * d * p, torch.float8_e4m3fn
+    return (pool[:half].view(f8).view(n, h, p, d), pool[half:2 * half].view(f8).view(n, h, d, p),
+            pool[2 * half:2 * half + 2 * n * h].view(n, h, 2))
+
+
+def cache8_append(c, r, k, v, pages, lens, n_new, pool, stream=None):
+    """tfm_cache8_append.  k, v: device tensors whose first elements are the first rows' (rows
+    r.stride_k and r.stride_v apart); pages int32 [B, max_pages], lens, n_new int32 [B], each or
+    None; pool: device bytes, cache8_bytes(c) of them."""
+    import torch
+    i32, n, dtype = torch.int32, (r.B, r.L, c.heads), _torch_dtype(r.dtype)
+    _tensors("cache8_append", _strided_rows("cache8_append", "k", k, dtype, n, r.stride_k, c.d),
+             _strided_rows("cache8_append", "v", v, dtype, n, r.stride_v, c.d),
+             ("pages", pages, i32, (r.B, r.max_pages)), ("lens", lens, i32, (r.B,)),
+             ("n_new", n_new, i32, (r.B,)), ("pool", pool, None, None))
+    rc = lib().tfm_cache8_append(ctypes.byref(c), ctypes.byref(r), _ptr(k), _ptr(v), _ptr(pages),
+                                 _ptr(lens), _ptr(n_new), _ptr(pool), _nbytes(pool),
+                                 _stream(stream))
+    _check(rc)
+
+
+def cache8_attend_workspace_bytes(c, a):
+    return lib().tfm_cache8_attend_workspace_bytes(ctypes.byref(c), ctypes.byref(a))
+
+
+def cache8_attend(c, a, q, pages, lens, n_rows, pool, out, lse, workspace, stream=None):
+    """tfm_cache8_attend.  q, out: device tensors whose first elements are the first rows' (rows
+    a.stride_q and a.stride_out apart); pages int32 [B, max_pages] or None; lens int32 [B]; n_rows
+    int32 [B] or None; lse float32 [B, L, heads] or None; workspace: device bytes,
+    cache8_attend_workspace_bytes(c, a) of them (None for 0)."""
+    import torch
+    i32, n, dtype = torch.int32, (a.B, a.L, a.heads), _torch_dtype(a.dtype)
+    _tensors("cache8_attend", _strided_rows("cache8_attend", "q", q, dtype, n, a.stride_q, c.d),
+             _strided_rows("cache8_attend", "out", out, dtype, n, a.stride_out, c.d),
+             ("pages", pages, i32, (a.B, a.max_pages)), ("lens", lens, i32, (a.B,)),
+             ("n_rows", n_rows, i32, (a.B,)), ("pool", pool, None, None),
+             ("lse", lse, torch.float32, n), ("workspace", workspace, None, None))
+    rc = lib().tfm_cache8_attend(ctypes.byref(c), ctypes.byref(a), _ptr(q), _ptr(pages),
+                                 _ptr(lens), _ptr(n_rows), _ptr(pool), _nbytes(pool), _ptr(out),
+                                 _ptr(lse), _ptr(workspace), _nbytes(workspace), _stream(stream))
     _check(rc)
 
 

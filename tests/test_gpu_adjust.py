@@ -1,0 +1,289 @@
+"""Adjusted logits (include/tfm_vocab.h) on the GPU against the float64 oracle, at the sizes and values
+where they can go wrong; and the operators of answering from a kept context run together.
+
+Tolerances: every step rounds once, by at most U = 2^-24 of its result, and a bfloat16 output once
+more, by B = 2^-8; the oracle gives the sum of the results' magnitudes.
+"""
+
+import sys
+
+import numpy as np
+import pytest
+
+from oracle import vocab as ov
+from paper_2606_03681_amd import workloads as wl
+
+pytestmark = pytest.mark.gpu
+U, B = 2.0 ** -24, 2.0 ** -8
+
+
+def _say(*a):
+    print(*a, file=sys.stderr, flush=True)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible")
+    from paper_2606_03681_amd import tfm
+    tfm.lib()
+
+
+def _torch(dtype):
+    import torch
+    return {"f32": torch.float32, "bf16": torch.bfloat16}[dtype]
+
+
+def _dev(a, dtype=None):
+    import torch
+    if a is None:
+        return None
+    t = torch.from_numpy(np.ascontiguousarray(a)).cuda()
+    return t if dtype is None else t.to(_torch(dtype))
+
+
+def _inputs(rng, N, V, seen, nb, mask, classes, dtype):
+    s = dict(logits=wl.storage_to_f64(wl.to_storage(3 * rng.normal(size=(N, V)), dtype), dtype),
+             n_class=None, history=None, n_history=None, repetition=None, presence=None,
+             frequency=None, bias_idx=None, bias=None, allowed=None)
+    if classes:
+        s["n_class"] = rng.integers(-1, V + 2, N).astype(np.int32)
+    if seen:
+        h = np.minimum(rng.integers(-2, V + 2, (N, seen)), rng.integers(-2, V + 2, (N, seen)))
+        s["history"] = np.where(rng.random((N, seen)) < 0.3, h[:, :1], h).astype(np.int32)
+        s["n_history"] = rng.integers(-1, seen + 2, N).astype(np.int32)
+        s["repetition"] = rng.choice([1.0, 1.3, 0.7, 0.0, -2.0, np.nan], N).astype(np.float32)
+        s["presence"] = rng.normal(size=N).astype(np.float32)
+        s["frequency"] = rng.normal(size=N).astype(np.float32)
+    if nb:
+        s["bias_idx"] = rng.integers(-2, V + 2, (N if nb > 0 else 1, abs(nb))).astype(np.int32)
+        s["bias"] = rng.normal(size=s["bias_idx"].shape).astype(np.float32)
+    if mask:
+        words = rng.integers(0, 2 ** 32, (N if mask == 2 else 1, (V + 31) // 32), dtype=np.uint32)
+        s["allowed"] = words.view(np.int32)
+    return s
+
+
+def _want(s, N, V):
+    x, size = np.zeros((N, V)), np.zeros((N, V))
+    for n in range(N):
+        at = lambda k, d=None: d if s[k] is None else s[k][n if len(s[k]) > 1 else 0]  # noqa: E731
+        h = at("history", [])
+        m = at("n_history")
+        h = h if m is None else h[:max(0, int(m))]
+        x[n], size[n] = ov.adjust_row(
+            s["logits"][n], at("n_class"), h, float(at("repetition", 1.0)),
+            float(at("presence", 0.0)), float(at("frequency", 0.0)), at("bias_idx", []),
+            at("bias", []), None if s["allowed"] is None else at("allowed").view(np.uint32))
+    return x, size
+
+
+def _call(s, N, V, dtype, pad=0, in_place=False, stream=None, side=0):
+    """Through rows `pad` elements apart (and side entries, `side` apart): whole buffer, out rows."""
+    import torch
+    from paper_2606_03681_amd import tfm
+    buf = torch.full((N, V + pad), 7.5, dtype=_torch(dtype), device="cuda")
+    buf[:, :V] = _dev(s["logits"], dtype)
+    out = buf if in_place else torch.full((N, V + 2 * pad), 3.5, dtype=_torch(dtype), device="cuda")
+
+    def rows(k):
+        t = _dev(s[k])
+        if t is None:
+            return None, None
+        if t.shape[0] == 1 and N > 1:
+            return t, 0
+        wide = torch.zeros((N, t.shape[1] + side), dtype=t.dtype, device="cuda")
+        wide[:, :t.shape[1]] = t
+        return wide[:, :t.shape[1]], t.shape[1] + side
+
+    (h, lh), (bi, lb), (b, _), (al, la) = (rows(k) for k in ("history", "bias_idx", "bias", "allowed"))
+    a = tfm.make_adjust(N, V, V + pad, dtype, 0 if h is None else s["history"].shape[1],
+                        0 if b is None else s["bias"].shape[1], V + pad if in_place else V + 2 * pad,
+                        lh, lb, la)
+    tfm.adjust_logits(a, buf[:, :V], _dev(s["n_class"]), h, _dev(s["n_history"]),
+                      _dev(s["repetition"]), _dev(s["presence"]), _dev(s["frequency"]), bi, b, al,
+                      out[:, :V], stream)
+    return out
+
+
+# N, V, history, bias (negative: one row for all), mask (1: one for all), classes, pad
+ADJUST = [
+    (1, 1, 1, 1, 2, 0, 0), (1, 2, 0, 2, 0, 0, 0), (3, 10, 0, -10, 1, 1, 0), (5, 31, 40, 3, 2, 1, 0),
+    (4, 32, 5, 0, 1, 0, 1), (2, 33, 0, 0, 2, 0, 0), (70, 64, 20, 4, 2, 1, 3), (3, 100, 1000, 300, 0, 0, 5),
+    (2, 257, 100, 0, 0, 1, 0), (3, 1000, 30, 7, 2, 0, 8), (2, 2047, 64, 9, 1, 1, 1),
+    (2, 4097, 500, 50, 2, 1, 0), (1, 8200, 3000, 0, 0, 0, 0), (2, 20001, 1000, 33, 2, 0, 7),
+    (1, 70000, 200, 20, 2, 1, 0), (300, 7, 3, 2, 1, 1, 1),
+]
+
+
+@pytest.mark.parametrize("in_place", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("case", range(len(ADJUST)))
+def test_adjust(case, dtype, in_place):
+    N, V, seen, nb, mask, classes, pad = ADJUST[case]
+    rng = np.random.default_rng(case)
+    s = _inputs(rng, N, V, seen, nb, mask, classes, dtype)
+    whole = _call(s, N, V, dtype, pad, in_place, side=case % 3).double().cpu().numpy()
+    got = whole[:, :V]
+    want, size = _want(s, N, V)
+    assert np.all(whole[:, V:] == (7.5 if in_place else 3.5))
+    gone = want == -np.inf
+    assert np.array_equal(got == -np.inf, gone)
+    d = np.abs(got - np.where(gone, 0, want))[~gone]
+    bound = U * size[~gone] * 1.01
+    assert np.all(d <= bound + (B if dtype == "bf16" else 0) * (np.abs(want[~gone]) + bound))
+    same = (size == 0) & ~gone                      # classes that nothing is said about
+    assert np.array_equal(got[same], s["logits"][same])
+
+
+@pytest.mark.parametrize("V", [8, 300, 5000])
+def test_adjust_values_that_are_not_finite(V):
+    """NaN and infinities stay what they are where allowed, and are -inf where not; rows that the mask
+    empties; biases that forbid."""
+    rng = np.random.default_rng(V)
+    s = _inputs(rng, 4, V, 0, 0, 2, 0, "f32")
+    s["logits"][:, 0], s["logits"][:, 1], s["logits"][:, 2] = np.nan, np.inf, -np.inf
+    s["allowed"] = s["allowed"].copy()
+    s["allowed"][0] = 0
+    s["allowed"][1] = -1
+    s["allowed"][2, 0] = 0
+    s["history"] = np.tile(np.array([[0, 1, 2, 3]], np.int32), (4, 1))
+    s["repetition"] = np.full(4, 2.0, np.float32)
+    s["bias_idx"] = np.tile(np.array([[4, 4]], np.int32), (4, 1))
+    s["bias"] = np.tile(np.array([[-np.inf, 5.0]], np.float32), (4, 1))
+    got = _call(s, 4, V, "f32").double().cpu().numpy()
+    with np.errstate(invalid="ignore"):
+        want, _ = _want(s, 4, V)
+    assert np.array_equal(np.isnan(got), np.isnan(want))
+    assert np.array_equal(np.isinf(got), np.isinf(want)) and np.all(got[0] == -np.inf)
+    assert np.isnan(got[1, 0]) and got[1, 1] == np.inf and np.all(got[:, 4] == -np.inf)
+    fine = np.isfinite(want)
+    assert np.allclose(got[fine], want[fine], rtol=4 * U, atol=0)
+
+
+def test_adjust_side_arrays_one_by_one():
+    """Each of the arrays left out, and rows of history shared by all rows."""
+    rng = np.random.default_rng(5)
+    full = _inputs(rng, 6, 500, 30, 5, 2, 1, "f32")
+    for gone in ("n_class", "n_history", "repetition", "presence", "frequency", "allowed", "shared"):
+        s = dict(full)
+        if gone == "shared":
+            s["history"] = full["history"][:1]
+        else:
+            s[gone] = None
+        got = _call(s, 6, 500, "f32").double().cpu().numpy()
+        want, size = _want(s, 6, 500)
+        ok = want > -np.inf
+        assert np.array_equal(got > -np.inf, ok)
+        assert np.all(np.abs(got - np.where(ok, want, 0))[ok] <= 1.01 * U * size[ok]), gone
+
+
+def test_adjust_past_32_bit_offsets():
+    import torch
+    from paper_2606_03681_amd import tfm
+    N, V, ld = 3, 1000, 1 << 31
+    buf = torch.empty((N - 1) * ld + V, dtype=torch.bfloat16, device="cuda")
+    rows = buf.as_strided((N, V), (ld, 1))
+    z = torch.randn((N, V), device="cuda").bfloat16()
+    rows.copy_(z)
+    bias_idx = torch.arange(N, dtype=torch.int32, device="cuda")[:, None].contiguous()
+    a = tfm.make_adjust(N, V, ld, "bf16", n_bias=1)
+    tfm.adjust_logits(a, rows, None, None, None, None, None, None, bias_idx,
+                      torch.full((N, 1), -float("inf"), device="cuda"), None, rows)
+    z[torch.arange(N), torch.arange(N)] = -float("inf")
+    assert torch.equal(rows, z)
+
+
+def test_adjust_on_a_side_stream_and_replayed_from_a_graph():
+    import torch
+    from paper_2606_03681_amd import tfm
+    rng = np.random.default_rng(9)
+    N, V = 5, 3001
+    s = _inputs(rng, N, V, 60, 4, 2, 1, "bf16")
+    want = _call(s, N, V, "bf16")
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(st):
+        assert torch.equal(_call(s, N, V, "bf16"), want)
+    d = {k: _dev(v) for k, v in s.items()}
+    d["logits"] = _dev(s["logits"], "bf16")
+    out = torch.empty_like(d["logits"])
+    a = tfm.make_adjust(N, V, V, "bf16", 60, 4)
+
+    def call():
+        tfm.adjust_logits(a, d["logits"], d["n_class"], d["history"], d["n_history"],
+                          d["repetition"], d["presence"], d["frequency"], d["bias_idx"], d["bias"],
+                          d["allowed"], out)
+
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for i in range(4):
+        d["logits"].copy_(torch.randn_like(d["logits"]))
+        d["history"].random_(0, V)
+        g.replay()
+        replayed = out.clone()
+        call()
+        torch.cuda.synchronize()
+        assert torch.equal(replayed, out)
+
+
+def test_a_serving_loop_of_all_of_them():
+    """append -> attend -> logits -> adjust -> sample, each step's token in the next one's history,
+    against the oracles step by step: pools and tokens are equal, logits within the bounds' order."""
+    import torch
+    from oracle import cache as oc
+    from paper_2606_03681_amd import tfm
+    rng = np.random.default_rng(12)
+    Bn, H, kv, d, page, mp, V, steps = 3, 4, 2, 32, 16, 3, 40, 36
+    c = tfm.make_cache8(kv, d, page, Bn * mp)
+    pool = torch.zeros(tfm.cache8_bytes(c), dtype=torch.uint8, device="cuda")
+    host = tuple(np.zeros(sh, np.uint8) for sh in ((Bn * mp, kv, page, d), (Bn * mp, kv, d, page),
+                                                   (Bn * mp, kv, 2)))
+    pages = rng.permutation(Bn * mp).reshape(Bn, mp).astype(np.int32)
+    W = _dev(rng.normal(size=(H * d, V)) / np.sqrt(H * d), "f32")
+    lens = torch.zeros(Bn, dtype=torch.int32, device="cuda")
+    history = torch.full((Bn, steps), -1, dtype=torch.int32, device="cuda")
+    said = torch.zeros(Bn, dtype=torch.int32, device="cuda")
+    rep, pres = torch.full((Bn,), 1.5, device="cuda"), torch.full((Bn,), 0.3, device="cuda")
+    bias_idx, bias = _dev(np.array([[3, 5]], np.int32)), _dev(np.array([[1.0, -np.inf]], np.float32))
+    words = rng.integers(0, 2 ** 32, (Bn, 2), dtype=np.uint32) | 8
+    allowed = _dev(words.view(np.int32))
+    out = torch.empty((Bn, 1, H, d), dtype=torch.bfloat16, device="cuda")
+    token = torch.empty(Bn, dtype=torch.int32, device="cuda")
+    r = tfm.make_cache8_rows(Bn, 1, mp, "bf16", (kv * d, kv * d, d), (kv * d, kv * d, d))
+    a = tfm.make_cache8_query(Bn, 1, H, mp, "bf16", out.stride()[:3], out.stride()[:3], 0.4, True)
+    ws = torch.empty(tfm.cache8_attend_workspace_bytes(c, a), dtype=torch.uint8, device="cuda")
+    adj = tfm.make_adjust(Bn, V, V, "f32", steps, 2, ld_bias=0)
+    smp = tfm.make_sampling(Bn, V, V, "f32")
+    for i in range(steps):
+        k, v, q = (_dev(rng.normal(size=(Bn, 1, n, d)), "bf16") for n in (kv, kv, H))
+        u = _dev(rng.random(Bn).astype(np.float32))
+        tfm.cache8_append(c, r, k, v, _dev(pages), lens, None, pool)
+        lens.add_(1)
+        tfm.cache8_attend(c, a, q, _dev(pages), lens, None, pool, out, None, ws)
+        logits = (out.view(Bn, H * d).float() @ W) * 3
+        raw = logits.clone()
+        tfm.adjust_logits(adj, logits, None, history, said, rep, pres, None, bias_idx, bias, allowed,
+                          logits)
+        tfm.sample(smp, logits, None, None, None, None, None, u, token)
+        # the oracles
+        host = oc.append(*host, k.double().cpu().numpy(), v.double().cpu().numpy(), mp, pages,
+                         [i] * Bn)
+        want = oc.attend(q.double().cpu().numpy(), *host, mp, pages, [i + 1] * Bn, None,
+                         float(np.float32(0.4)), True)[0]
+        assert np.allclose(out.double().cpu().numpy(), want, rtol=2 * B, atol=4 * 2.0 ** -12)
+        for b in range(Bn):
+            x, _ = ov.adjust_row(raw[b].double().cpu().numpy(), None, history[b, :i].tolist(), 1.5,
+                                 float(np.float32(0.3)), 0.0, [3, 5], [1.0, -np.inf], words[b])
+            got = logits[b].double().cpu().numpy()
+            assert np.array_equal(got == -np.inf, x == -np.inf)
+            assert np.allclose(got[x > -np.inf], x[x > -np.inf], rtol=8 * U, atol=8 * U * 10)
+            assert ov.sample_row(got, u=float(u[b]))[0] == int(token[b])
+        history[:, i] = token
+        said.add_(1)
+    from paper_2606_03681_amd.tfm import cache8_views
+    for x, y in zip(cache8_views(c, pool), host):
+        assert np.array_equal(x.view(torch.uint8).cpu().numpy(), y)
