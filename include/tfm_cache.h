@@ -55,7 +55,7 @@ size_t tfm_cache8_bytes(const tfm_cache8* c);
  * lens[b]) its power does not fall; where it grows, the codes of these rows are rounded again to the
  * new power.  NaN, infinities and values above 448 2^48 do not count for the power and become NaN
  * codes.  Everything else of the pool is left as it was.
- * Limits: B, L, max_pages >= 0, B max_pages <= 2^31 - 1, max_pages page <= 2^31 - 1; strides in
+ * Limits: B, L, max_pages >= 0, B max_pages <= 2^31 - 1, max_pages page <= 2^30; strides in
  * [0, 2^40], the last row at most 2^48 elements from the first.  k, v and the pool must not share
  * memory. */
 typedef struct {
@@ -88,7 +88,8 @@ int tfm_cache8_append(const tfm_cache8* c, const tfm_cache8_rows* r, const void*
  * Rows of q and out (dtype both) lie by their strides as above; out's rows must not overlap.  out may
  * be q itself (with equal strides: in place); it shares no element with q otherwise, and none with
  * the pool, lse and the workspace.  A query row that is not finite has undefined outputs, others not.
- * Limits: B, L >= 0, heads a multiple of the cache's with at most 2^16 of them, B L heads <= 2^31 - 1;
+ * Limits: B, L >= 0, heads a multiple of the cache's with at most 2^16 of them, L heads <= 2^26,
+ * B L heads <= 2^31 - 1;
  * max_pages, strides as above; scale finite. */
 typedef struct {
   int32_t B, L, max_pages, max_len;

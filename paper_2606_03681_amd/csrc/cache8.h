@@ -43,7 +43,7 @@ struct Cache8Attend {
   float* lse;                // nullable
   void* ws;
 };
-size_t cache8_attend_bytes(const Cache8Attend& a);
+size_t cache8_attend_bytes(const Cache8Attend& a, bool f32);
 template <class T>
 hipError_t launch_cache8_attend(const Cache8Attend& a, const T* q, T* out, hipStream_t s);
 

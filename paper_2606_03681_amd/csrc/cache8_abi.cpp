@@ -66,8 +66,8 @@ int pool_check(const tfm_cache8* c) {
 
 int batch_check(const tfm_cache8* c, int32_t B, int32_t L, int32_t max_pages, int32_t dtype) {
   if (B < 0 || L < 0) return fail(TFM_ERR_DIMS, "B=%d or L=%d is negative", B, L);
-  if (max_pages < 0 || (int64_t)max_pages * c->page > kMax31)
-    return fail(TFM_ERR_DIMS, "max_pages=%d of %d rows outside [0, 2^31 - 1]", max_pages, c->page);
+  if (max_pages < 0 || (int64_t)max_pages * c->page > (1 << 30))
+    return fail(TFM_ERR_DIMS, "max_pages=%d of %d rows outside [0, 2^30]", max_pages, c->page);
   if ((int64_t)B * max_pages > kMax31)
     return fail(TFM_ERR_DIMS, "%d x %d page indices are more than 2^31 - 1", B, max_pages);
   if (dtype != TFM_F32 && dtype != TFM_BF16)
@@ -150,6 +150,8 @@ int query_check(const tfm_cache8* c, const tfm_cache8_query* a, tfm::Cache8Atten
                 c->heads);
   if ((double)a->B * a->L * a->heads > (double)kMax31)
     return fail(TFM_ERR_DIMS, "%d x %d x %d query rows are more than 2^31 - 1", a->B, a->L, a->heads);
+  if ((int64_t)a->L * a->heads > (1 << 26))
+    return fail(TFM_ERR_DIMS, "%d rows of %d heads are more than 2^26", a->L, a->heads);
   if (a->max_len < 0) return fail(TFM_ERR_DIMS, "max_len=%d is negative", a->max_len);
   if (!std::isfinite(a->scale)) return fail(TFM_ERR_DIMS, "scale is not finite");
   const int32_t n[3] = {a->B, a->L, a->heads};
@@ -205,7 +207,7 @@ int tfm_cache8_append(const tfm_cache8* c, const tfm_cache8_rows* r, const void*
 size_t tfm_cache8_attend_workspace_bytes(const tfm_cache8* c, const tfm_cache8_query* a) {
   tfm::Cache8Attend t;
   if (query_check(c, a, t)) return 0;
-  return tfm::cache8_attend_bytes(t);
+  return tfm::cache8_attend_bytes(t, a->dtype == TFM_F32);
 }
 
 int tfm_cache8_attend(const tfm_cache8* c, const tfm_cache8_query* a, const void* q,
@@ -229,7 +231,7 @@ int tfm_cache8_attend(const tfm_cache8* c, const tfm_cache8_query* a, const void
   if (overlap(out, span, pool, (double)pool_size(c)) ||
       overlap(out, span, lse, 4.0 * a->B * a->L * a->heads))
     return fail(TFM_ERR_POINTER, "out overlaps the pool or lse");
-  const size_t need = tfm::cache8_attend_bytes(t);
+  const size_t need = tfm::cache8_attend_bytes(t, a->dtype == TFM_F32);
   if (need && !aligned(workspace, 16))
     return fail(TFM_ERR_POINTER, "workspace null or not 16-byte aligned");
   if (workspace_bytes < need)

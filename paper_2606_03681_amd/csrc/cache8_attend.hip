@@ -1,92 +1,641 @@
 // Attention of query rows over a pool of e4m3 codes (declarations in cache8.h).
 //
-// One wave per (sequence, row, head): a lane has a key of each 64, then a few channels of the sum.
+// The query rows of all heads that share a key/value head of a sequence are the columns of one
+// problem, row i and head j of G at column i G + j: one row of a group of heads and many rows of one
+// head are the same work.  A wave takes 16 QB columns and tiles of 64 rows of the cache (keys, below):
+//
+//   S^T = K Q^T     v_mfma_f32_16x16x32_bf16: codes are exact as bfloat16, the block's power goes into
+//                   the scores' factor
+//   p = 2^(S c - ref), online, ref a running reference of the exponent per column
+//   O^T += V^T P^T  v_mfma_f32_16x16x32_f16: codes are exact as half; the block's power goes into p as
+//                   2^(power - unit), unit the largest power that the column has seen so far
+//
+// Row m of the t-th of the tile's four 16-row products is key 16 (m / 4) + 4 t + m % 4, so that a lane's
+// 16 scores are those of 16 keys in a row: one block's, since pages are multiples of 16, and in the
+// order in which the lane reads 16 bytes of V^T.  Nothing moves between lanes, and codes go from memory
+// to registers without LDS.
+//
+// p is held as half with 2^14 in front, at most 2^15 with the reference at most 2 below the largest:
+// 2^-12 of each weight, and 2^-39 of the largest where half has no more bits.  bfloat16 would have
+// doubled the output's own rounding error.  Float32 queries are three bfloat16 parts (24 bits) and
+// their weights two halves.
+//
+// Few columns (SPLIT): the four waves of a workgroup share the columns and take turns over the tiles;
+// many: each wave has columns of its own.  Where the workgroups are too few the keys are split over
+// more of them, and a second launch joins their sums.
+#include <float.h>
+
 #include "cache8.h"
 #include "mfma.h"
-#include "wave.h"
 
 namespace tfm {
 namespace {
 
-constexpr int kMaxBlocks = 1 << 20;
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-template <class T>
-__global__ __launch_bounds__(64) void k_cache8_attend(Cache8Attend a, const T* __restrict__ q,
-                                                      T* __restrict__ out, int64_t items) {
-  __shared__ float qs[128], ps[64];
-  __shared__ int64_t blocks[64];
-  __shared__ float vs[64];
-  const Cache8Geo& g = a.g;
-  const int d = g.d, lane = threadIdx.x;
-  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
-    const int h = (int)(it % a.heads), kh = h / (a.heads / g.heads);
-    const int64_t bi = it / a.heads, b = bi / a.L;
-    const int i = (int)(bi % a.L);
-    const int rows = a.n_rows ? min(max(a.n_rows[b], 0), a.L) : a.L;
-    if (i >= rows) continue;
-    const int len = min(max(a.lens[b], 0), a.max_rows);
-    const int64_t upto64 = a.causal ? (int64_t)len - rows + i + 1 : len;
-    const int upto = (int)max((int64_t)0, min(upto64, (int64_t)len));
-    const T* qr = q + b * a.sq[0] + i * a.sq[1] + h * a.sq[2];
-    __syncthreads();
-    for (int c = lane; c < d; c += 64) qs[c] = ld(qr + c) ;
-    __syncthreads();
-    float m = -3e38f, l = 0.f, o0 = 0.f, o1 = 0.f;
-    for (int j0 = 0; j0 < upto; j0 += 64) {
-      const int j = j0 + lane;
-      float s = -INFINITY;
-      int pid = -1;
-      if (j < upto) pid = cache8_page(g, b, j >> g.shift);
-      if (pid >= 0) {
-        const int64_t block = (int64_t)pid * g.heads + kh;
-        const uint8_t* kr = g.keys + (block * g.page + (j & (g.page - 1))) * d;
-        s = 0.f;
-        for (int c = 0; c < d; ++c) s += qs[c] * __builtin_amdgcn_cvt_f32_fp8(kr[c], 0);
-        const int ek = min(max((int)g.powers[2 * block], CACHE8_E_MIN), CACHE8_E_MAX);
-        const int ev = min(max((int)g.powers[2 * block + 1], CACHE8_E_MIN), CACHE8_E_MAX);
-        s *= __uint_as_float((uint32_t)ek << 23) * a.scale_log2;
-        vs[lane] = __uint_as_float((uint32_t)ev << 23);
-        blocks[lane] = block * g.page * d + (j & (g.page - 1));
-      } else {
-        blocks[lane] = -1;
-      }
-      const float top = fmaxf(m, wave_max(s));
-      const float p = pid >= 0 ? exp2f(s - top) : 0.f, keep = exp2f(m - top);
-      m = top;
-      l = l * keep + wave_sum(p);
-      o0 *= keep;
-      o1 *= keep;
-      __syncthreads();
-      ps[lane] = p;
-      __syncthreads();
-      for (int t = 0; t < 64; ++t) {
-        if (blocks[t] < 0) continue;
-        const uint8_t* vr = g.values + blocks[t];
-        const float w = ps[t] * vs[t];
-        if (lane < d) o0 += w * __builtin_amdgcn_cvt_f32_fp8(vr[lane * g.page], 0);
-        if (lane + 64 < d) o1 += w * __builtin_amdgcn_cvt_f32_fp8(vr[(lane + 64) * g.page], 0);
-      }
-      __syncthreads();
-    }
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    T* orow = out + b * a.so[0] + i * a.so[1] + h * a.so[2];
-    if (lane < d) st(orow + lane, l == 0.f ? 0.f : o0 * inv);
-    if (lane + 64 < d) st(orow + lane + 64, l == 0.f ? 0.f : o1 * inv);
-    if (a.lse && lane == 0)
-      a.lse[bi * a.heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+constexpr int KT = 64;              // keys per tile
+constexpr float SLACK = 1.0f;       // ref may lag by this much
+constexpr int P_BIAS = 14;          // weights are held times 2^P_BIAS
+
+__device__ __forceinline__ float exp2i(int e) {  // 2^e, e in [-126, 127]
+  return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+__device__ __forceinline__ int power_byte(uint32_t e) {
+  return min(max((int)e, CACHE8_E_MIN), CACHE8_E_MAX);
+}
+
+// 8 codes (two dwords) as bfloat16 and as half.
+__device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+  bf16x8 r = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  return r;
+}
+__device__ __forceinline__ f16x8 codes_f16(uint32_t lo, uint32_t hi) {
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false);
+  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
+  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false);
+  const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+  f16x8 r = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+  return r;
+}
+// Bytes of w that are NaN codes, as 0x80.
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) {
+  return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
+}
+
+// A float as three bfloat16 whose sum it is.
+__device__ __forceinline__ void three_parts(float x, uint16_t* p) {
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    p[i] = f2bf(x);
+    x -= bf2f(p[i]);
   }
+}
+
+// Operand of S^T: CH products over 32 channels (one over 16 at D = 16).
+template <int D>
+struct KQ {
+  static constexpr int CH = D / 32;
+  typedef bf16x8 frag;
+  static __device__ __forceinline__ f32x4 mma(const frag& k, const frag& q, const f32x4& s) {
+    return mfma16(k, q, s);
+  }
+};
+template <>
+struct KQ<16> {
+  static constexpr int CH = 1;
+  typedef s16x4 frag;
+  static __device__ __forceinline__ f32x4 mma(const frag& k, const frag& q, const f32x4& s) {
+    return __builtin_amdgcn_mfma_f32_16x16x16bf16_1k(k, q, s, 0, 0, 0);
+  }
+};
+
+// What a lane reads of a tile: keys' codes, values' codes, the bytes of both powers of its 16 keys'
+// block, and whether there is one.
+template <int D>
+struct Codes {
+  uint32_t k[4][D / 16];
+  uint4 v[D / 16];
+  uint32_t power;
+  bool here;
+};
+
+template <int D, class T, int QB, bool SPLIT, bool UNI>
+__global__ __launch_bounds__(256) void k_cache8_attend(Cache8Attend a, const T* __restrict__ q,
+                                                       T* __restrict__ out, float* __restrict__ part,
+                                                       float* __restrict__ part_ml, int64_t prob0,
+                                                       int coltiles, int splits, int chunk,
+                                                       int wide) {
+  constexpr int DB = D / 16, CH = KQ<D>::CH, KW = D / 16;  // KW: dwords of a key per lane
+  constexpr bool F32 = sizeof(T) == 4;
+  constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 2 : 1;
+  typedef typename KQ<D>::frag QF;
+  const Cache8Geo& g = a.g;
+  const int lane = threadIdx.x & 63, wave = wave_id(), c = lane & 15, lg = lane >> 4;
+  const int ct = blockIdx.x % coltiles;
+  const int64_t rest = blockIdx.x / coltiles;
+  const int sp = (int)(rest % splits);
+  const int64_t prob = prob0 + rest / splits;
+  const int64_t b = prob / g.heads;
+  const int kh = (int)(prob - b * g.heads), G = a.heads / g.heads;
+  const int rows = a.n_rows ? min(max(a.n_rows[b], 0), a.L) : a.L;
+  const int len = min(max(a.lens[b], 0), a.max_rows);
+  const int ncols = rows * G;
+  const int col0 = (SPLIT ? ct : ct * 4 + wave) * 16 * QB;
+  if (col0 >= ncols && (!SPLIT || ct * 16 * QB >= ncols)) return;
+  const int k0 = sp * chunk;
+  if (splits > 1 && k0 >= len) return;
+
+  // the columns' rows, and the keys that each sees
+  int64_t qrow[QB];
+  int upto[QB], lo = 0x7fffffff, hi = 0;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const int col = min(col0 + qb * 16 + c, ncols - 1), i = col / G;
+    qrow[qb] = ((int64_t)i << 32) | (kh * G + col - i * G);
+    upto[qb] = a.causal ? min(max(len - rows + i + 1, 0), len) : len;
+    lo = min(lo, upto[qb]);
+    hi = max(hi, upto[qb]);
+  }
+#pragma unroll
+  for (int o = 1; o < 16; o <<= 1) {
+    lo = min(lo, __shfl_xor(lo, o, 64));
+    hi = max(hi, __shfl_xor(hi, o, 64));
+  }
+  lo = __builtin_amdgcn_readfirstlane(lo);
+  hi = __builtin_amdgcn_readfirstlane(hi);
+
+  QF qf[NQ][QB][CH];
+  const bool neg = a.scale_log2 < 0;
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const T* p = q + b * a.sq[0] + (qrow[qb] >> 32) * a.sq[1] + (int)qrow[qb] * a.sq[2] + lg * (D / 4);
+    uint16_t e[NQ][D / 4];
+    if (wide) {
+      constexpr int V = D / 4 * sizeof(T) / 8;  // 8-byte pieces
+      uint2 u[V];
+#pragma unroll
+      for (int j = 0; j < V; ++j) u[j] = reinterpret_cast<const uint2*>(p)[j];
+      const T* x = reinterpret_cast<const T*>(u);
+#pragma unroll
+      for (int j = 0; j < D / 4; ++j) {
+        if constexpr (F32) {
+          uint16_t t[3];
+          three_parts(x[j], t);
+#pragma unroll
+          for (int n = 0; n < 3; ++n) e[n][j] = t[n];
+        } else {
+          e[0][j] = x[j];
+        }
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < D / 4; ++j) {
+        if constexpr (F32) {
+          uint16_t t[3];
+          three_parts(p[j], t);
+#pragma unroll
+          for (int n = 0; n < 3; ++n) e[n][j] = t[n];
+        } else {
+          e[0][j] = p[j];
+        }
+      }
+    }
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+#pragma unroll
+      for (int ch = 0; ch < CH; ++ch) {
+        uint16_t f[sizeof(QF) / 2];
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(QF) / 2; ++j)
+          f[j] = (uint16_t)(e[n][ch * 8 + j] ^ (neg ? 0x8000u : 0u));
+        __builtin_memcpy(&qf[n][qb][ch], f, sizeof(QF));
+      }
+  }
+  const float scale = fabsf(a.scale_log2);
+
+  const int kend = min(splits > 1 ? k0 + chunk : len, hi);
+  constexpr int STEP = SPLIT ? 4 * KT : KT;
+  const int page = g.page, shift = g.shift;
+  const int64_t hd = (int64_t)g.heads * page * D;  // bytes of a page
+  // of the keys 16 (c / 4) .. and 16 lg .. of the tile
+  auto pid_of = [&](int t0, int grp) {
+    const int e = min((t0 + 16 * grp) >> shift, g.max_pages - 1);
+    return cache8_page(g, b, e);
+  };
+  auto load = [&](Codes<D>& x, int t0, int pk, int pv) {
+    // UNI: one page, and pk == pv is the same in every lane
+    const int ck = c >> 2;
+    const uint8_t *kb, *vb, *pb;
+    x.here = pv >= 0;
+    pk = max(pk, 0);
+    pv = max(pv, 0);
+    if constexpr (UNI) {
+      const int slot = t0 & (page - 1);
+      kb = g.keys + pk * hd + ((int64_t)kh * page + slot) * D + (16 * ck + (c & 3)) * D + lg * (D / 4);
+      vb = g.values + pk * hd + (int64_t)kh * page * D + slot + c * page + 16 * lg;
+    } else {
+      const int sk = (t0 + 16 * ck) & (page - 1), sv = (t0 + 16 * lg) & (page - 1);
+      kb = g.keys + pk * hd + ((int64_t)kh * page + sk + (c & 3)) * D + lg * (D / 4);
+      vb = g.values + pv * hd + (int64_t)kh * page * D + sv + c * page;
+    }
+    pb = g.powers + ((int64_t)pv * g.heads + kh) * 2;
+    x.power = *reinterpret_cast<const uint16_t*>(pb);
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+      if constexpr (D == 16) {
+        x.k[t][0] = *reinterpret_cast<const uint32_t*>(kb + 4 * t * D);
+      } else if constexpr (D == 32) {
+        const uint2 u = *reinterpret_cast<const uint2*>(kb + 4 * t * D);
+        x.k[t][0] = u.x; x.k[t][1] = u.y;
+      } else {
+#pragma unroll
+        for (int w = 0; w < KW; w += 4) {
+          const uint4 u = *reinterpret_cast<const uint4*>(kb + 4 * t * D + 4 * w);
+          x.k[t][w] = u.x; x.k[t][w + 1] = u.y; x.k[t][w + 2] = u.z; x.k[t][w + 3] = u.w;
+        }
+      }
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+      x.v[db] = *reinterpret_cast<const uint4*>(vb + (int64_t)db * 16 * page);
+  };
+
+  float ref[QB], lsum[QB];
+  int unit[QB];
+  f32x4 oacc[DB][QB];
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    unit[qb] = CACHE8_E_MIN;
+    ref[qb] = -FLT_MAX;
+    lsum[qb] = 0.f;
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[db][qb] = zero4();
+  }
+
+  auto compute = [&](Codes<D>& x, int t0) {
+    f32x4 s[4][QB];
+#pragma unroll
+    for (int t = 0; t < 4; ++t) {
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) s[t][qb] = zero4();
+#pragma unroll
+      for (int ch = 0; ch < CH; ++ch) {
+        QF kf;
+        if constexpr (D == 16) {
+          const bf16x8 w = codes_bf16(x.k[t][0], 0);
+          __builtin_memcpy(&kf, &w, 8);
+        } else {
+          kf = codes_bf16(x.k[t][2 * ch], x.k[t][2 * ch + 1]);
+        }
+#pragma unroll
+        for (int n = NQ - 1; n >= 0; --n)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) s[t][qb] = KQ<D>::mma(kf, qf[n][qb][ch], s[t][qb]);
+      }
+    }
+    const int ek = power_byte(x.power & 0xff), ev = power_byte(x.power >> 8);
+    const float cs = fmaxf(scale * exp2i(ek - 127), 0x1p-126f);
+    const bool partial = t0 + KT > lo || __any(!x.here);
+    // the largest power of values that a column has seen; a larger one than before rescales its sums
+    // (a block that the column does not see must not: its power may be anything)
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      int top = ev;
+      if (partial) top = x.here && t0 + 16 * lg < upto[qb] ? ev : 0;
+      if constexpr (!UNI) {
+        top = max(top, __shfl_xor(top, 16, 64));
+        top = max(top, __shfl_xor(top, 32, 64));
+      } else if (partial) {
+        top = __shfl(top, c, 64);
+      }
+      if (__any(top > unit[qb])) {
+        const int now = max(top, unit[qb]);
+        const float f = exp2i(unit[qb] - now);
+#pragma unroll
+        for (int db = 0; db < DB; ++db) oacc[db][qb] *= f;
+        unit[qb] = now;
+      }
+    }
+    uint32_t nans = 0;
+    if (partial) {
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = t0 + 16 * lg + 4 * t + i;
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+            if (key >= upto[qb] || !x.here) s[t][qb][i] = -INFINITY;
+        }
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        nans |= nan_bytes(x.v[db].x) | nan_bytes(x.v[db].y) | nan_bytes(x.v[db].z) | nan_bytes(x.v[db].w);
+    }
+    f16x8 pf[NP][QB][2];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      float mx = fmaxf(fmaxf(s[0][qb][0], s[0][qb][1]), fmaxf(s[0][qb][2], s[0][qb][3]));
+#pragma unroll
+      for (int t = 1; t < 4; ++t)
+        mx = fmaxf(mx, fmaxf(fmaxf(s[t][qb][0], s[t][qb][1]), fmaxf(s[t][qb][2], s[t][qb][3])));
+      mx *= cs;
+      if (__any(mx > ref[qb] + SLACK)) {
+        const float now = fmaxf(ref[qb], rows4_max(mx)), corr = exp2_hw(ref[qb] - now);
+        ref[qb] = now;
+        lsum[qb] *= corr;
+#pragma unroll
+        for (int db = 0; db < DB; ++db) oacc[db][qb] *= corr;
+      }
+      const int rel = ev - unit[qb] + P_BIAS;
+      const float off = (float)rel - ref[qb];
+      float sum = 0.f;
+#pragma unroll
+      for (int kc = 0; kc < 2; ++kc) {
+        float p[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          p[j] = exp2_hw(fmaf(s[2 * kc + j / 4][qb][j % 4], cs, off));
+          sum += p[j];
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const _Float16 h = (_Float16)p[j];
+          pf[0][qb][kc][j] = h;
+          if constexpr (NP == 2) pf[1][qb][kc][j] = (_Float16)(p[j] - (float)h);
+        }
+      }
+      lsum[qb] = fmaf(sum, exp2i(-rel), lsum[qb]);
+    }
+    if (partial && __any(nans != 0)) {
+      // NaN codes (or what lies behind the last key): out of the products, whose weight for them
+      // may be 0, and NaN in the sums of the columns that see them
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        uint32_t* w = reinterpret_cast<uint32_t*>(&x.v[db]);
+        f32x4 cnt[QB];
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) cnt[qb] = zero4();
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc) {
+          f16x8 is;
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const uint32_t m = nan_bytes(w[2 * kc + j / 4]) >> (8 * (j % 4) + 7) & 1;
+            is[j] = (_Float16)(float)m;
+          }
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) {
+            f16x8 sees;
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              sees[j] = (_Float16)(x.here && t0 + 16 * lg + 8 * kc + j < upto[qb] ? 1.f : 0.f);
+            cnt[qb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(is, sees, cnt[qb], 0, 0, 0);
+          }
+        }
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (cnt[qb][i] > 0.f) oacc[db][qb][i] = __builtin_nanf("");
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const uint32_t m = nan_bytes(w[j]);
+          w[j] &= ~(m | (m - (m >> 7)));  // 0x80 to 0xff
+        }
+      }
+    }
+#pragma unroll
+    for (int db = 0; db < DB; ++db)
+#pragma unroll
+      for (int kc = 0; kc < 2; ++kc) {
+        const f16x8 vf = kc ? codes_f16(x.v[db].z, x.v[db].w) : codes_f16(x.v[db].x, x.v[db].y);
+#pragma unroll
+        for (int n = NP - 1; n >= 0; --n)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+            oacc[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n][qb][kc], oacc[db][qb], 0, 0, 0);
+      }
+  };
+
+  // tiles t0, t0 + STEP, ...: the next tile's codes are on their way while one is computed, and the
+  // page of the one after it
+  int t0 = k0 + (SPLIT ? wave * KT : 0);
+  if (t0 < kend) {
+    Codes<D> x, y;
+    const int gk = UNI ? 0 : c >> 2, gv = UNI ? 0 : lg;
+    int pk = pid_of(t0, gk), pv = UNI ? pk : pid_of(t0, gv);
+    load(x, t0, pk, pv);
+    if (t0 + STEP < kend) {
+      pk = pid_of(t0 + STEP, gk);
+      pv = UNI ? pk : pid_of(t0 + STEP, gv);
+    }
+    for (;;) {
+      if (t0 + STEP < kend) {
+        load(y, t0 + STEP, pk, pv);
+        if (t0 + 2 * STEP < kend) {
+          pk = pid_of(t0 + 2 * STEP, gk);
+          pv = UNI ? pk : pid_of(t0 + 2 * STEP, gv);
+        }
+      }
+      compute(x, t0);
+      t0 += STEP;
+      if (t0 >= kend) break;
+      if (t0 + STEP < kend) {
+        load(x, t0 + STEP, pk, pv);
+        if (t0 + 2 * STEP < kend) {
+          pk = pid_of(t0 + 2 * STEP, gk);
+          pv = UNI ? pk : pid_of(t0 + 2 * STEP, gv);
+        }
+      }
+      compute(y, t0);
+      t0 += STEP;
+      if (t0 >= kend) break;
+    }
+  }
+
+  // the sums in units of 1, over all lanes of a column
+#pragma unroll
+  for (int qb = 0; qb < QB; ++qb) {
+    const float one = exp2i(unit[qb] - 127 - P_BIAS);
+    lsum[qb] = rows4_sum(lsum[qb]);
+#pragma unroll
+    for (int db = 0; db < DB; ++db) oacc[db][qb] *= one;
+  }
+  if constexpr (SPLIT) {
+    // the four waves' sums, in LDS: wave w's of column k
+    __shared__ float ml[4][16 * QB][2];
+    __shared__ __attribute__((aligned(16))) float ow[4][16 * QB][D + 4];
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int k = qb * 16 + c;
+      if (lg == 0) ml[wave][k][0] = ref[qb], ml[wave][k][1] = lsum[qb];
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+        *reinterpret_cast<f32x4*>(&ow[wave][k][db * 16 + lg * 4]) = oacc[db][qb];
+    }
+    __syncthreads();
+    // 4 channels of a column per thread
+    for (int it = threadIdx.x; it < 16 * QB * (D / 4); it += 256) {
+      const int k = it / (D / 4), d0 = it % (D / 4) * 4, col = col0 + k;
+      if (col >= ncols) continue;
+      const float m = fmaxf(fmaxf(ml[0][k][0], ml[1][k][0]), fmaxf(ml[2][k][0], ml[3][k][0]));
+      float l = 0.f;
+      f32x4 o = zero4();
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const float f = exp2_hw(ml[w][k][0] - m);
+        l = fmaf(ml[w][k][1], f, l);
+        o += *reinterpret_cast<const f32x4*>(&ow[w][k][d0]) * f;
+      }
+      const int i = col / G, h = kh * G + col - i * G;
+      if (splits > 1) {
+        const int64_t at = (prob * a.L * G + col) * splits + sp;
+        *reinterpret_cast<f32x4*>(part + at * D + d0) = o;
+        if (d0 == 0) part_ml[at * 2] = m, part_ml[at * 2 + 1] = l;
+      } else {
+        T* p = out + b * a.so[0] + i * a.so[1] + h * a.so[2] + d0;
+        const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) st(p + j, l == 0.f ? 0.f : o[j] * inv);
+        if (a.lse && d0 == 0)
+          a.lse[(b * a.L + i) * a.heads + h] =
+              l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int qb = 0; qb < QB; ++qb) {
+      const int col = col0 + qb * 16 + c;
+      if (col >= ncols) continue;
+      const int i = (int)(qrow[qb] >> 32), h = (int)qrow[qb];
+      const float l = lsum[qb];
+      if (splits > 1) {
+        const int64_t at = (prob * a.L * G + col) * splits + sp;
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+          *reinterpret_cast<f32x4*>(part + at * D + db * 16 + lg * 4) = oacc[db][qb];
+        if (lg == 0) part_ml[at * 2] = ref[qb], part_ml[at * 2 + 1] = l;
+        continue;
+      }
+      T* p = out + b * a.so[0] + i * a.so[1] + h * a.so[2] + lg * 4;
+      const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) {
+        float y[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) y[j] = l == 0.f ? 0.f : oacc[db][qb][j] * inv;
+        if (wide) {
+          if constexpr (F32)
+            *reinterpret_cast<float4*>(p + db * 16) = make_float4(y[0], y[1], y[2], y[3]);
+          else
+            *reinterpret_cast<uint2*>(p + db * 16) = make_uint2(pack2(y[0], y[1]), pack2(y[2], y[3]));
+        } else {
+#pragma unroll
+          for (int j = 0; j < 4; ++j) st(p + db * 16 + j, y[j]);
+        }
+      }
+      if (a.lse && lg == 0)
+        a.lse[(b * a.L + i) * a.heads + h] =
+            l == 0.f ? -INFINITY : (ref[qb] + log2f(l)) * 0.69314718055994531f;
+    }
+  }
+}
+
+// The sums of the splits of each column, in their order: D / 4 lanes per column.
+template <int D, class T>
+__global__ __launch_bounds__(256) void k_cache8_join(Cache8Attend a, T* __restrict__ out,
+                                                     const float* __restrict__ part,
+                                                     const float* __restrict__ part_ml,
+                                                     int64_t columns, int splits, int chunk) {
+  const Cache8Geo& g = a.g;
+  const int64_t at = (int64_t)blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4);
+  if (at >= columns) return;
+  const int d0 = threadIdx.x % (D / 4) * 4, G = a.heads / g.heads;
+  const int64_t per = (int64_t)a.L * G, prob = at / per, b = prob / g.heads;
+  const int col = (int)(at - prob * per), i = col / G;
+  const int h = (int)(prob - b * g.heads) * G + col - i * G;
+  if (a.n_rows && i >= a.n_rows[b]) return;
+  const int len = min(max(a.lens[b], 0), a.max_rows), live = min(splits, (len + chunk - 1) / chunk);
+  float m = -FLT_MAX, l = 0.f;
+  f32x4 o = zero4();
+  for (int s = 0; s < live; ++s) m = fmaxf(m, part_ml[(at * splits + s) * 2]);
+  for (int s = 0; s < live; ++s) {
+    const float f = exp2_hw(part_ml[(at * splits + s) * 2] - m);
+    l = fmaf(part_ml[(at * splits + s) * 2 + 1], f, l);
+    o += *reinterpret_cast<const f32x4*>(part + (at * splits + s) * D + d0) * f;
+  }
+  T* p = out + b * a.so[0] + i * a.so[1] + h * a.so[2] + d0;
+  const float inv = l == 0.f ? 0.f : 1.0f / l;
+#pragma unroll
+  for (int j = 0; j < 4; ++j) st(p + j, l == 0.f ? 0.f : o[j] * inv);
+  if (a.lse && d0 == 0)
+    a.lse[(b * a.L + i) * a.heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+}
+
+// How a call is cut: 16 QB columns per wave, the waves of a workgroup on the same columns or not, and
+// the keys in `splits` pieces of `chunk`.
+struct Cut {
+  int qb, coltiles, splits, chunk;
+  bool split;
+};
+
+Cut cut_of(const Cache8Attend& a, bool f32) {
+  Cut c;
+  const int64_t cols = (int64_t)a.L * (a.heads / a.g.heads), probs = (int64_t)a.B * a.g.heads;
+  c.split = cols <= 32;
+  c.qb = c.split ? (cols <= 16 ? 1 : 2) : (f32 ? 1 : a.g.d <= 32 ? 4 : 2);
+  const int per = 16 * c.qb * (c.split ? 1 : 4);
+  c.coltiles = (int)((cols + per - 1) / per);
+  const int64_t blocks = probs * c.coltiles, want = 2048;
+  const int least = c.split ? 512 : 1024;  // keys worth a workgroup of their own
+  int64_t s = blocks > 0 ? (want + blocks - 1) / blocks : 1;
+  s = s < (a.max_rows + least - 1) / least ? s : (a.max_rows + least - 1) / least;
+  if (s < 1) s = 1;
+  c.chunk = (int)((((int64_t)a.max_rows + s - 1) / s + 255) / 256 * 256);
+  if (c.chunk < 256) c.chunk = 256;
+  c.splits = (int)(((int64_t)a.max_rows + c.chunk - 1) / c.chunk);
+  if (c.splits < 1) c.splits = 1;
+  return c;
+}
+
+int64_t partials(const Cache8Attend& a, const Cut& c) {
+  return c.splits > 1 ? (int64_t)a.B * a.g.heads * a.L * (a.heads / a.g.heads) * c.splits : 0;
+}
+
+template <int D, class T, int QB, bool SPLIT>
+hipError_t go(const Cache8Attend& a, const Cut& c, const T* q, T* out, hipStream_t s) {
+  const int64_t probs = (int64_t)a.B * a.g.heads, n = partials(a, c);
+  float* part = (float*)a.ws;
+  float* ml = part + n * D;
+  bool wide = (uintptr_t)q % 16 == 0 && (uintptr_t)out % 16 == 0;
+  for (int i = 0; i < 3; ++i)
+    wide = wide && a.sq[i] * sizeof(T) % 16 == 0 && a.so[i] * sizeof(T) % 16 == 0;
+  const int64_t each = (int64_t)c.coltiles * c.splits, most = ((int64_t(1) << 32) - 1) / 256 / each;
+  for (int64_t p0 = 0; p0 < probs; p0 += most) {
+    const unsigned blocks = (unsigned)((probs - p0 < most ? probs - p0 : most) * each);
+    if (a.g.page >= KT)
+      k_cache8_attend<D, T, QB, SPLIT, true><<<blocks, 256, 0, s>>>(
+          a, q, out, part, ml, p0, c.coltiles, c.splits, c.chunk, wide);
+    else
+      k_cache8_attend<D, T, QB, SPLIT, false><<<blocks, 256, 0, s>>>(
+          a, q, out, part, ml, p0, c.coltiles, c.splits, c.chunk, wide);
+  }
+  if (c.splits > 1) {
+    const int64_t columns = n / c.splits, per = 256 / (D / 4);
+    k_cache8_join<D, T><<<(unsigned)((columns + per - 1) / per), 256, 0, s>>>(
+        a, out, part, ml, columns, c.splits, c.chunk);
+  }
+  return hipGetLastError();
+}
+
+template <int D, class T>
+hipError_t go_d(const Cache8Attend& a, const T* q, T* out, hipStream_t s) {
+  const Cut c = cut_of(a, sizeof(T) == 4);
+  if (c.split)
+    return c.qb == 1 ? go<D, T, 1, true>(a, c, q, out, s) : go<D, T, 2, true>(a, c, q, out, s);
+  return go<D, T, sizeof(T) == 4 ? 1 : D <= 32 ? 4 : 2, false>(a, c, q, out, s);
 }
 
 }  // namespace
 
-size_t cache8_attend_bytes(const Cache8Attend&) { return 0; }
+size_t cache8_attend_bytes(const Cache8Attend& a, bool f32) {
+  return (size_t)partials(a, cut_of(a, f32)) * (a.g.d + 2) * 4;
+}
 
 template <class T>
 hipError_t launch_cache8_attend(const Cache8Attend& a, const T* q, T* out, hipStream_t s) {
-  const int64_t items = (int64_t)a.B * a.L * a.heads;
-  k_cache8_attend<T><<<(unsigned)(items < kMaxBlocks ? items : kMaxBlocks), 64, 0, s>>>(a, q, out,
-                                                                                       items);
-  return hipGetLastError();
+  switch (a.g.d) {
+    case 16: return go_d<16>(a, q, out, s);
+    case 32: return go_d<32>(a, q, out, s);
+    case 64: return go_d<64>(a, q, out, s);
+    default: return go_d<128>(a, q, out, s);
+  }
 }
 template hipError_t launch_cache8_attend(const Cache8Attend&, const float*, float*, hipStream_t);
 template hipError_t launch_cache8_attend(const Cache8Attend&, const bf16*, bf16*, hipStream_t);

@@ -67,7 +67,7 @@ def test_pool_bytes():
 
 
 @pytest.mark.parametrize("kw", [
-    dict(B=-1), dict(L=-1), dict(max_pages=-1), dict(max_pages=(1 << 31) // 64),
+    dict(B=-1), dict(L=-1), dict(max_pages=-1), dict(max_pages=(1 << 30) // 64 + 1),
     dict(B=1 << 16, max_pages=1 << 15), dict(dtype=2), dict(stride_k=(-1, 64, 32)),
     dict(stride_v=(0, (1 << 40) + 1, 0)), dict(B=1 << 20, stride_k=(1 << 40, 0, 0)),
 ])
@@ -77,9 +77,9 @@ def test_rows_refused(kw):
 
 
 @pytest.mark.parametrize("kw", [
-    dict(B=-1), dict(L=-1), dict(max_pages=-1), dict(max_pages=(1 << 31) // 64), dict(dtype=-1),
+    dict(B=-1), dict(L=-1), dict(max_pages=-1), dict(max_pages=(1 << 30) // 64 + 1), dict(dtype=-1),
     dict(heads=0), dict(heads=3), dict(heads=(1 << 16) + 2), dict(B=1 << 16, L=1 << 15),
-    dict(max_len=-1), dict(scale=NAN), dict(scale=INF), dict(stride_q=(0, -1, 0)),
+    dict(B=1, L=1 << 25), dict(max_len=-1), dict(scale=NAN), dict(scale=INF), dict(stride_q=(0, -1, 0)),
     dict(stride_out=(5 * 128, 128, 31)), dict(stride_out=(5 * 128, 100, 32)),
     dict(stride_out=(100, 128, 32)), dict(stride_out=(0, 128, 32)),
     dict(stride_q=((1 << 40) + 1, 0, 0)),
