@@ -7,9 +7,11 @@
 //   S^T = K Q^T     v_mfma_f32_16x16x32_bf16: codes are exact as bfloat16, the block's power goes into
 //                   the scores' factor
 //   p = 2^(S c - ref), online, ref a running reference of the exponent per column
-//   O^T += V^T P^T  v_mfma_f32_16x16x32_f16: codes are exact as half; the block's power goes into p as
-//                   2^(power - unit), unit the largest power that the column has seen so far
+//   O^T += V^T P^T  v_mfma_f32_16x16x32_f16: codes times 2^(power - unit) are exact as half, unit the
+//                   largest power that the wave's columns have seen so far
 //
+// The weights' sum is of the unrounded ones, in float32 (as one more product, 1 P^T, it would cost fewer
+// cycles, but the rounded weights put lse off by up to 2^-12).
 // Row m of the t-th of the tile's four 16-row products is key 16 (m / 4) + 4 t + m % 4, so that a lane's
 // 16 scores are those of 16 keys in a row: one block's, since pages are multiples of 16, and in the
 // order in which the lane reads 16 bytes of V^T.  Nothing moves between lanes, and codes go from memory
@@ -17,12 +19,14 @@
 //
 // p is held as half with 2^14 in front, at most 2^15 with the reference at most 2 below the largest:
 // 2^-12 of each weight, and 2^-39 of the largest where half has no more bits.  bfloat16 would have
-// doubled the output's own rounding error.  Float32 queries are three bfloat16 parts (24 bits) and
-// their weights two halves.
+// doubled the output's own rounding error.  Values are held with 2^7 in front: exact unless their block
+// is 2^22 below the largest, 2^-41 of that one's largest code then.  Float32 queries are three bfloat16
+// parts (24 bits) and their weights two halves.
 //
 // Few columns (SPLIT): the four waves of a workgroup share the columns and take turns over the tiles;
-// many: each wave has columns of its own.  Where the workgroups are too few the keys are split over
-// more of them, and a second launch joins their sums.
+// many: each wave has columns of its own.  A tile's keys are read while the one before it is weighed
+// and summed, its values from then on, and the page after it is looked up.  Where the workgroups are too
+// few the keys are split over more of them, and a second launch joins their sums.
 #include <float.h>
 
 #include "cache8.h"
@@ -37,7 +41,8 @@ typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int KT = 64;              // keys per tile
 constexpr float SLACK = 1.0f;       // ref may lag by this much
-constexpr int P_BIAS = 14;          // weights are held times 2^P_BIAS
+constexpr int P_BIAS = 14, V_BIAS = 7;  // weights and values are held times 2 to these
+constexpr int V_GAP = 20;               // powers of two by which blocks of a product may differ
 
 __device__ __forceinline__ float exp2i(int e) {  // 2^e, e in [-126, 127]
   return __uint_as_float((uint32_t)(e + 127) << 23);
@@ -46,7 +51,7 @@ __device__ __forceinline__ int power_byte(uint32_t e) {
   return min(max((int)e, CACHE8_E_MIN), CACHE8_E_MAX);
 }
 
-// 8 codes (two dwords) as bfloat16 and as half.
+// 8 codes (two dwords) as bfloat16 and, times a power of two, as half.
 __device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
   const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
@@ -55,11 +60,11 @@ __device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi) {
   bf16x8 r = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
   return r;
 }
-__device__ __forceinline__ f16x8 codes_f16(uint32_t lo, uint32_t hi) {
-  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, false);
-  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, 1.0f, true);
-  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, false);
-  const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, 1.0f, true);
+__device__ __forceinline__ f16x8 codes_f16(uint32_t lo, uint32_t hi, float two) {  // times two
+  const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, two, false);
+  const f16x2 b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(lo, two, true);
+  const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, two, false);
+  const f16x2 d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(hi, two, true);
   f16x8 r = {a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
   return r;
 }
@@ -95,18 +100,25 @@ struct KQ<16> {
   }
 };
 
-// What a lane reads of a tile: keys' codes, values' codes, the bytes of both powers of its 16 keys'
+// What a lane reads of a tile: keys' codes; values' codes, the bytes of both powers of its 16 keys'
 // block, and whether there is one.
 template <int D>
-struct Codes {
+struct Keys {
   uint32_t k[4][D / 16];
-  uint4 v[D / 16];
   uint32_t power;
   bool here;
 };
+template <int D>
+struct Values {
+  uint4 v[D / 16];
+};
+
+// Waves per SIMD that the registers of a kernel leave room for.
+template <int D, bool F32, int QB, bool SPLIT>
+constexpr int waves() { return D == 128 && QB == 2 ? 1 : 2; }
 
 template <int D, class T, int QB, bool SPLIT, bool UNI>
-__global__ __launch_bounds__(256) void k_cache8_attend(Cache8Attend a, const T* __restrict__ q,
+__global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void k_cache8_attend(Cache8Attend a, const T* __restrict__ q,
                                                        T* __restrict__ out, float* __restrict__ part,
                                                        float* __restrict__ part_ml, int64_t prob0,
                                                        int coltiles, int splits, int chunk,
@@ -203,29 +215,25 @@ __global__ __launch_bounds__(256) void k_cache8_attend(Cache8Attend a, const T* 
   constexpr int STEP = SPLIT ? 4 * KT : KT;
   const int page = g.page, shift = g.shift;
   const int64_t hd = (int64_t)g.heads * page * D;  // bytes of a page
-  // of the keys 16 (c / 4) .. and 16 lg .. of the tile
+  // the pages of the keys 16 (c / 4) .. and 16 lg .. of a tile (UNI: one page, the same in every lane)
+  const int gk = UNI ? 0 : c >> 2, gv = UNI ? 0 : lg;
   auto pid_of = [&](int t0, int grp) {
     const int e = min((t0 + 16 * grp) >> shift, g.max_pages - 1);
     return cache8_page(g, b, e);
   };
-  auto load = [&](Codes<D>& x, int t0, int pk, int pv) {
-    // UNI: one page, and pk == pv is the same in every lane
-    const int ck = c >> 2;
-    const uint8_t *kb, *vb, *pb;
+  auto load_k = [&](Keys<D>& x, int t0, int pk, int pv) {
     x.here = pv >= 0;
     pk = max(pk, 0);
     pv = max(pv, 0);
-    if constexpr (UNI) {
-      const int slot = t0 & (page - 1);
-      kb = g.keys + pk * hd + ((int64_t)kh * page + slot) * D + (16 * ck + (c & 3)) * D + lg * (D / 4);
-      vb = g.values + pk * hd + (int64_t)kh * page * D + slot + c * page + 16 * lg;
-    } else {
-      const int sk = (t0 + 16 * ck) & (page - 1), sv = (t0 + 16 * lg) & (page - 1);
-      kb = g.keys + pk * hd + ((int64_t)kh * page + sk + (c & 3)) * D + lg * (D / 4);
-      vb = g.values + pv * hd + (int64_t)kh * page * D + sv + c * page;
-    }
-    pb = g.powers + ((int64_t)pv * g.heads + kh) * 2;
-    x.power = *reinterpret_cast<const uint16_t*>(pb);
+    const int ck = c >> 2;
+    const uint8_t* kb;
+    if constexpr (UNI)
+      kb = g.keys + pk * hd + ((int64_t)kh * page + (t0 & (page - 1))) * D +
+           (16 * ck + (c & 3)) * D + lg * (D / 4);
+    else
+      kb = g.keys + pk * hd + ((int64_t)kh * page + ((t0 + 16 * ck) & (page - 1)) + (c & 3)) * D +
+           lg * (D / 4);
+    x.power = *reinterpret_cast<const uint16_t*>(g.powers + ((int64_t)pv * g.heads + kh) * 2);
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       if constexpr (D == 16) {
@@ -241,209 +249,253 @@ __global__ __launch_bounds__(256) void k_cache8_attend(Cache8Attend a, const T* 
         }
       }
     }
+  };
+  auto load_v = [&](Values<D>& x, int t0, int pv) {
+    pv = max(pv, 0);
+    const uint8_t* vb = g.values + pv * hd + (int64_t)kh * page * D +
+                        (UNI ? (t0 & (page - 1)) + 16 * lg : (t0 + 16 * lg) & (page - 1)) + c * page;
 #pragma unroll
     for (int db = 0; db < DB; ++db)
       x.v[db] = *reinterpret_cast<const uint4*>(vb + (int64_t)db * 16 * page);
   };
 
-  float ref[QB], lsum[QB];
-  int unit[QB];
+  float ref[QB], lsum[QB];  // lsum: of the lane's own keys
   f32x4 oacc[DB][QB];
+  int unit = CACHE8_E_MIN;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    unit[qb] = CACHE8_E_MIN;
     ref[qb] = -FLT_MAX;
     lsum[qb] = 0.f;
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db][qb] = zero4();
   }
-
-  auto compute = [&](Codes<D>& x, int t0) {
-    f32x4 s[4][QB];
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) s[t][qb] = zero4();
-#pragma unroll
-      for (int ch = 0; ch < CH; ++ch) {
-        QF kf;
-        if constexpr (D == 16) {
-          const bf16x8 w = codes_bf16(x.k[t][0], 0);
-          __builtin_memcpy(&kf, &w, 8);
-        } else {
-          kf = codes_bf16(x.k[t][2 * ch], x.k[t][2 * ch + 1]);
-        }
-#pragma unroll
-        for (int n = NQ - 1; n >= 0; --n)
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb) s[t][qb] = KQ<D>::mma(kf, qf[n][qb][ch], s[t][qb]);
-      }
+  auto key_frag = [&](const Keys<D>& x, int t, int ch) {
+    QF kf;
+    if constexpr (D == 16) {
+      const bf16x8 w = codes_bf16(x.k[t][0], 0);
+      __builtin_memcpy(&kf, &w, 8);
+    } else {
+      kf = codes_bf16(x.k[t][2 * ch], x.k[t][2 * ch + 1]);
     }
-    const int ek = power_byte(x.power & 0xff), ev = power_byte(x.power >> 8);
-    const float cs = fmaxf(scale * exp2i(ek - 127), 0x1p-126f);
-    const bool partial = t0 + KT > lo || __any(!x.here);
-    // the largest power of values that a column has seen; a larger one than before rescales its sums
-    // (a block that the column does not see must not: its power may be anything)
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      int top = ev;
-      if (partial) top = x.here && t0 + 16 * lg < upto[qb] ? ev : 0;
-      if constexpr (!UNI) {
-        top = max(top, __shfl_xor(top, 16, 64));
-        top = max(top, __shfl_xor(top, 32, 64));
-      } else if (partial) {
-        top = __shfl(top, c, 64);
-      }
-      if (__any(top > unit[qb])) {
-        const int now = max(top, unit[qb]);
-        const float f = exp2i(unit[qb] - now);
-#pragma unroll
-        for (int db = 0; db < DB; ++db) oacc[db][qb] *= f;
-        unit[qb] = now;
-      }
-    }
-    uint32_t nans = 0;
+    return kf;
+  };
+  // Scores of block qb (in place) to its weights.
+  auto weigh = [&](f32x4* s, int qb, float cs, int t0, bool partial, bool here, f16x8 (*pf)[2]) {
     if (partial) {
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = t0 + 16 * lg + 4 * t + i;
+        for (int i = 0; i < 4; ++i)
+          if (t0 + 16 * lg + 4 * t + i >= upto[qb] || !here) s[t][i] = -INFINITY;
+    }
+    float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb)
-            if (key >= upto[qb] || !x.here) s[t][qb][i] = -INFINITY;
+    for (int t = 1; t < 4; ++t) mx = fmaxf(mx, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
+    mx *= cs;
+    if (__any(mx > ref[qb] + SLACK)) {
+      const float now = fmaxf(ref[qb], rows4_max(mx)), corr = exp2_hw(ref[qb] - now);
+      ref[qb] = now;
+      lsum[qb] *= corr;
+#pragma unroll
+      for (int db = 0; db < DB; ++db) oacc[db][qb] *= corr;
+    }
+    const float off = (float)P_BIAS - ref[qb];
+    float sum[2] = {0.f, 0.f};
+#pragma unroll
+    for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float p = exp2_hw(fmaf(s[2 * kc + j / 4][j % 4], cs, off));
+        sum[kc] += p;
+        const _Float16 h = (_Float16)p;
+        pf[0][kc][j] = h;
+        if constexpr (NP == 2) pf[1][kc][j] = (_Float16)(p - (float)h);
+      }
+    lsum[qb] += sum[0] + sum[1];
+  };
+  auto compute = [&](Keys<D>& x, Values<D>& y, int t0, auto keys_read) {
+    const int ek = power_byte(x.power & 0xff), ev = power_byte(x.power >> 8);
+    const bool here = x.here;
+    const float cs = fmaxf(scale * exp2i(ek - 127), 0x1p-126f);
+    const bool partial = t0 + KT > lo || __any(!here);
+    f16x8 pf[QB][NP][2];
+    if constexpr (D <= 32) {
+      // one block of columns after another, the next one's products under way
+      QF kf[4][CH];
+#pragma unroll
+      for (int t = 0; t < 4; ++t)
+#pragma unroll
+        for (int ch = 0; ch < CH; ++ch) kf[t][ch] = key_frag(x, t, ch);
+      keys_read();
+      f32x4 s[2][4];
+      auto products = [&](f32x4* r, int qb) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          r[t] = zero4();
+#pragma unroll
+          for (int ch = 0; ch < CH; ++ch)
+#pragma unroll
+            for (int n = NQ - 1; n >= 0; --n) r[t] = KQ<D>::mma(kf[t][ch], qf[n][qb][ch], r[t]);
         }
+      };
+      products(s[0], 0);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        if (qb + 1 < QB) products(s[(qb + 1) & 1], qb + 1);
+        weigh(s[qb & 1], qb, cs, t0, partial, here, pf[qb]);
+      }
+    } else {
+      f32x4 s[QB][4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+#pragma unroll
+        for (int qb = 0; qb < QB; ++qb) s[qb][t] = zero4();
+#pragma unroll
+        for (int ch = 0; ch < CH; ++ch) {
+          const QF kf = key_frag(x, t, ch);
+#pragma unroll
+          for (int n = NQ - 1; n >= 0; --n)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) s[qb][t] = KQ<D>::mma(kf, qf[n][qb][ch], s[qb][t]);
+        }
+      }
+      keys_read();
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) weigh(s[qb], qb, cs, t0, partial, here, pf[qb]);
+    }
+    uint32_t nans = 0;
+    bool apart = false;
+    // the largest power among the blocks that any column sees; others' bytes may be anything
+    int top = ev;
+    if (partial) {
+      const bool seen = here && t0 + 16 * lg < hi;
+      top = seen ? ev : 0;
 #pragma unroll
       for (int db = 0; db < DB; ++db)
-        nans |= nan_bytes(x.v[db].x) | nan_bytes(x.v[db].y) | nan_bytes(x.v[db].z) | nan_bytes(x.v[db].w);
-    }
-    f16x8 pf[NP][QB][2];
-#pragma unroll
-    for (int qb = 0; qb < QB; ++qb) {
-      float mx = fmaxf(fmaxf(s[0][qb][0], s[0][qb][1]), fmaxf(s[0][qb][2], s[0][qb][3]));
-#pragma unroll
-      for (int t = 1; t < 4; ++t)
-        mx = fmaxf(mx, fmaxf(fmaxf(s[t][qb][0], s[t][qb][1]), fmaxf(s[t][qb][2], s[t][qb][3])));
-      mx *= cs;
-      if (__any(mx > ref[qb] + SLACK)) {
-        const float now = fmaxf(ref[qb], rows4_max(mx)), corr = exp2_hw(ref[qb] - now);
-        ref[qb] = now;
-        lsum[qb] *= corr;
-#pragma unroll
-        for (int db = 0; db < DB; ++db) oacc[db][qb] *= corr;
+        nans |= nan_bytes(y.v[db].x) | nan_bytes(y.v[db].y) | nan_bytes(y.v[db].z) | nan_bytes(y.v[db].w);
+      if constexpr (!UNI) {
+        int low = seen ? ev : 255, high = top;
+        low = min(low, __shfl_xor(low, 16, 64));
+        low = min(low, __shfl_xor(low, 32, 64));
+        high = max(high, __shfl_xor(high, 16, 64));
+        high = max(high, __shfl_xor(high, 32, 64));
+        apart = __builtin_amdgcn_readfirstlane(high - low) > V_GAP;
       }
-      const int rel = ev - unit[qb] + P_BIAS;
-      const float off = (float)rel - ref[qb];
-      float sum = 0.f;
+      if (__any(nans != 0)) {
+        // NaN codes (or what lies behind the last key): out of the products, whose weight for them
+        // may be 0, and NaN in the sums of the columns that see them
 #pragma unroll
-      for (int kc = 0; kc < 2; ++kc) {
-        float p[8];
+        for (int db = 0; db < DB; ++db) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(&y.v[db]);
+          f32x4 cnt[QB];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          p[j] = exp2_hw(fmaf(s[2 * kc + j / 4][qb][j % 4], cs, off));
-          sum += p[j];
-        }
+          for (int qb = 0; qb < QB; ++qb) cnt[qb] = zero4();
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          const _Float16 h = (_Float16)p[j];
-          pf[0][qb][kc][j] = h;
-          if constexpr (NP == 2) pf[1][qb][kc][j] = (_Float16)(p[j] - (float)h);
-        }
-      }
-      lsum[qb] = fmaf(sum, exp2i(-rel), lsum[qb]);
-    }
-    if (partial && __any(nans != 0)) {
-      // NaN codes (or what lies behind the last key): out of the products, whose weight for them
-      // may be 0, and NaN in the sums of the columns that see them
-#pragma unroll
-      for (int db = 0; db < DB; ++db) {
-        uint32_t* w = reinterpret_cast<uint32_t*>(&x.v[db]);
-        f32x4 cnt[QB];
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) cnt[qb] = zero4();
-#pragma unroll
-        for (int kc = 0; kc < 2; ++kc) {
-          f16x8 is;
-#pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const uint32_t m = nan_bytes(w[2 * kc + j / 4]) >> (8 * (j % 4) + 7) & 1;
-            is[j] = (_Float16)(float)m;
-          }
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb) {
-            f16x8 sees;
+          for (int kc = 0; kc < 2; ++kc) {
+            f16x8 is;
 #pragma unroll
             for (int j = 0; j < 8; ++j)
-              sees[j] = (_Float16)(x.here && t0 + 16 * lg + 8 * kc + j < upto[qb] ? 1.f : 0.f);
-            cnt[qb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(is, sees, cnt[qb], 0, 0, 0);
+              is[j] = (_Float16)(float)(nan_bytes(w[2 * kc + j / 4]) >> (8 * (j % 4) + 7) & 1);
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) {
+              f16x8 sees;
+#pragma unroll
+              for (int j = 0; j < 8; ++j)
+                sees[j] = (_Float16)(here && t0 + 16 * lg + 8 * kc + j < upto[qb] ? 1.f : 0.f);
+              cnt[qb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(is, sees, cnt[qb], 0, 0, 0);
+            }
+          }
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+              if (cnt[qb][i] > 0.f) oacc[db][qb][i] = __builtin_nanf("");
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const uint32_t m = nan_bytes(w[j]);
+            w[j] &= ~(m | (m - (m >> 7)));  // 0x80 to 0xff
           }
         }
+      }
+    }
+    // only: the group of lanes whose keys count, -1: all
+    auto sum = [&](int only) {
+      int now = only < 0 || lg == only ? top : 0;
+      if constexpr (UNI) {
+        now = __builtin_amdgcn_readfirstlane(now);
+      } else {
+        now = max(now, __shfl_xor(now, 16, 64));
+        now = __builtin_amdgcn_readfirstlane(max(now, __shfl_xor(now, 32, 64)));
+      }
+      if (now > unit) {
+        const float f = exp2i(unit - now);
+#pragma unroll
+        for (int db = 0; db < DB; ++db)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) oacc[db][qb] *= f;
+        unit = now;
+      }
+      // (a block that no column sees: any power will do)
+      const float two = exp2i(min(ev - unit, 0) + V_BIAS);
+#pragma unroll
+      for (int kc = 0; kc < 2; ++kc) {
+        f16x8 pw[QB][NP];
 #pragma unroll
         for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (cnt[qb][i] > 0.f) oacc[db][qb][i] = __builtin_nanf("");
+          for (int n = 0; n < NP; ++n) {
+            pw[qb][n] = pf[qb][n][kc];
+            if (only >= 0 && lg != only) pw[qb][n] = f16x8{};
+          }
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const uint32_t m = nan_bytes(w[j]);
-          w[j] &= ~(m | (m - (m >> 7)));  // 0x80 to 0xff
+        for (int db = 0; db < DB; ++db) {
+          const f16x8 vf = kc ? codes_f16(y.v[db].z, y.v[db].w, two)
+                              : codes_f16(y.v[db].x, y.v[db].y, two);
+#pragma unroll
+          for (int n = NP - 1; n >= 0; --n)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb)
+              oacc[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pw[qb][n], oacc[db][qb], 0, 0, 0);
         }
       }
+    };
+    if (UNI || !apart) {
+      sum(-1);
+    } else {
+      // a block far larger than another, and columns that may see the other alone: block by block
+      for (int grp = 0; grp < 4; ++grp) sum(grp);
     }
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-      for (int kc = 0; kc < 2; ++kc) {
-        const f16x8 vf = kc ? codes_f16(x.v[db].z, x.v[db].w) : codes_f16(x.v[db].x, x.v[db].y);
-#pragma unroll
-        for (int n = NP - 1; n >= 0; --n)
-#pragma unroll
-          for (int qb = 0; qb < QB; ++qb)
-            oacc[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n][qb][kc], oacc[db][qb], 0, 0, 0);
-      }
   };
 
-  // tiles t0, t0 + STEP, ...: the next tile's codes are on their way while one is computed, and the
-  // page of the one after it
   int t0 = k0 + (SPLIT ? wave * KT : 0);
   if (t0 < kend) {
-    Codes<D> x, y;
-    const int gk = UNI ? 0 : c >> 2, gv = UNI ? 0 : lg;
+    Keys<D> x;
+    Values<D> y;
     int pk = pid_of(t0, gk), pv = UNI ? pk : pid_of(t0, gv);
-    load(x, t0, pk, pv);
-    if (t0 + STEP < kend) {
-      pk = pid_of(t0 + STEP, gk);
-      pv = UNI ? pk : pid_of(t0 + STEP, gv);
-    }
-    for (;;) {
-      if (t0 + STEP < kend) {
-        load(y, t0 + STEP, pk, pv);
-        if (t0 + 2 * STEP < kend) {
-          pk = pid_of(t0 + 2 * STEP, gk);
-          pv = UNI ? pk : pid_of(t0 + 2 * STEP, gv);
-        }
+    auto next_page = [&](int t) {
+      if (t < kend) {
+        pk = pid_of(t, gk);
+        pv = UNI ? pk : pid_of(t, gv);
       }
-      compute(x, t0);
-      t0 += STEP;
-      if (t0 >= kend) break;
-      if (t0 + STEP < kend) {
-        load(x, t0 + STEP, pk, pv);
-        if (t0 + 2 * STEP < kend) {
-          pk = pid_of(t0 + 2 * STEP, gk);
-          pv = UNI ? pk : pid_of(t0 + 2 * STEP, gv);
-        }
-      }
-      compute(y, t0);
-      t0 += STEP;
-      if (t0 >= kend) break;
+    };
+    load_k(x, t0, pk, pv);
+    load_v(y, t0, pv);
+    next_page(t0 + STEP);
+    for (; t0 < kend; t0 += STEP) {
+      const bool more = t0 + STEP < kend;
+      compute(x, y, t0, [&] {
+        if (more) load_k(x, t0 + STEP, pk, pv);
+      });
+      if (more) load_v(y, t0 + STEP, pv);
+      next_page(t0 + 2 * STEP);
     }
   }
 
   // the sums in units of 1, over all lanes of a column
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    const float one = exp2i(unit[qb] - 127 - P_BIAS);
-    lsum[qb] = rows4_sum(lsum[qb]);
+    const float one = exp2i(unit - 127 - V_BIAS - P_BIAS);
+    lsum[qb] = rows4_sum(lsum[qb]) * exp2i(-P_BIAS);
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db][qb] *= one;
   }
