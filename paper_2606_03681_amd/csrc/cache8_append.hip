@@ -1,14 +1,22 @@
 // Rows of keys and values into a pool of e4m3 codes (declarations in cache8.h).
 //
-// A workgroup per block (page, head) that gets rows.  Every step is exact but the rounding to a code,
-// so that the bytes do not depend on how the work is split: the power of two comes from the bits of
-// the block's largest magnitude, and products with powers of two do not round.
+// A block (page, head) that gets rows goes to one wave, or to a workgroup where it may get more than a
+// wave's registers hold.  A lane has 8 channels of 4 rows in a row: it reads them once (again, from the
+// caches, where there are more than one such piece for a lane), the lanes' largest magnitudes give the
+// block's power, and the codes of the keys go out as they are, those of the values through LDS, where
+// 4 rows of a channel are one word and 16 leave together.
+//
+// Every step is exact but the rounding to a code, so that the bytes do not depend on how the work is
+// split: the power of two comes from the bits of the largest magnitude, and products with powers of two
+// do not round.
 #include "cache8.h"
+#include "mfma.h"
+#include "wave.h"
 
 namespace tfm {
 namespace {
 
-constexpr int kMaxBlocks = 1 << 20;
+constexpr int kMaxBlocks = 1 << 23;
 
 // The byte of the least power with m <= 448 2^(e - 127): 448 = 1.75 2^8.
 __device__ __forceinline__ int power_of(float m) {
@@ -16,80 +24,184 @@ __device__ __forceinline__ int power_of(float m) {
   const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u);
   return min(max(e, CACHE8_E_MIN), CACHE8_E_MAX);
 }
+__device__ __forceinline__ int power_byte(uint32_t e) {
+  return min(max((int)e, CACHE8_E_MIN), CACHE8_E_MAX);
+}
 __device__ __forceinline__ float two_to(int e) {  // 2^e, -126 <= e <= 127
   return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 __device__ __forceinline__ bool fits(float x) { return fabsf(x) <= 0x1.cp56f; }  // 448 2^48
-__device__ __forceinline__ uint8_t code_of(float x) {
-  return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(x, 0.f, 0, false);
+
+// Four codes of x f, NaN where x does not fit.
+__device__ __forceinline__ uint32_t codes(const float* x, float f) {
+  float y[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) y[i] = fits(x[i]) ? x[i] * f : __builtin_nanf("");
+  int w = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], w, true);
+}
+__device__ __forceinline__ uint8_t again(uint8_t c, float f) {  // a code under another power
+  if ((c & 0x7f) == 0x7f) return c;
+  return (uint8_t)__builtin_amdgcn_cvt_pk_fp8_f32(__builtin_amdgcn_cvt_f32_fp8(c, 0) * f, 0.f, 0, false);
 }
 
+// 8 channels of a row, as they lie.
 template <class T>
+struct Piece {
+  uint32_t w[2 * sizeof(T)];
+  __device__ __forceinline__ void load(const T* p, bool wide, bool on) {
+#pragma unroll
+    for (int i = 0; i < (int)(2 * sizeof(T)); ++i) w[i] = 0;
+    if (!on) return;
+    if (wide) {
+#pragma unroll
+      for (int i = 0; i < (int)sizeof(T) / 2; ++i) {
+        const uint4 u = reinterpret_cast<const uint4*>(p)[i];
+        w[4 * i] = u.x; w[4 * i + 1] = u.y; w[4 * i + 2] = u.z; w[4 * i + 3] = u.w;
+      }
+    } else if constexpr (sizeof(T) == 4) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(p[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = p[2 * i] | (uint32_t)p[2 * i + 1] << 16;
+    }
+  }
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    return __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
+  }
+};
+
+template <class T>
+__device__ __forceinline__ float largest(const Piece<T>* x, float m) {
+#pragma unroll
+  for (int r = 0; r < 4; ++r)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const float a = fabsf(x[r].get(i));
+      m = fits(a) ? fmaxf(m, a) : m;
+    }
+  return m;
+}
+
+// W: waves to a block; HOLD: its rows are read once; ls: bytes between channels in LDS.
+template <class T, int W, bool HOLD>
 __global__ __launch_bounds__(256) void k_cache8_append(Cache8Append a, const T* __restrict__ k,
                                                        const T* __restrict__ v, int slots,
-                                                       int64_t items) {
-  __shared__ uint32_t top[2];
+                                                       int64_t items, int ls, int wide) {
+  extern __shared__ __attribute__((aligned(16))) uint8_t lds[];
+  __shared__ float tops[4][2];
   const Cache8Geo& g = a.g;
-  const int d = g.d, page = g.page, tid = threadIdx.x;
-  for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
+  const int d = g.d, page = g.page, wave = wave_id(), lane = threadIdx.x & 63;
+  const int tid = W == 1 ? lane : (int)threadIdx.x;
+  constexpr int N = 64 * W;
+  uint8_t* img = lds + (W == 1 ? wave * ls * d : 0);
+  const int64_t u0 = (int64_t)blockIdx.x * (4 / W) + (W == 1 ? wave : 0);
+  const int64_t cap = (int64_t)g.max_pages << g.shift;
+  const int dp = d / 8;  // pieces of a row
+  for (int64_t it = u0; it < items; it += (int64_t)gridDim.x * (4 / W)) {
     const int h = (int)(it % g.heads);
-    const int64_t bs = it / g.heads;
-    const int64_t b = bs / slots;
-    const int64_t cap = (int64_t)g.max_pages << g.shift;
+    const int64_t bs = it / g.heads, b = bs / slots;
     const int64_t first = a.lens ? min(max((int64_t)a.lens[b], (int64_t)0), cap) : 0;
     const int64_t n = a.n_new ? min(max(a.n_new[b], 0), a.L) : a.L;
-    const int64_t e = (first >> g.shift) + bs % slots;
+    const int64_t e = (first >> g.shift) + (bs - b * slots);
     const int64_t lo = max(first, e << g.shift), hi = min(min(first + n, (e + 1) << g.shift), cap);
     if (lo >= hi) continue;
     const int pid = cache8_page(g, b, (int)e);
     if (pid < 0) continue;
-    const int had = (int)(lo - (e << g.shift)), m = (int)(hi - lo);
+    const int had = (int)(lo - (e << g.shift)), end = had + (int)(hi - lo);
     const int64_t block = (int64_t)pid * g.heads + h;
-    const T* kr = k + b * a.sk[0] + (lo - first) * a.sk[1] + h * a.sk[2];
-    const T* vr = v + b * a.sv[0] + (lo - first) * a.sv[1] + h * a.sv[2];
-    __syncthreads();
-    if (tid < 2) top[tid] = 0;
-    __syncthreads();
-    float mk = 0.f, mv = 0.f;
-    for (int i = tid; i < m * d; i += 256) {
-      const float x = fabsf(ld(kr + (i / d) * a.sk[1] + i % d));
-      const float y = fabsf(ld(vr + (i / d) * a.sv[1] + i % d));
-      if (fits(x)) mk = fmaxf(mk, x);
-      if (fits(y)) mv = fmaxf(mv, y);
-    }
-    atomicMax(&top[0], __float_as_uint(mk));
-    atomicMax(&top[1], __float_as_uint(mv));
-    __syncthreads();
+    const int g0 = had / 16, ng = (end + 15) / 16 - g0;  // the image: slots from 16 g0 on
+    // slot s of the block is row lo - first + s - had
+    const T* kr = k + b * a.sk[0] + (lo - first - had) * a.sk[1] + h * a.sk[2];
+    const T* vr = v + b * a.sv[0] + (lo - first - had) * a.sv[1] + h * a.sv[2];
     uint8_t* pw = g.powers + block * 2;
-    int ek = power_of(__uint_as_float(top[0])), ev = power_of(__uint_as_float(top[1]));
-    int ok = ek, ov = ev;
-    if (had) {
-      ok = min(max((int)pw[0], CACHE8_E_MIN), CACHE8_E_MAX);
-      ov = min(max((int)pw[1], CACHE8_E_MIN), CACHE8_E_MAX);
-      ek = max(ek, ok);
-      ev = max(ev, ov);
-    }
-    __syncthreads();
-    if (tid == 0) pw[0] = (uint8_t)ek, pw[1] = (uint8_t)ev;
-    uint8_t* kc = g.keys + block * page * d;
-    uint8_t* vc = g.values + block * page * d;
-    if (ok != ek || ov != ev) {
-      for (int i = tid; i < had * d; i += 256) {
-        uint8_t* p = kc + i;
-        uint8_t* r = vc + (i % d) * page + i / d;
-        if (ok != ek && (*p & 0x7f) != 0x7f)
-          *p = code_of(__builtin_amdgcn_cvt_f32_fp8(*p, 0) * two_to(ok - ek));
-        if (ov != ev && (*r & 0x7f) != 0x7f)
-          *r = code_of(__builtin_amdgcn_cvt_f32_fp8(*r, 0) * two_to(ov - ev));
+    const uint8_t pk = pw[0], pv = pw[1];
+    const int q0 = had / 4, nq = ((end + 3) / 4 - q0) * dp;  // pieces of four rows
+    Piece<T> x[4], y[4];
+    auto load = [&](int i) {
+      const int s0 = 4 * (q0 + i / dp), c0 = i % dp * 8;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const bool on = i < nq && s0 + r >= had && s0 + r < end;
+        x[r].load(kr + (s0 + r) * a.sk[1] + c0, wide, on);
+        y[r].load(vr + (s0 + r) * a.sv[1] + c0, wide, on);
+      }
+    };
+    float mk = 0.f, mv = 0.f;
+    if constexpr (HOLD) {
+      load(tid);
+      mk = largest(x, mk);
+      mv = largest(y, mv);
+    } else {
+      for (int i = tid; i < nq; i += N) {
+        load(i);
+        mk = largest(x, mk);
+        mv = largest(y, mv);
       }
     }
-    const float fk = two_to(127 - ek), fv = two_to(127 - ev);
-    for (int i = tid; i < m * d; i += 256) {
-      const float x = ld(kr + (i / d) * a.sk[1] + i % d);
-      const float y = ld(vr + (i / d) * a.sv[1] + i % d);
-      kc[had * d + i] = fits(x) ? code_of(x * fk) : CACHE8_NAN;
-      vc[(i % d) * page + had + i / d] = fits(y) ? code_of(y * fv) : CACHE8_NAN;
+    mk = wave_max(mk);
+    mv = wave_max(mv);
+    if constexpr (W > 1) {
+      __syncthreads();  // the last block's image has left
+      if (lane == 0) tops[wave][0] = mk, tops[wave][1] = mv;
+      __syncthreads();
+      mk = fmaxf(fmaxf(tops[0][0], tops[1][0]), fmaxf(tops[2][0], tops[3][0]));
+      mv = fmaxf(fmaxf(tops[0][1], tops[1][1]), fmaxf(tops[2][1], tops[3][1]));
     }
+    int ek = power_of(mk), ev = power_of(mv);
+    uint8_t* kc = g.keys + block * page * d;
+    uint8_t* vc = g.values + block * page * d;
+    if (had) {
+      const int ok = power_byte(pk), ov = power_byte(pv);
+      ek = max(ek, ok);
+      ev = max(ev, ov);
+      if (ok != ek) {
+        for (int i = tid; i < had * d; i += N) kc[i] = again(kc[i], two_to(ok - ek));
+      }
+      if (ov != ev) {
+        for (int i = tid; i < had * d; i += N) {
+          uint8_t* p = vc + (i % d) * page + i / d;
+          *p = again(*p, two_to(ov - ev));
+        }
+      }
+    }
+    if (tid == 0) *reinterpret_cast<uint16_t*>(pw) = (uint16_t)(ek | ev << 8);
+    const float fk = two_to(127 - ek), fv = two_to(127 - ev);
+    for (int i = tid; i < nq; i += N) {
+      if constexpr (!HOLD) load(i);
+      const int s0 = 4 * (q0 + i / dp), c0 = i % dp * 8;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        float z[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = x[r].get(j);
+        if (s0 + r >= had && s0 + r < end)
+          *reinterpret_cast<uint2*>(kc + (s0 + r) * d + c0) = make_uint2(codes(z, fk), codes(z + 4, fk));
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const float z[4] = {y[0].get(j), y[1].get(j), y[2].get(j), y[3].get(j)};
+        *reinterpret_cast<uint32_t*>(img + (c0 + j) * ls + s0 - 16 * g0) = codes(z, fv);
+      }
+    }
+    if constexpr (W > 1)
+      __syncthreads();
+    else
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+    // 16 slots of a channel at a time
+    for (int i = tid; i < ng * d; i += N) {
+      const int ch = i / ng, s0 = 16 * (g0 + i - ch * ng);
+      const uint8_t* from = img + ch * ls + s0 - 16 * g0;
+      uint8_t* to = vc + ch * page + s0;
+      if (s0 >= had && s0 + 16 <= end) {
+        *reinterpret_cast<uint4*>(to) = *reinterpret_cast<const uint4*>(from);
+      } else {
+        for (int j = max(had - s0, 0); j < min(end - s0, 16); ++j) to[j] = from[j];
+      }
+    }
+    if constexpr (W == 1) asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 }
 
@@ -97,10 +209,26 @@ __global__ __launch_bounds__(256) void k_cache8_append(Cache8Append a, const T* 
 
 template <class T>
 hipError_t launch_cache8_append(const Cache8Append& a, const T* k, const T* v, hipStream_t s) {
-  const int slots = (int)(((int64_t)a.L + a.g.page - 2) / a.g.page + 1);
-  const int64_t items = (int64_t)a.B * slots * a.g.heads;
-  k_cache8_append<T><<<(unsigned)(items < kMaxBlocks ? items : kMaxBlocks), 256, 0, s>>>(
-      a, k, v, slots, items);
+  const Cache8Geo& g = a.g;
+  const int slots = (int)(((int64_t)a.L + g.page - 2) / g.page + 1);
+  const int64_t items = (int64_t)a.B * slots * g.heads;
+  bool wide = (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0;
+  for (int i = 0; i < 3; ++i)
+    wide = wide && a.sk[i] * sizeof(T) % 16 == 0 && a.sv[i] * sizeof(T) % 16 == 0;
+  // pieces of 4 rows x 8 channels that a block may get
+  const int rows = a.L < g.page ? a.L : g.page;
+  const int most = ((rows + 2) / 4 + 1 < g.page / 4 ? (rows + 2) / 4 + 1 : g.page / 4) * (g.d / 8);
+  const int W = most <= 64 ? 1 : 4;
+  const int64_t groups = (items + 4 / W - 1) / (4 / W);
+  const unsigned blocks = (unsigned)(groups < kMaxBlocks ? groups : kMaxBlocks);
+  const int span = (rows + 30) / 16 * 16, ls = (span < g.page ? span : g.page) + 16;
+  const size_t lds = (size_t)(4 / W) * g.d * ls;  // at most 34 KB
+  if (W == 1)
+    k_cache8_append<T, 1, true><<<blocks, 256, lds, s>>>(a, k, v, slots, items, ls, wide);
+  else if (most <= 256)
+    k_cache8_append<T, 4, true><<<blocks, 256, lds, s>>>(a, k, v, slots, items, ls, wide);
+  else
+    k_cache8_append<T, 4, false><<<blocks, 256, lds, s>>>(a, k, v, slots, items, ls, wide);
   return hipGetLastError();
 }
 template hipError_t launch_cache8_append(const Cache8Append&, const float*, const float*, hipStream_t);

@@ -579,29 +579,54 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   }
 }
 
-// The sums of the splits of each column, in their order: D / 4 lanes per column.
+// The sums of the splits of each column: `share` groups of D / 4 lanes take them in turns, then the
+// groups' sums are added in their order.
 template <int D, class T>
 __global__ __launch_bounds__(256) void k_cache8_join(Cache8Attend a, T* __restrict__ out,
                                                      const float* __restrict__ part,
                                                      const float* __restrict__ part_ml,
-                                                     int64_t columns, int splits, int chunk) {
+                                                     int64_t columns, int splits, int chunk,
+                                                     int share) {
+  __shared__ float gm[256], gl[256];
+  __shared__ f32x4 go[256];
   const Cache8Geo& g = a.g;
-  const int64_t at = (int64_t)blockIdx.x * (256 / (D / 4)) + threadIdx.x / (D / 4);
-  if (at >= columns) return;
-  const int d0 = threadIdx.x % (D / 4) * 4, G = a.heads / g.heads;
+  constexpr int W = D / 4;
+  const int lanes = W * share, tid = threadIdx.x, sub = tid % lanes / W, d0 = tid % W * 4;
+  const int64_t at = (int64_t)blockIdx.x * (256 / lanes) + tid / lanes;
+  const int G = a.heads / g.heads;
   const int64_t per = (int64_t)a.L * G, prob = at / per, b = prob / g.heads;
   const int col = (int)(at - prob * per), i = col / G;
   const int h = (int)(prob - b * g.heads) * G + col - i * G;
-  if (a.n_rows && i >= a.n_rows[b]) return;
-  const int len = min(max(a.lens[b], 0), a.max_rows), live = min(splits, (len + chunk - 1) / chunk);
+  const bool on = at < columns && !(a.n_rows && i >= a.n_rows[b]);
   float m = -FLT_MAX, l = 0.f;
   f32x4 o = zero4();
-  for (int s = 0; s < live; ++s) m = fmaxf(m, part_ml[(at * splits + s) * 2]);
-  for (int s = 0; s < live; ++s) {
-    const float f = exp2_hw(part_ml[(at * splits + s) * 2] - m);
-    l = fmaf(part_ml[(at * splits + s) * 2 + 1], f, l);
-    o += *reinterpret_cast<const f32x4*>(part + (at * splits + s) * D + d0) * f;
+  if (on) {
+    const int len = min(max(a.lens[b], 0), a.max_rows), live = min(splits, (len + chunk - 1) / chunk);
+    for (int s = sub; s < live; s += share) m = fmaxf(m, part_ml[(at * splits + s) * 2]);
+    for (int s = sub; s < live; s += share) {
+      const float f = exp2_hw(part_ml[(at * splits + s) * 2] - m);
+      l = fmaf(part_ml[(at * splits + s) * 2 + 1], f, l);
+      o += *reinterpret_cast<const f32x4*>(part + (at * splits + s) * D + d0) * f;
+    }
   }
+  if (share > 1) {
+    gm[tid] = m;
+    gl[tid] = l;
+    go[tid] = o;
+    __syncthreads();
+    if (sub) return;
+    const float mine = m;
+    for (int s = 1; s < share; ++s) m = fmaxf(m, gm[tid + s * W]);
+    const float f0 = exp2_hw(mine - m);
+    l *= f0;
+    o *= f0;
+    for (int s = 1; s < share; ++s) {
+      const float f = exp2_hw(gm[tid + s * W] - m);
+      l = fmaf(gl[tid + s * W], f, l);
+      o += go[tid + s * W] * f;
+    }
+  }
+  if (!on) return;
   T* p = out + b * a.so[0] + i * a.so[1] + h * a.so[2] + d0;
   const float inv = l == 0.f ? 0.f : 1.0f / l;
 #pragma unroll
@@ -659,9 +684,11 @@ hipError_t go(const Cache8Attend& a, const Cut& c, const T* q, T* out, hipStream
           a, q, out, part, ml, p0, c.coltiles, c.splits, c.chunk, wide);
   }
   if (c.splits > 1) {
-    const int64_t columns = n / c.splits, per = 256 / (D / 4);
+    int share = 1;  // some eight splits to a group
+    while (share * 8 < c.splits && share < 256 / (D / 4)) share *= 2;
+    const int64_t columns = n / c.splits, per = 256 / (D / 4 * share);
     k_cache8_join<D, T><<<(unsigned)((columns + per - 1) / per), 256, 0, s>>>(
-        a, out, part, ml, columns, c.splits, c.chunk);
+        a, out, part, ml, columns, c.splits, c.chunk, share);
   }
   return hipGetLastError();
 }
