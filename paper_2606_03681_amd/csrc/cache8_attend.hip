@@ -17,10 +17,13 @@
 // order in which the lane reads 16 bytes of V^T.  Nothing moves between lanes, and codes go from memory
 // to registers without LDS.
 //
-// p is held as half with 2^14 in front, at most 2^15 with the reference at most 2 below the largest:
-// 2^-12 of each weight, and 2^-39 of the largest where half has no more bits.  bfloat16 would have
-// doubled the output's own rounding error.  Values are held with 2^7 in front: exact unless their block
-// is 2^22 below the largest, 2^-41 of that one's largest code then.  Float32 queries are three bfloat16
+// p is held as half with 2^11 in front: 2^-12 of each weight, and 2^-36 of the largest where half has no
+// more bits (bfloat16 would have doubled the output's own rounding error).  The reference is looked at
+// only where a lane's weights sum to more than half can hold, the first tile's among them, whose
+// reference is the lowest float: then it becomes the largest score, the sums are rescaled and the tile
+// weighed again.  With the largest score as reference 16 weights sum to at most 2^15, so that this is
+// rare, and other tiles need no maximum.  Values are held with 2^7 in front: exact unless their block is
+// 2^22 below the largest, 2^-41 of that one's largest code then.  Float32 queries are three bfloat16
 // parts (24 bits) and their weights two halves.
 //
 // Few columns (SPLIT): the four waves of a workgroup share the columns and take turns over the tiles;
@@ -40,8 +43,8 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int KT = 64;              // keys per tile
-constexpr float SLACK = 1.0f;       // ref may lag by this much
-constexpr int P_BIAS = 14, V_BIAS = 7;  // weights and values are held times 2 to these
+constexpr int P_BIAS = 11, V_BIAS = 7;  // weights and values are held times 2 to these
+constexpr float P_MOST = 61440.f;       // a lane's 16 weights may sum to this, and half holds each
 constexpr int V_GAP = 20;               // powers of two by which blocks of a product may differ
 
 __device__ __forceinline__ float exp2i(int e) {  // 2^e, e in [-126, 127]
@@ -288,30 +291,35 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
         for (int i = 0; i < 4; ++i)
           if (t0 + 16 * lg + 4 * t + i >= upto[qb] || !here) s[t][i] = -INFINITY;
     }
-    float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+    auto weights = [&]() {
+      const float off = (float)P_BIAS - ref[qb];
+      float sum[2] = {0.f, 0.f};
 #pragma unroll
-    for (int t = 1; t < 4; ++t) mx = fmaxf(mx, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
-    mx *= cs;
-    if (__any(mx > ref[qb] + SLACK)) {
-      const float now = fmaxf(ref[qb], rows4_max(mx)), corr = exp2_hw(ref[qb] - now);
+      for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const float p = exp2_hw(fmaf(s[2 * kc + j / 4][j % 4], cs, off));
+          sum[kc] += p;
+          const _Float16 h = (_Float16)p;
+          pf[0][kc][j] = h;
+          if constexpr (NP == 2) pf[1][kc][j] = (_Float16)(p - (float)h);
+        }
+      return sum[0] + sum[1];
+    };
+    float sum = weights();
+    if (__any(!(sum <= P_MOST))) {
+      float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
+#pragma unroll
+      for (int t = 1; t < 4; ++t)
+        mx = fmaxf(mx, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
+      const float now = fmaxf(ref[qb], rows4_max(mx * cs)), corr = exp2_hw(ref[qb] - now);
       ref[qb] = now;
       lsum[qb] *= corr;
 #pragma unroll
       for (int db = 0; db < DB; ++db) oacc[db][qb] *= corr;
+      sum = weights();
     }
-    const float off = (float)P_BIAS - ref[qb];
-    float sum[2] = {0.f, 0.f};
-#pragma unroll
-    for (int kc = 0; kc < 2; ++kc)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const float p = exp2_hw(fmaf(s[2 * kc + j / 4][j % 4], cs, off));
-        sum[kc] += p;
-        const _Float16 h = (_Float16)p;
-        pf[0][kc][j] = h;
-        if constexpr (NP == 2) pf[1][kc][j] = (_Float16)(p - (float)h);
-      }
-    lsum[qb] += sum[0] + sum[1];
+    lsum[qb] += sum;
   };
   auto compute = [&](Keys<D>& x, Values<D>& y, int t0, auto keys_read) {
     const int ek = power_byte(x.power & 0xff), ev = power_byte(x.power >> 8);
