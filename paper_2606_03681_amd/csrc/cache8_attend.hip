@@ -17,18 +17,18 @@
 // order in which the lane reads 16 bytes of V^T.  Nothing moves between lanes, and codes go from memory
 // to registers without LDS.
 //
-// p is held as half with 2^11 in front: 2^-12 of each weight, and 2^-36 of the largest where half has no
+// p is held as half with 2^8 in front: 2^-12 of each weight, and 2^-33 of the largest where half has no
 // more bits (bfloat16 would have doubled the output's own rounding error).  The reference is looked at
 // only where a lane's weights sum to more than half can hold, the first tile's among them, whose
 // reference is the lowest float: then it becomes the largest score, the sums are rescaled and the tile
-// weighed again.  With the largest score as reference 16 weights sum to at most 2^15, so that this is
-// rare, and other tiles need no maximum.  Values are held with 2^7 in front: exact unless their block is
+// weighed again.  With the largest score as reference 16 weights sum to at most 2^12, and a later score
+// may be up to 2^7 of it, so that this is rare, and other tiles need no maximum.  Values are held with 2^7 in front: exact unless their block is
 // 2^22 below the largest, 2^-41 of that one's largest code then.  Float32 queries are three bfloat16
 // parts (24 bits) and their weights two halves.
 //
 // Few columns (SPLIT): the four waves of a workgroup share the columns and take turns over the tiles;
 // many: each wave has columns of its own.  A tile's keys are read while the one before it is weighed
-// and summed, its values from then on, and the page after it is looked up.  Where the workgroups are too
+// and summed, its values from then on.  Where the workgroups are too
 // few the keys are split over more of them, and a second launch joins their sums.
 #include <float.h>
 
@@ -43,7 +43,7 @@ typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int KT = 64;              // keys per tile
-constexpr int P_BIAS = 11, V_BIAS = 7;  // weights and values are held times 2 to these
+constexpr int P_BIAS = 8, V_BIAS = 7;  // weights and values are held times 2 to these
 constexpr float P_MOST = 61440.f;       // a lane's 16 weights may sum to this, and half holds each
 constexpr int V_GAP = 20;               // powers of two by which blocks of a product may differ
 
@@ -123,7 +123,7 @@ constexpr int waves() { return D == 128 && QB == 2 ? 1 : 2; }
 template <int D, class T, int QB, bool SPLIT, bool UNI>
 __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void k_cache8_attend(Cache8Attend a, const T* __restrict__ q,
                                                        T* __restrict__ out, float* __restrict__ part,
-                                                       float* __restrict__ part_ml, int64_t prob0,
+                                                       float* __restrict__ part_ml, uint32_t prob0,
                                                        int coltiles, int splits, int chunk,
                                                        int wide) {
   constexpr int DB = D / 16, CH = KQ<D>::CH, KW = D / 16;  // KW: dwords of a key per lane
@@ -132,12 +132,11 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   typedef typename KQ<D>::frag QF;
   const Cache8Geo& g = a.g;
   const int lane = threadIdx.x & 63, wave = wave_id(), c = lane & 15, lg = lane >> 4;
-  const int ct = blockIdx.x % coltiles;
-  const int64_t rest = blockIdx.x / coltiles;
-  const int sp = (int)(rest % splits);
-  const int64_t prob = prob0 + rest / splits;
-  const int64_t b = prob / g.heads;
-  const int kh = (int)(prob - b * g.heads), G = a.heads / g.heads;
+  const uint32_t rest = blockIdx.x / (uint32_t)coltiles, pr = rest / (uint32_t)splits;
+  const int ct = blockIdx.x - rest * coltiles, sp = rest - pr * splits;
+  const uint32_t prob = prob0 + pr, bq = prob / (uint32_t)g.heads;  // below 2^31, as B L heads is
+  const int64_t b = bq;
+  const int kh = prob - bq * g.heads, G = a.heads / g.heads;
   const int rows = a.n_rows ? min(max(a.n_rows[b], 0), a.L) : a.L;
   const int len = min(max(a.lens[b], 0), a.max_rows);
   const int ncols = rows * G;
@@ -146,30 +145,45 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   const int k0 = sp * chunk;
   if (splits > 1 && k0 >= len) return;
 
-  // the columns' rows, and the keys that each sees
-  int64_t qrow[QB];
-  int upto[QB], lo = 0x7fffffff, hi = 0;
+  // the columns' rows and heads, and the keys that each sees
+  int row[QB], head[QB], upto[QB], lo = len, hi = len;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    const int col = min(col0 + qb * 16 + c, ncols - 1), i = col / G;
-    qrow[qb] = ((int64_t)i << 32) | (kh * G + col - i * G);
-    upto[qb] = a.causal ? min(max(len - rows + i + 1, 0), len) : len;
-    lo = min(lo, upto[qb]);
-    hi = max(hi, upto[qb]);
+    const int col = min(col0 + qb * 16 + c, ncols - 1);
+    row[qb] = (int)((uint32_t)col / (uint32_t)G);
+    head[qb] = kh * G + col - row[qb] * G;
+    upto[qb] = len;
   }
+  if (a.causal) {
+    lo = 0x7fffffff;
+    hi = 0;
 #pragma unroll
-  for (int o = 1; o < 16; o <<= 1) {
-    lo = min(lo, __shfl_xor(lo, o, 64));
-    hi = max(hi, __shfl_xor(hi, o, 64));
+    for (int qb = 0; qb < QB; ++qb) {
+      upto[qb] = min(max(len - rows + row[qb] + 1, 0), len);
+      lo = min(lo, upto[qb]);
+      hi = max(hi, upto[qb]);
+    }
+#pragma unroll
+    for (int o = 1; o < 16; o <<= 1) {
+      lo = min(lo, __shfl_xor(lo, o, 64));
+      hi = max(hi, __shfl_xor(hi, o, 64));
+    }
+    lo = __builtin_amdgcn_readfirstlane(lo);
+    hi = __builtin_amdgcn_readfirstlane(hi);
   }
-  lo = __builtin_amdgcn_readfirstlane(lo);
-  hi = __builtin_amdgcn_readfirstlane(hi);
 
-  QF qf[NQ][QB][CH];
+  // the queries' operands, in LDS at D >= 64, where registers are short
+  constexpr bool QLDS = D >= 64;
+  constexpr int QBYTES = QLDS ? NQ * QB * CH * 1024 : 0;  // of a wave
+  constexpr int OBYTES = SPLIT ? 4 * 16 * QB * (D + 4) * 4 : 0;
+  constexpr int LBYTES = 4 * QBYTES > OBYTES ? 4 * QBYTES : OBYTES;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[LBYTES > 0 ? LBYTES : 16];
+  QF qf[NQ][QB][CH];  // (dead behind the stores below where it is in LDS)
+  uint8_t* ql = lds + wave * QBYTES + lane * 16;
   const bool neg = a.scale_log2 < 0;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    const T* p = q + b * a.sq[0] + (qrow[qb] >> 32) * a.sq[1] + (int)qrow[qb] * a.sq[2] + lg * (D / 4);
+    const T* p = q + b * a.sq[0] + row[qb] * a.sq[1] + head[qb] * a.sq[2] + lg * (D / 4);
     uint16_t e[NQ][D / 4];
     if (wide) {
       constexpr int V = D / 4 * sizeof(T) / 8;  // 8-byte pieces
@@ -210,8 +224,14 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
         for (int j = 0; j < (int)sizeof(QF) / 2; ++j)
           f[j] = (uint16_t)(e[n][ch * 8 + j] ^ (neg ? 0x8000u : 0u));
         __builtin_memcpy(&qf[n][qb][ch], f, sizeof(QF));
+        if constexpr (QLDS)
+          *reinterpret_cast<QF*>(ql + ((n * QB + qb) * CH + ch) * 1024) = qf[n][qb][ch];
       }
   }
+  auto query_frag = [&](int n, int qb, int ch) {
+    if constexpr (QLDS) return *reinterpret_cast<const QF*>(ql + ((n * QB + qb) * CH + ch) * 1024);
+    return qf[n][qb][ch];
+  };
   const float scale = fabsf(a.scale_log2);
 
   const int kend = min(splits > 1 ? k0 + chunk : len, hi);
@@ -220,9 +240,25 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   const int64_t hd = (int64_t)g.heads * page * D;  // bytes of a page
   // the pages of the keys 16 (c / 4) .. and 16 lg .. of a tile (UNI: one page, the same in every lane)
   const int gk = UNI ? 0 : c >> 2, gv = UNI ? 0 : lg;
+  // The table's entries from ebase (a multiple of 64) on, one a lane, and the 64 after them: a tile's
+  // pages come from these registers, so that none waits for its page's number.
+  int ebase = -256, near = -1, far = -1;
+  auto entries = [&](int e0) { return cache8_page(g, b, min(e0 + lane, g.max_pages - 1)); };
+  auto look = [&](int t0) {  // before pid_of of tile t0
+    const int e = t0 >> shift;
+    if (e - ebase < 64) return;
+    if (e - ebase < 128) {
+      ebase += 64;
+      near = far;
+    } else {
+      ebase = e & ~63;
+      near = entries(ebase);
+    }
+    far = entries(ebase + 64);
+  };
   auto pid_of = [&](int t0, int grp) {
-    const int e = min((t0 + 16 * grp) >> shift, g.max_pages - 1);
-    return cache8_page(g, b, e);
+    const int e = ((t0 + 16 * grp) >> shift) - ebase;
+    return UNI ? __builtin_amdgcn_readlane(near, e) : __shfl(near, e, 64);
   };
   auto load_k = [&](Keys<D>& x, int t0, int pk, int pv) {
     x.here = pv >= 0;
@@ -283,6 +319,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
     return kf;
   };
   // Scores of block qb (in place) to its weights.
+  bool first = true;  // (then the reference says nothing yet)
   auto weigh = [&](f32x4* s, int qb, float cs, int t0, bool partial, bool here, f16x8 (*pf)[2]) {
     if (partial) {
 #pragma unroll
@@ -293,20 +330,21 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
     }
     auto weights = [&]() {
       const float off = (float)P_BIAS - ref[qb];
-      float sum[2] = {0.f, 0.f};
+      float sum[2];
 #pragma unroll
       for (int kc = 0; kc < 2; ++kc)
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float p = exp2_hw(fmaf(s[2 * kc + j / 4][j % 4], cs, off));
-          sum[kc] += p;
+          sum[kc] = j ? sum[kc] + p : p;
           const _Float16 h = (_Float16)p;
           pf[0][kc][j] = h;
           if constexpr (NP == 2) pf[1][kc][j] = (_Float16)(p - (float)h);
         }
       return sum[0] + sum[1];
     };
-    float sum = weights();
+    float sum = INFINITY;
+    if (!first) sum = weights();
     if (__any(!(sum <= P_MOST))) {
       float mx = fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3]));
 #pragma unroll
@@ -321,114 +359,66 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
     }
     lsum[qb] += sum;
   };
-  auto compute = [&](Keys<D>& x, Values<D>& y, int t0, auto keys_read) {
+  // Scores of a tile, weights, sums, of the keys of one group of lanes (only) or of all (-1).
+  // keys_read: called once the keys' registers are free.
+  auto compute = [&](Keys<D>& x, Values<D>& y, int t0, int only, auto keys_read) {
     const int ek = power_byte(x.power & 0xff), ev = power_byte(x.power >> 8);
-    const bool here = x.here;
+    const bool here = x.here && (UNI || only < 0 || lg == only);
     const float cs = fmaxf(scale * exp2i(ek - 127), 0x1p-126f);
     const bool partial = t0 + KT > lo || __any(!here);
-    f16x8 pf[QB][NP][2];
-    if constexpr (D <= 32) {
-      // one block of columns after another, the next one's products under way
-      QF kf[4][CH];
-#pragma unroll
-      for (int t = 0; t < 4; ++t)
-#pragma unroll
-        for (int ch = 0; ch < CH; ++ch) kf[t][ch] = key_frag(x, t, ch);
-      keys_read();
-      f32x4 s[2][4];
-      auto products = [&](f32x4* r, int qb) {
-#pragma unroll
-        for (int t = 0; t < 4; ++t) {
-          r[t] = zero4();
-#pragma unroll
-          for (int ch = 0; ch < CH; ++ch)
-#pragma unroll
-            for (int n = NQ - 1; n >= 0; --n) r[t] = KQ<D>::mma(kf[t][ch], qf[n][qb][ch], r[t]);
-        }
-      };
-      products(s[0], 0);
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) {
-        if (qb + 1 < QB) products(s[(qb + 1) & 1], qb + 1);
-        weigh(s[qb & 1], qb, cs, t0, partial, here, pf[qb]);
-      }
-    } else {
-      f32x4 s[QB][4];
-#pragma unroll
-      for (int t = 0; t < 4; ++t) {
-#pragma unroll
-        for (int qb = 0; qb < QB; ++qb) s[qb][t] = zero4();
-#pragma unroll
-        for (int ch = 0; ch < CH; ++ch) {
-          const QF kf = key_frag(x, t, ch);
-#pragma unroll
-          for (int n = NQ - 1; n >= 0; --n)
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) s[qb][t] = KQ<D>::mma(kf, qf[n][qb][ch], s[qb][t]);
-        }
-      }
-      keys_read();
-#pragma unroll
-      for (int qb = 0; qb < QB; ++qb) weigh(s[qb], qb, cs, t0, partial, here, pf[qb]);
-    }
-    uint32_t nans = 0;
-    bool apart = false;
-    // the largest power among the blocks that any column sees; others' bytes may be anything
     int top = ev;
-    if (partial) {
-      const bool seen = here && t0 + 16 * lg < hi;
-      top = seen ? ev : 0;
+    // What values say before the weights are there: the largest power among the blocks that any column
+    // sees (others' bytes may be anything), and where the NaN codes are.
+    auto look_at_values = [&]() {
+      if (partial) {
+        const bool seen = here && t0 + 16 * lg < hi;
+        top = seen ? ev : 0;
+        uint32_t nans = 0;
 #pragma unroll
-      for (int db = 0; db < DB; ++db)
-        nans |= nan_bytes(y.v[db].x) | nan_bytes(y.v[db].y) | nan_bytes(y.v[db].z) | nan_bytes(y.v[db].w);
-      if constexpr (!UNI) {
-        int low = seen ? ev : 255, high = top;
-        low = min(low, __shfl_xor(low, 16, 64));
-        low = min(low, __shfl_xor(low, 32, 64));
-        high = max(high, __shfl_xor(high, 16, 64));
-        high = max(high, __shfl_xor(high, 32, 64));
-        apart = __builtin_amdgcn_readfirstlane(high - low) > V_GAP;
-      }
-      if (__any(nans != 0)) {
-        // NaN codes (or what lies behind the last key): out of the products, whose weight for them
-        // may be 0, and NaN in the sums of the columns that see them
+        for (int db = 0; db < DB; ++db)
+          nans |= nan_bytes(y.v[db].x) | nan_bytes(y.v[db].y) | nan_bytes(y.v[db].z) |
+                  nan_bytes(y.v[db].w);
+        if (__any(nans != 0)) {
+          // NaN codes (or what lies behind the last key): out of the products, whose weight for them
+          // may be 0, and NaN in the sums of the columns that see them
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          uint32_t* w = reinterpret_cast<uint32_t*>(&y.v[db]);
-          f32x4 cnt[QB];
+          for (int db = 0; db < DB; ++db) {
+            uint32_t* w = reinterpret_cast<uint32_t*>(&y.v[db]);
+            f32x4 cnt[QB];
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) cnt[qb] = zero4();
+            for (int qb = 0; qb < QB; ++qb) cnt[qb] = zero4();
 #pragma unroll
-          for (int kc = 0; kc < 2; ++kc) {
-            f16x8 is;
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-              is[j] = (_Float16)(float)(nan_bytes(w[2 * kc + j / 4]) >> (8 * (j % 4) + 7) & 1);
-#pragma unroll
-            for (int qb = 0; qb < QB; ++qb) {
-              f16x8 sees;
+            for (int kc = 0; kc < 2; ++kc) {
+              f16x8 is;
 #pragma unroll
               for (int j = 0; j < 8; ++j)
-                sees[j] = (_Float16)(here && t0 + 16 * lg + 8 * kc + j < upto[qb] ? 1.f : 0.f);
-              cnt[qb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(is, sees, cnt[qb], 0, 0, 0);
+                is[j] = (_Float16)(float)(nan_bytes(w[2 * kc + j / 4]) >> (8 * (j % 4) + 7) & 1);
+#pragma unroll
+              for (int qb = 0; qb < QB; ++qb) {
+                f16x8 sees;
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                  sees[j] = (_Float16)(here && t0 + 16 * lg + 8 * kc + j < upto[qb] ? 1.f : 0.f);
+                cnt[qb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(is, sees, cnt[qb], 0, 0, 0);
+              }
             }
-          }
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb)
+            for (int qb = 0; qb < QB; ++qb)
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
-              if (cnt[qb][i] > 0.f) oacc[db][qb][i] = __builtin_nanf("");
+              for (int i = 0; i < 4; ++i)
+                if (cnt[qb][i] > 0.f) oacc[db][qb][i] = __builtin_nanf("");
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            const uint32_t m = nan_bytes(w[j]);
-            w[j] &= ~(m | (m - (m >> 7)));  // 0x80 to 0xff
+            for (int j = 0; j < 4; ++j) {
+              const uint32_t m = nan_bytes(w[j]);
+              w[j] &= ~(m | (m - (m >> 7)));  // 0x80 to 0xff
+            }
           }
         }
       }
-    }
-    // only: the group of lanes whose keys count, -1: all
-    auto sum = [&](int only) {
-      int now = only < 0 || lg == only ? top : 0;
+    };
+    // The unit for this tile, and the factor of this lane's values.
+    auto raise = [&]() {
+      int now = top;
       if constexpr (UNI) {
         now = __builtin_amdgcn_readfirstlane(now);
       } else {
@@ -444,58 +434,139 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
         unit = now;
       }
       // (a block that no column sees: any power will do)
-      const float two = exp2i(min(ev - unit, 0) + V_BIAS);
+      return exp2i(min(ev - unit, 0) + V_BIAS);
+    };
+    auto value_frag = [&](int db, int kc, float two) {
+      return kc ? codes_f16(y.v[db].z, y.v[db].w, two) : codes_f16(y.v[db].x, y.v[db].y, two);
+    };
+    auto add = [&](const f16x8& vf, const f16x8 (*pf)[2], int db, int kc, int qb) {
 #pragma unroll
-      for (int kc = 0; kc < 2; ++kc) {
-        f16x8 pw[QB][NP];
+      for (int n = NP - 1; n >= 0; --n)
+        oacc[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pf[n][kc], oacc[db][qb], 0, 0, 0);
+    };
+    if constexpr (D <= 32) {
+      // one block of columns after another, the next one's products under way
+      look_at_values();
+      QF kf[4][CH];
 #pragma unroll
-        for (int qb = 0; qb < QB; ++qb)
+      for (int t = 0; t < 4; ++t)
 #pragma unroll
-          for (int n = 0; n < NP; ++n) {
-            pw[qb][n] = pf[qb][n][kc];
-            if (only >= 0 && lg != only) pw[qb][n] = f16x8{};
-          }
+        for (int ch = 0; ch < CH; ++ch) kf[t][ch] = key_frag(x, t, ch);
+      keys_read();
+      auto products = [&](f32x4* r, int qb) {
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const f16x8 vf = kc ? codes_f16(y.v[db].z, y.v[db].w, two)
-                              : codes_f16(y.v[db].x, y.v[db].y, two);
+        for (int t = 0; t < 4; ++t) {
+          r[t] = zero4();
 #pragma unroll
-          for (int n = NP - 1; n >= 0; --n)
+          for (int ch = 0; ch < CH; ++ch)
 #pragma unroll
-            for (int qb = 0; qb < QB; ++qb)
-              oacc[db][qb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vf, pw[qb][n], oacc[db][qb], 0, 0, 0);
+            for (int n = NQ - 1; n >= 0; --n) r[t] = KQ<D>::mma(kf[t][ch], query_frag(n, qb, ch), r[t]);
+        }
+      };
+      const float two = raise();
+      f16x8 vf[DB][2];
+#pragma unroll
+      for (int db = 0; db < DB; ++db)
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc) vf[db][kc] = value_frag(db, kc, two);
+      f32x4 s[2][4];
+      products(s[0], 0);
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) {
+        f16x8 pf[NP][2];
+        if (qb + 1 < QB) products(s[(qb + 1) & 1], qb + 1);
+        weigh(s[qb & 1], qb, cs, t0, partial, here, pf);
+#pragma unroll
+        for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+          for (int db = 0; db < DB; ++db) add(vf[db][kc], pf, db, kc, qb);
+      }
+    } else {
+      f16x8 pf[QB][NP][2];
+      f32x4 s[QB][4];
+      asm volatile("" ::: "memory");  // the queries stay in LDS
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) s[qb][t] = zero4();
+#pragma unroll
+      for (int ch = 0; ch < CH; ++ch) {
+        QF f[NQ][QB];
+#pragma unroll
+        for (int n = 0; n < NQ; ++n)
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) f[n][qb] = query_frag(n, qb, ch);
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const QF kf = key_frag(x, t, ch);
+#pragma unroll
+          for (int n = NQ - 1; n >= 0; --n)
+#pragma unroll
+            for (int qb = 0; qb < QB; ++qb) s[qb][t] = KQ<D>::mma(kf, f[n][qb], s[qb][t]);
         }
       }
-    };
-    if (UNI || !apart) {
-      sum(-1);
-    } else {
-      // a block far larger than another, and columns that may see the other alone: block by block
-      for (int grp = 0; grp < 4; ++grp) sum(grp);
+      keys_read();
+#pragma unroll
+      for (int qb = 0; qb < QB; ++qb) weigh(s[qb], qb, cs, t0, partial, here, pf[qb]);
+      look_at_values();
+      const float two = raise();
+#pragma unroll
+      for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+        for (int db = 0; db < DB; ++db) {
+          const f16x8 vf = value_frag(db, kc, two);
+#pragma unroll
+          for (int qb = 0; qb < QB; ++qb) add(vf, pf[qb], db, kc, qb);
+        }
     }
+    first = false;
+  };
+  // Whether a tile has blocks far apart and columns that may see the smaller one alone.
+  auto apart = [&](const Keys<D>& x, int t0) {
+    if (UNI || t0 + KT <= lo) return false;
+    const bool seen = x.here && t0 + 16 * lg < hi;
+    const int ev = power_byte(x.power >> 8);
+    int low = seen ? ev : 255, high = seen ? ev : 0;
+#pragma unroll
+    for (int o = 16; o < 64; o <<= 1) {
+      low = min(low, __shfl_xor(low, o, 64));
+      high = max(high, __shfl_xor(high, o, 64));
+    }
+    return __builtin_amdgcn_readfirstlane(high - low) > V_GAP;
   };
 
   int t0 = k0 + (SPLIT ? wave * KT : 0);
   if (t0 < kend) {
     Keys<D> x;
     Values<D> y;
+    look(t0);
     int pk = pid_of(t0, gk), pv = UNI ? pk : pid_of(t0, gv);
-    auto next_page = [&](int t) {
-      if (t < kend) {
-        pk = pid_of(t, gk);
-        pv = UNI ? pk : pid_of(t, gv);
-      }
-    };
     load_k(x, t0, pk, pv);
     load_v(y, t0, pv);
-    next_page(t0 + STEP);
     for (; t0 < kend; t0 += STEP) {
       const bool more = t0 + STEP < kend;
-      compute(x, y, t0, [&] {
-        if (more) load_k(x, t0 + STEP, pk, pv);
-      });
-      if (more) load_v(y, t0 + STEP, pv);
-      next_page(t0 + 2 * STEP);
+      Values<D> y2;
+      int only = -1, last = -1;
+      if (apart(x, t0)) only = 0, last = 3;
+      for (;; ++only) {
+        if (only >= 0) {  // one block of the tile at a time, without the others' values
+          load_v(y, t0, pv);
+          if (lg != only) y = Values<D>{};
+        }
+        compute(x, y, t0, only, [&] {
+          if (!more || only != last) return;
+          look(t0 + STEP);
+          pk = pid_of(t0 + STEP, gk);
+          pv = UNI ? pk : pid_of(t0 + STEP, gv);
+          load_k(x, t0 + STEP, pk, pv);
+          if constexpr (D <= 32) load_v(y2, t0 + STEP, pv);
+        });
+        if (UNI || only == last) break;
+      }
+      if constexpr (D <= 32)
+        y = y2;
+      else if (more)
+        load_v(y, t0 + STEP, pv);
     }
   }
 
@@ -510,7 +581,8 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   if constexpr (SPLIT) {
     // the four waves' sums, in LDS: wave w's of column k
     __shared__ float ml[4][16 * QB][2];
-    __shared__ __attribute__((aligned(16))) float ow[4][16 * QB][D + 4];
+    float(*ow)[16 * QB][D + 4] = reinterpret_cast<float(*)[16 * QB][D + 4]>(lds);
+    if constexpr (QLDS) __syncthreads();  // every wave has done with its queries
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
       const int k = qb * 16 + c;
@@ -535,17 +607,17 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
       }
       const int i = col / G, h = kh * G + col - i * G;
       if (splits > 1) {
-        const int64_t at = (prob * a.L * G + col) * splits + sp;
+        const int64_t at = ((int64_t)prob * a.L * G + col) * splits + sp;
         *reinterpret_cast<f32x4*>(part + at * D + d0) = o;
         if (d0 == 0) part_ml[at * 2] = m, part_ml[at * 2 + 1] = l;
       } else {
         T* p = out + b * a.so[0] + i * a.so[1] + h * a.so[2] + d0;
-        const float inv = l == 0.f ? 0.f : 1.0f / l;
+        const float inv = l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l);
 #pragma unroll
         for (int j = 0; j < 4; ++j) st(p + j, l == 0.f ? 0.f : o[j] * inv);
         if (a.lse && d0 == 0)
           a.lse[(b * a.L + i) * a.heads + h] =
-              l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+              l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
       }
     }
   } else {
@@ -553,10 +625,10 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
     for (int qb = 0; qb < QB; ++qb) {
       const int col = col0 + qb * 16 + c;
       if (col >= ncols) continue;
-      const int i = (int)(qrow[qb] >> 32), h = (int)qrow[qb];
+      const int i = row[qb], h = head[qb];
       const float l = lsum[qb];
       if (splits > 1) {
-        const int64_t at = (prob * a.L * G + col) * splits + sp;
+        const int64_t at = ((int64_t)prob * a.L * G + col) * splits + sp;
 #pragma unroll
         for (int db = 0; db < DB; ++db)
           *reinterpret_cast<f32x4*>(part + at * D + db * 16 + lg * 4) = oacc[db][qb];
@@ -564,7 +636,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
         continue;
       }
       T* p = out + b * a.so[0] + i * a.so[1] + h * a.so[2] + lg * 4;
-      const float inv = l == 0.f ? 0.f : 1.0f / l;
+      const float inv = l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l);
 #pragma unroll
       for (int db = 0; db < DB; ++db) {
         float y[4];
@@ -582,7 +654,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
       }
       if (a.lse && lg == 0)
         a.lse[(b * a.L + i) * a.heads + h] =
-            l == 0.f ? -INFINITY : (ref[qb] + log2f(l)) * 0.69314718055994531f;
+            l == 0.f ? -INFINITY : (ref[qb] + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
     }
   }
 }
@@ -636,11 +708,11 @@ __global__ __launch_bounds__(256) void k_cache8_join(Cache8Attend a, T* __restri
   }
   if (!on) return;
   T* p = out + b * a.so[0] + i * a.so[1] + h * a.so[2] + d0;
-  const float inv = l == 0.f ? 0.f : 1.0f / l;
+  const float inv = l == 0.f ? 0.f : __builtin_amdgcn_rcpf(l);
 #pragma unroll
   for (int j = 0; j < 4; ++j) st(p + j, l == 0.f ? 0.f : o[j] * inv);
   if (a.lse && d0 == 0)
-    a.lse[(b * a.L + i) * a.heads + h] = l == 0.f ? -INFINITY : (m + log2f(l)) * 0.69314718055994531f;
+    a.lse[(b * a.L + i) * a.heads + h] = l == 0.f ? -INFINITY : (m + __builtin_amdgcn_logf(l)) * 0.69314718055994531f;
 }
 
 // How a call is cut: 16 QB columns per wave, the waves of a workgroup on the same columns or not, and
@@ -686,10 +758,10 @@ hipError_t go(const Cache8Attend& a, const Cut& c, const T* q, T* out, hipStream
     const unsigned blocks = (unsigned)((probs - p0 < most ? probs - p0 : most) * each);
     if (a.g.page >= KT)
       k_cache8_attend<D, T, QB, SPLIT, true><<<blocks, 256, 0, s>>>(
-          a, q, out, part, ml, p0, c.coltiles, c.splits, c.chunk, wide);
+          a, q, out, part, ml, (uint32_t)p0, c.coltiles, c.splits, c.chunk, wide);
     else
       k_cache8_attend<D, T, QB, SPLIT, false><<<blocks, 256, 0, s>>>(
-          a, q, out, part, ml, p0, c.coltiles, c.splits, c.chunk, wide);
+          a, q, out, part, ml, (uint32_t)p0, c.coltiles, c.splits, c.chunk, wide);
   }
   if (c.splits > 1) {
     int share = 1;  // some eight splits to a group
