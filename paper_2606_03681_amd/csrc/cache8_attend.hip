@@ -118,7 +118,7 @@ struct Values {
 
 // Waves per SIMD that the registers of a kernel leave room for.
 template <int D, bool F32, int QB, bool SPLIT>
-constexpr int waves() { return D == 128 && QB == 2 ? 1 : 2; }
+constexpr int waves() { return D <= 32 && QB == 4 ? 3 : D == 128 && QB == 2 ? 1 : 2; }
 
 template <int D, class T, int QB, bool SPLIT, bool UNI>
 __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void k_cache8_attend(Cache8Attend a, const T* __restrict__ q,
@@ -145,21 +145,17 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   const int k0 = sp * chunk;
   if (splits > 1 && k0 >= len) return;
 
-  // the columns' rows and heads, and the keys that each sees
-  int row[QB], head[QB], upto[QB], lo = len, hi = len;
+  // the keys that each column sees
+  auto row_of = [&](int col) { return (int)((uint32_t)col / (uint32_t)G); };
+  int upto[QB], lo = len, hi = len;
 #pragma unroll
-  for (int qb = 0; qb < QB; ++qb) {
-    const int col = min(col0 + qb * 16 + c, ncols - 1);
-    row[qb] = (int)((uint32_t)col / (uint32_t)G);
-    head[qb] = kh * G + col - row[qb] * G;
-    upto[qb] = len;
-  }
+  for (int qb = 0; qb < QB; ++qb) upto[qb] = len;
   if (a.causal) {
     lo = 0x7fffffff;
     hi = 0;
 #pragma unroll
     for (int qb = 0; qb < QB; ++qb) {
-      upto[qb] = min(max(len - rows + row[qb] + 1, 0), len);
+      upto[qb] = min(max(len - rows + row_of(min(col0 + qb * 16 + c, ncols - 1)) + 1, 0), len);
       lo = min(lo, upto[qb]);
       hi = max(hi, upto[qb]);
     }
@@ -173,7 +169,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   }
 
   // the queries' operands, in LDS at D >= 64, where registers are short
-  constexpr bool QLDS = D >= 64;
+  constexpr bool QLDS = D >= 64 || (D == 32 && QB == 4);
   constexpr int QBYTES = QLDS ? NQ * QB * CH * 1024 : 0;  // of a wave
   constexpr int OBYTES = SPLIT ? 4 * 16 * QB * (D + 4) * 4 : 0;
   constexpr int LBYTES = 4 * QBYTES > OBYTES ? 4 * QBYTES : OBYTES;
@@ -183,7 +179,8 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   const bool neg = a.scale_log2 < 0;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    const T* p = q + b * a.sq[0] + row[qb] * a.sq[1] + head[qb] * a.sq[2] + lg * (D / 4);
+    const int col = min(col0 + qb * 16 + c, ncols - 1), i = row_of(col), h = kh * G + col - i * G;
+    const T* p = q + b * a.sq[0] + i * a.sq[1] + h * a.sq[2] + lg * (D / 4);
     uint16_t e[NQ][D / 4];
     if (wide) {
       constexpr int V = D / 4 * sizeof(T) / 8;  // 8-byte pieces
@@ -350,18 +347,21 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
 #pragma unroll
       for (int t = 1; t < 4; ++t)
         mx = fmaxf(mx, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
-      const float now = fmaxf(ref[qb], rows4_max(mx * cs)), corr = exp2_hw(ref[qb] - now);
-      ref[qb] = now;
-      lsum[qb] *= corr;
+      const float now = fmaxf(ref[qb], rows4_max(mx * cs));
+      if (!first) {
+        const float corr = exp2_hw(ref[qb] - now);
+        lsum[qb] *= corr;
 #pragma unroll
-      for (int db = 0; db < DB; ++db) oacc[db][qb] *= corr;
+        for (int db = 0; db < DB; ++db) oacc[db][qb] *= corr;
+      }
+      ref[qb] = now;
       sum = weights();
     }
     lsum[qb] += sum;
   };
   // Scores of a tile, weights, sums, of the keys of one group of lanes (only) or of all (-1).
-  // keys_read: called once the keys' registers are free.
-  auto compute = [&](Keys<D>& x, Values<D>& y, int t0, int only, auto keys_read) {
+  // codes_read: called once the registers of the keys (and, at D <= 32, of the values) are free.
+  auto compute = [&](Keys<D>& x, Values<D>& y, int t0, int only, auto codes_read) {
     const int ek = power_byte(x.power & 0xff), ev = power_byte(x.power >> 8);
     const bool here = x.here && (UNI || only < 0 || lg == only);
     const float cs = fmaxf(scale * exp2i(ek - 127), 0x1p-126f);
@@ -447,12 +447,12 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
     if constexpr (D <= 32) {
       // one block of columns after another, the next one's products under way
       look_at_values();
+      if constexpr (QLDS) asm volatile("" ::: "memory");  // the queries stay in LDS
       QF kf[4][CH];
 #pragma unroll
       for (int t = 0; t < 4; ++t)
 #pragma unroll
         for (int ch = 0; ch < CH; ++ch) kf[t][ch] = key_frag(x, t, ch);
-      keys_read();
       auto products = [&](f32x4* r, int qb) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
@@ -469,13 +469,13 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
       for (int db = 0; db < DB; ++db)
 #pragma unroll
         for (int kc = 0; kc < 2; ++kc) vf[db][kc] = value_frag(db, kc, two);
-      f32x4 s[2][4];
-      products(s[0], 0);
+      codes_read();
+      f32x4 s[4];
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) {
         f16x8 pf[NP][2];
-        if (qb + 1 < QB) products(s[(qb + 1) & 1], qb + 1);
-        weigh(s[qb & 1], qb, cs, t0, partial, here, pf);
+        products(s, qb);
+        weigh(s, qb, cs, t0, partial, here, pf);
 #pragma unroll
         for (int kc = 0; kc < 2; ++kc)
 #pragma unroll
@@ -505,7 +505,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
             for (int qb = 0; qb < QB; ++qb) s[qb][t] = KQ<D>::mma(kf, f[n][qb], s[qb][t]);
         }
       }
-      keys_read();
+      codes_read();
 #pragma unroll
       for (int qb = 0; qb < QB; ++qb) weigh(s[qb], qb, cs, t0, partial, here, pf[qb]);
       look_at_values();
@@ -542,10 +542,12 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
     look(t0);
     int pk = pid_of(t0, gk), pv = UNI ? pk : pid_of(t0, gv);
     load_k(x, t0, pk, pv);
+    // (in this order, as in the loop: a wait for the keys must not be one for the values)
+    __builtin_amdgcn_sched_barrier(0);
     load_v(y, t0, pv);
+    __builtin_amdgcn_sched_barrier(0);
     for (; t0 < kend; t0 += STEP) {
       const bool more = t0 + STEP < kend;
-      Values<D> y2;
       int only = -1, last = -1;
       if (apart(x, t0)) only = 0, last = 3;
       for (;; ++only) {
@@ -559,14 +561,13 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
           pk = pid_of(t0 + STEP, gk);
           pv = UNI ? pk : pid_of(t0 + STEP, gv);
           load_k(x, t0 + STEP, pk, pv);
-          if constexpr (D <= 32) load_v(y2, t0 + STEP, pv);
+          if constexpr (D <= 32) load_v(y, t0 + STEP, pv);
         });
         if (UNI || only == last) break;
       }
-      if constexpr (D <= 32)
-        y = y2;
-      else if (more)
-        load_v(y, t0 + STEP, pv);
+      if constexpr (D > 32) {
+        if (more) load_v(y, t0 + STEP, pv);
+      }
     }
   }
 
@@ -625,7 +626,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
     for (int qb = 0; qb < QB; ++qb) {
       const int col = col0 + qb * 16 + c;
       if (col >= ncols) continue;
-      const int i = row[qb], h = head[qb];
+      const int i = row_of(col), h = kh * G + col - i * G;
       const float l = lsum[qb];
       if (splits > 1) {
         const int64_t at = ((int64_t)prob * a.L * G + col) * splits + sp;
@@ -726,7 +727,7 @@ Cut cut_of(const Cache8Attend& a, bool f32) {
   Cut c;
   const int64_t cols = (int64_t)a.L * (a.heads / a.g.heads), probs = (int64_t)a.B * a.g.heads;
   c.split = cols <= 32;
-  c.qb = c.split ? (cols <= 16 ? 1 : 2) : (f32 ? 1 : a.g.d <= 32 ? 4 : 2);
+  c.qb = c.split ? (cols <= 16 ? 1 : 2) : (f32 ? 1 : a.g.d <= 32 ? 4 : a.g.d == 128 ? 1 : 2);
   const int per = 16 * c.qb * (c.split ? 1 : 4);
   c.coltiles = (int)((cols + per - 1) / per);
   const int64_t blocks = probs * c.coltiles, want = 2048;
@@ -778,7 +779,7 @@ hipError_t go_d(const Cache8Attend& a, const T* q, T* out, hipStream_t s) {
   const Cut c = cut_of(a, sizeof(T) == 4);
   if (c.split)
     return c.qb == 1 ? go<D, T, 1, true>(a, c, q, out, s) : go<D, T, 2, true>(a, c, q, out, s);
-  return go<D, T, sizeof(T) == 4 ? 1 : D <= 32 ? 4 : 2, false>(a, c, q, out, s);
+  return go<D, T, sizeof(T) == 4 ? 1 : D <= 32 ? 4 : D == 128 ? 1 : 2, false>(a, c, q, out, s);
 }
 
 }  // namespace
