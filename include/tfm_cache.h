@@ -108,6 +108,32 @@ int tfm_cache8_attend(const tfm_cache8* c, const tfm_cache8_query* a, const void
                       const void* pool, size_t pool_bytes, void* out, float* lse, void* workspace,
                       size_t workspace_bytes, void* stream);
 
+/* ---- forward-only layer calls ---------------------------------------------------------------------
+ * tfm_layer_fwd_context and tfm_layer_fwd_query with the item axis' keys and values kept in 8 bits:
+ *
+ *   tfm_layer_fwd_context8  the context call (the same Y and kv_cache), after which the train rows'
+ *       keys and values are appended to cache8.  kv_cache is scratch here (tfm_infer_cache_bytes of
+ *       the context's dims): one serves every layer of a stack.
+ *   tfm_layer_fwd_query8    the query call against cache8.  Each query row's answer depends on itself
+ *       and the context alone, up to the order of sums, which goes by dims and context_rows.
+ *
+ * cache8 (tfm_infer_cache8_bytes of the context's dims, opaque layout) is a pool of pages of 64 rows
+ * with a power of two for each page and head: half the bfloat16 cache's bytes, three bits of fraction.
+ * Limits and conditions are those of the two calls; tfm_infer8_workspace_bytes is the scratch of
+ * query8 (dims->R: the query rows), tfm_infer_workspace_bytes that of context8. */
+size_t tfm_infer_cache8_bytes(const tfm_dims* dims);
+size_t tfm_infer8_workspace_bytes(const tfm_dims* dims, int32_t context_rows);
+
+int tfm_layer_fwd_context8(const tfm_dims* dims, const int32_t* n_train, const uint8_t* cell_mask,
+                           const void* X, const float* params, void* Y, void* kv_cache,
+                           size_t cache_bytes, void* cache8, size_t cache8_bytes, void* workspace,
+                           size_t workspace_bytes, void* stream);
+
+int tfm_layer_fwd_query8(const tfm_dims* dims, int32_t context_rows, const int32_t* n_train,
+                         const uint8_t* cell_mask, const void* X, const float* params,
+                         const void* cache8, size_t cache8_bytes, void* Y, void* workspace,
+                         size_t workspace_bytes, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -33,10 +33,32 @@ struct Cache8Append {
 template <class T>
 hipError_t launch_cache8_append(const Cache8Append& a, const T* k, const T* v, hipStream_t s);
 
+// A pool of n_pages pages at `at`: keys, values, powers.
+inline Cache8Geo cache8_geo(int heads, int d, int page, int n_pages, void* at, int max_pages,
+                            const int32_t* pages) {
+  Cache8Geo g;
+  g.heads = heads; g.d = d; g.page = page;
+  g.shift = 31 - __builtin_clz((unsigned)page);
+  g.n_pages = n_pages; g.max_pages = max_pages;
+  g.keys = g.values = g.powers = nullptr;
+  if (at) {
+    const size_t half = (size_t)n_pages * heads * page * d;
+    g.keys = (uint8_t*)at;
+    g.values = g.keys + half;
+    g.powers = g.values + half;
+  }
+  g.pages = pages;
+  return g;
+}
+inline size_t cache8_pool_bytes(int heads, int d, int page, int64_t n_pages) {
+  return (size_t)n_pages * heads * (2 * (size_t)page * d + 2);
+}
+
 struct Cache8Attend {
   Cache8Geo g;
   int32_t B, L, heads, causal;
   int32_t max_rows;          // of a sequence: the table's room, or less by the caller's word
+  int32_t plan_B, plan_rows; // B and max_rows by which the work is cut (not less than these two)
   float scale_log2;          // the scores' factor, with log2(e)
   int64_t sq[3], so[3];
   const int32_t *lens, *n_rows;  // n_rows nullable

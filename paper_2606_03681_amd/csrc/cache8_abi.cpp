@@ -44,11 +44,8 @@ size_t elem(int32_t d) { return d == TFM_BF16 ? 2 : 4; }
     tfm::prof_end(st);               \
   } while (0)
 
-size_t pool_half(const tfm_cache8* c) {
-  return (size_t)c->n_pages * c->heads * c->page * c->d;
-}
 size_t pool_size(const tfm_cache8* c) {
-  return 2 * pool_half(c) + (size_t)2 * c->n_pages * c->heads;
+  return tfm::cache8_pool_bytes(c->heads, c->d, c->page, c->n_pages);
 }
 
 int pool_check(const tfm_cache8* c) {
@@ -107,18 +104,7 @@ bool overlap(const void* p, double bytes, const void* q, double more) {
 }
 
 tfm::Cache8Geo geo_of(const tfm_cache8* c, void* pool, int32_t max_pages, const int32_t* pages) {
-  tfm::Cache8Geo g;
-  g.heads = c->heads; g.d = c->d; g.page = c->page;
-  g.shift = 31 - __builtin_clz((unsigned)c->page);
-  g.n_pages = c->n_pages; g.max_pages = max_pages;
-  g.keys = g.values = g.powers = nullptr;
-  if (pool) {
-    g.keys = (uint8_t*)pool;
-    g.values = g.keys + pool_half(c);
-    g.powers = g.values + pool_half(c);
-  }
-  g.pages = pages;
-  return g;
+  return tfm::cache8_geo(c->heads, c->d, c->page, c->n_pages, pool, max_pages, pages);
 }
 
 int pool_given(const tfm_cache8* c, const void* pool, size_t bytes) {
@@ -164,6 +150,7 @@ int query_check(const tfm_cache8* c, const tfm_cache8_query* a, tfm::Cache8Atten
   t.B = a->B; t.L = a->L; t.heads = a->heads; t.causal = a->causal != 0;
   const int64_t room = (int64_t)a->max_pages * c->page;
   t.max_rows = (int32_t)(a->max_len > 0 && a->max_len < room ? a->max_len : room);
+  t.plan_B = t.B; t.plan_rows = t.max_rows;
   t.scale_log2 = (float)(a->scale * 1.4426950408889634);
   for (int i = 0; i < 3; ++i) t.sq[i] = a->stride_q[i], t.so[i] = a->stride_out[i];
   return TFM_OK;

@@ -725,7 +725,8 @@ struct Cut {
 
 Cut cut_of(const Cache8Attend& a, bool f32) {
   Cut c;
-  const int64_t cols = (int64_t)a.L * (a.heads / a.g.heads), probs = (int64_t)a.B * a.g.heads;
+  const int64_t cols = (int64_t)a.L * (a.heads / a.g.heads), probs = (int64_t)a.plan_B * a.g.heads;
+  const int64_t keys = a.plan_rows;
   c.split = cols <= 32;
   c.qb = c.split ? (cols <= 16 ? 1 : 2) : (f32 ? 1 : a.g.d <= 32 ? 4 : a.g.d == 128 ? 1 : 2);
   const int per = 16 * c.qb * (c.split ? 1 : 4);
@@ -733,17 +734,18 @@ Cut cut_of(const Cache8Attend& a, bool f32) {
   const int64_t blocks = probs * c.coltiles, want = 2048;
   const int least = c.split ? 512 : 1024;  // keys worth a workgroup of their own
   int64_t s = blocks > 0 ? (want + blocks - 1) / blocks : 1;
-  s = s < (a.max_rows + least - 1) / least ? s : (a.max_rows + least - 1) / least;
+  s = s < (keys + least - 1) / least ? s : (keys + least - 1) / least;
   if (s < 1) s = 1;
-  c.chunk = (int)((((int64_t)a.max_rows + s - 1) / s + 255) / 256 * 256);
+  c.chunk = (int)(((keys + s - 1) / s + 255) / 256 * 256);
   if (c.chunk < 256) c.chunk = 256;
-  c.splits = (int)(((int64_t)a.max_rows + c.chunk - 1) / c.chunk);
+  c.splits = (int)((keys + c.chunk - 1) / c.chunk);
   if (c.splits < 1) c.splits = 1;
   return c;
 }
 
+// Partial sums: of every column of plan_B sequences.
 int64_t partials(const Cache8Attend& a, const Cut& c) {
-  return c.splits > 1 ? (int64_t)a.B * a.g.heads * a.L * (a.heads / a.g.heads) * c.splits : 0;
+  return c.splits > 1 ? (int64_t)a.plan_B * a.g.heads * a.L * (a.heads / a.g.heads) * c.splits : 0;
 }
 
 template <int D, class T, int QB, bool SPLIT>
@@ -767,7 +769,7 @@ hipError_t go(const Cache8Attend& a, const Cut& c, const T* q, T* out, hipStream
   if (c.splits > 1) {
     int share = 1;  // some eight splits to a group
     while (share * 8 < c.splits && share < 256 / (D / 4)) share *= 2;
-    const int64_t columns = n / c.splits, per = 256 / (D / 4 * share);
+    const int64_t columns = probs * a.L * (a.heads / a.g.heads), per = 256 / (D / 4 * share);
     k_cache8_join<D, T><<<(unsigned)((columns + per - 1) / per), 256, 0, s>>>(
         a, out, part, ml, columns, c.splits, c.chunk, share);
   }

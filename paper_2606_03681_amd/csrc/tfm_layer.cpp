@@ -1,6 +1,7 @@
 // Host side of the C ABI declared in include/tfm_layer.h: argument validation, the
 // active-cell plan, buffer layouts and the launch sequences of the forward and backward pass.
 #include "tfm_layer.h"
+#include "tfm_cache.h"
 #include "tfm_prof.h"
 
 #include <hip/hip_runtime.h>
@@ -17,6 +18,7 @@
 
 #include "kernels.h"
 #include "attn.h"
+#include "cache8.h"
 #include "f32.h"
 #include "fast.h"
 #include "prof.h"
@@ -643,6 +645,7 @@ struct FwdBufs {
   bool query = false;  // ki / vi hold the keys and values of a context call: project Q only
   int kR = 0;          // rows per (column, head) of ki / vi; 0: R
   bool save = true;    // the forward keeps what its backward reads (false: forward-only calls)
+  const tfm::Cache8Attend* c8 = nullptr;  // query calls against an 8-bit cache (ki, vi unused)
 };
 
 FwdBufs bufs_from_saved(char* sv, const SavedLayout& S) {
@@ -656,6 +659,17 @@ FwdBufs bufs_from_saved(char* sv, const SavedLayout& S) {
   b.g = (T*)(sv + S.g); b.u = (T*)(sv + S.u); b.xh3 = (T*)(sv + S.xh3);
   b.rs3 = (float*)(sv + S.rs3);
   return b;
+}
+
+// Item attention of qi over ki and vi, or over the 8-bit cache of a context call.
+int item_fwd(const tfm::Geo& g, const FwdBufs& b, hipStream_t s) {
+  using namespace tfm;
+  if (b.c8)
+    STEP("item_attn8_fwd/mfma", launch_cache8_attend(*b.c8, b.qi, b.oi, s));
+  else
+    STEP("item_attn_fwd/mfma",
+         launch_item_attn_fwd(g, b.qi, b.ki, b.vi, b.oi, b.lsei, s, b.kR));
+  return TFM_OK;
 }
 
 // Feature Q|K|V (projection of the layer input x, rows per xmode), then the feature attention.
@@ -721,8 +735,7 @@ int fwd_fast(const Dims& d, const tfm::Geo& g, const tfm::bf16* X, const float* 
   a.A = b.h1; a.lda = E; a.Bt = f.w + f.wo.qkv_i; a.bias = fb;
   a.out = b.qi; a.out2 = b.ki; a.out3 = b.vi;
   STEP("item_qkv/mfma", launch_gemm(a, s));
-  STEP("item_attn_fwd/mfma",
-       launch_item_attn_fwd(g, b.qi, b.ki, b.vi, b.oi, b.lsei, s, b.kR));
+  STEP_ERR(item_fwd(g, b, s));
   if (mlp_fused_ok(E, H)) {
     // out-projection + LN2, MLP and LN3 in one kernel, the hidden layer in registers
     bf16* ms = f.w + f.wo.ms;
@@ -955,8 +968,7 @@ int fwd_pre(const Dims& d, const tfm::Geo& g, const tfm::bf16* X, const float* p
   a.A = b.r2; a.lda = E; a.Bt = f.w + f.wo.qkv_i; a.bias = prm + o.bqkv_i;
   a.out = b.qi; a.out2 = b.ki; a.out3 = b.vi;
   STEP("item_qkv/mfma", launch_gemm(a, s));
-  STEP("item_attn_fwd/mfma",
-       launch_item_attn_fwd(g, b.qi, b.ki, b.vi, b.oi, b.lsei, s, b.kR));
+  STEP_ERR(item_fwd(g, b, s));
   // h2 = h1 + O_i Wo_i^T + bo_i, r3 = RMS3(h2)
   a = gemm_base(g, N, E, E, EPI_RMS);
   a.A = b.oi; a.lda = E; a.Bt = f.w + f.wo.o_i; a.bias = prm + o.bo_i;
@@ -1133,6 +1145,36 @@ FwdBufs infer_bufs(const Dims& d, char* ws, const InferLayout& L, tfm::bf16* kc,
   return b;
 }
 
+// The 8-bit cache of one layer: every possible active column is a sequence whose pages lie one
+// after another.
+constexpr int kCache8Page = 64;
+int64_t cache8_pages(const Dims& d) { return ((int64_t)d.R + kCache8Page - 1) / kCache8Page; }
+size_t cache8_total(const Dims& d) {
+  return tfm::cache8_pool_bytes(d.heads, d.d, kCache8Page, (int64_t)d.B * d.S * cache8_pages(d));
+}
+int cache8_check(const Dims& d) {
+  if ((int64_t)d.B * d.S * cache8_pages(d) > 0x7fffffff)
+    return fail(TFM_ERR_DIMS, "the 8-bit cache has more than 2^31 - 1 pages");
+  return TFM_OK;
+}
+tfm::Cache8Geo layer_cache8(const Dims& d, void* pool) {
+  return tfm::cache8_geo(d.heads, d.d, kCache8Page, (int)(d.B * d.S * cache8_pages(d)), pool,
+                         (int)cache8_pages(d), nullptr);
+}
+// A query call's attention over it: d has the queries' rows, dc the context's.  Keys carry the
+// scale and log2(e), from the folded weights.
+tfm::Cache8Attend layer_attend8(const Dims& d, const Dims& dc, void* pool) {
+  tfm::Cache8Attend a{};
+  a.g = layer_cache8(dc, pool);
+  a.plan_B = d.B * d.S;  // by which the scratch is sized, whatever columns are active
+  a.plan_rows = a.max_rows = dc.R;
+  a.L = d.R; a.heads = d.heads;
+  a.scale_log2 = 1.0f;
+  a.sq[0] = (int64_t)d.heads * d.R * d.d; a.sq[1] = d.d; a.sq[2] = (int64_t)d.R * d.d;
+  a.so[0] = (int64_t)d.R * d.E; a.so[1] = d.E; a.so[2] = d.d;
+  return a;
+}
+
 FastWs infer_fast_ws(const Dims& d, char* ws, const InferLayout& L) {
   FastWs f{};
   f.wo = tfm::weight_offsets(d.E, d.H);
@@ -1140,20 +1182,21 @@ FastWs infer_fast_ws(const Dims& d, char* ws, const InferLayout& L) {
   return f;
 }
 
-// Shared part of the two forward-only calls.  ctx_rows < 0: a context call (dims->R rows, the
-// cache written); otherwise a query call whose cache came from a context call with ctx_rows
-// rows.
+// Shared part of the forward-only calls.  ctx_rows < 0: a context call (dims->R rows, the cache
+// written); otherwise a query call whose cache came from a context call with ctx_rows rows.
+// pool: the 8-bit cache that a context call fills from the bfloat16 one, or that a query call reads
+// in its place.
 int infer_call(const tfm_dims* dims, int ctx_rows, const int32_t* n_train,
                const uint8_t* cell_mask, const void* X, const float* params, void* Y,
-               void* cache, size_t cache_bytes, void* workspace, size_t workspace_bytes,
-               hipStream_t s) {
+               void* cache, size_t cache_bytes, bool eight, void* pool, size_t pool_bytes,
+               void* workspace, size_t workspace_bytes, hipStream_t s) {
   Dims d;
   int rc = check_dims(dims, d);
   if (rc) return rc;
   if (!infer_eligible(d))
     return fail(TFM_ERR_DIMS, "forward-only calls need TFM_BF16, E in {64, 128, 192, 256} and H "
                               "a multiple of E");
-  const bool query = ctx_rows >= 0;
+  const bool query = ctx_rows >= 0, plain = !(eight && query);  // plain: the bfloat16 cache is used
   Dims dc = d;  // the dims the cache was laid out for
   if (query) {
     if (ctx_rows < 1) return fail(TFM_ERR_DIMS, "context_rows=%d must be >= 1", ctx_rows);
@@ -1162,16 +1205,22 @@ int infer_call(const tfm_dims* dims, int ctx_rows, const int32_t* n_train,
     rc = check_dims(&pc, dc);
     if (rc) return rc;
   }
-  if (!aligned(X) || !aligned(params) || !aligned(Y) || !aligned(cache) || !aligned(workspace))
-    return fail(TFM_ERR_POINTER, "X, params, Y, kv_cache and workspace must be non-null and "
-                                 "16-byte aligned");
+  if (eight && (rc = cache8_check(dc))) return rc;
+  if (!aligned(X) || !aligned(params) || !aligned(Y) || (plain && !aligned(cache)) ||
+      (eight && !aligned(pool)) || !aligned(workspace))
+    return fail(TFM_ERR_POINTER, "X, params, Y, kv_cache (and cache8) and workspace must be "
+                                 "non-null and 16-byte aligned");
   const InferLayout L = infer_layout(d);
-  if (workspace_bytes < L.total)
-    return fail(TFM_ERR_BUFFER, "workspace has %zu bytes, %zu required", workspace_bytes,
-                L.total);
-  if (cache_bytes < 2 * cache_half(dc))
+  size_t need = L.total;
+  if (!plain) need += tfm::cache8_attend_bytes(layer_attend8(d, dc, pool), false);
+  if (workspace_bytes < need)
+    return fail(TFM_ERR_BUFFER, "workspace has %zu bytes, %zu required", workspace_bytes, need);
+  if (plain && cache_bytes < 2 * cache_half(dc))
     return fail(TFM_ERR_BUFFER, "kv_cache has %zu bytes, %zu required", cache_bytes,
                 2 * cache_half(dc));
+  if (eight && pool_bytes < cache8_total(dc))
+    return fail(TFM_ERR_BUFFER, "cache8 has %zu bytes, %zu required", pool_bytes,
+                cache8_total(dc));
   Plan P;
   rc = make_plan(d, n_train, cell_mask, P, query ? ctx_rows : d.R);
   if (rc) return rc;
@@ -1182,11 +1231,28 @@ int infer_call(const tfm_dims* dims, int ctx_rows, const int32_t* n_train,
   rc = setup_geo(d, P, ws, L.meta, g, &sw, s);
   if (rc) return rc;
   tfm::bf16* kc = (tfm::bf16*)cache;
-  tfm::bf16* vc = (tfm::bf16*)((char*)cache + cache_half(dc));
-  const FwdBufs b = infer_bufs(d, ws, L, kc, vc, query, query ? ctx_rows : d.R);
-  if (d.block == TFM_BLOCK_PRENORM)
-    return fwd_pre(d, g, (const tfm::bf16*)X, params, (tfm::bf16*)Y, b, f, s);
-  return fwd_fast(d, g, (const tfm::bf16*)X, params, (tfm::bf16*)Y, b, f, s);
+  tfm::bf16* vc = plain ? (tfm::bf16*)((char*)cache + cache_half(dc)) : nullptr;
+  FwdBufs b = infer_bufs(d, ws, L, kc, vc, query, query ? ctx_rows : d.R);
+  tfm::Cache8Attend a8;
+  if (!plain) {
+    a8 = layer_attend8(d, dc, pool);
+    a8.B = g.NC;
+    a8.lens = g.col_ntr;
+    a8.ws = ws + L.total;
+    b.c8 = &a8;
+  }
+  rc = d.block == TFM_BLOCK_PRENORM
+           ? fwd_pre(d, g, (const tfm::bf16*)X, params, (tfm::bf16*)Y, b, f, s)
+           : fwd_fast(d, g, (const tfm::bf16*)X, params, (tfm::bf16*)Y, b, f, s);
+  if (rc || !eight || query) return rc;
+  tfm::Cache8Append w{};
+  w.g = layer_cache8(d, pool);
+  w.B = g.NC; w.L = d.R;
+  w.sk[0] = (int64_t)d.heads * d.R * d.d; w.sk[1] = d.d; w.sk[2] = (int64_t)d.R * d.d;
+  for (int i = 0; i < 3; ++i) w.sv[i] = w.sk[i];
+  w.n_new = g.col_ntr;
+  STEP("cache8_append/hbm", tfm::launch_cache8_append(w, kc, vc, s));
+  return TFM_OK;
 }
 
 }  // namespace
@@ -1456,8 +1522,8 @@ int tfm_layer_fwd_context(const tfm_dims* dims, const int32_t* n_train, const ui
                           const void* X, const float* params, void* Y, void* kv_cache,
                           size_t cache_bytes, void* workspace, size_t workspace_bytes,
                           void* stream) {
-  return infer_call(dims, -1, n_train, cell_mask, X, params, Y, kv_cache, cache_bytes,
-                    workspace, workspace_bytes, (hipStream_t)stream);
+  return infer_call(dims, -1, n_train, cell_mask, X, params, Y, kv_cache, cache_bytes, false,
+                    nullptr, 0, workspace, workspace_bytes, (hipStream_t)stream);
 }
 
 int tfm_layer_fwd_query(const tfm_dims* dims, int32_t context_rows, const int32_t* n_train,
@@ -1466,7 +1532,47 @@ int tfm_layer_fwd_query(const tfm_dims* dims, int32_t context_rows, const int32_
                         size_t workspace_bytes, void* stream) {
   if (context_rows < 0) return fail(TFM_ERR_DIMS, "context_rows=%d must be >= 1", context_rows);
   return infer_call(dims, context_rows, n_train, cell_mask, X, params, Y,
-                    const_cast<void*>(kv_cache), cache_bytes, workspace, workspace_bytes,
+                    const_cast<void*>(kv_cache), cache_bytes, false, nullptr, 0, workspace,
+                    workspace_bytes, (hipStream_t)stream);
+}
+
+size_t tfm_infer_cache8_bytes(const tfm_dims* dims) {
+  Dims d;
+  if (check_dims(dims, d) != TFM_OK || cache8_check(d) != TFM_OK) return 0;
+  if (!infer_eligible(d)) {
+    fail(TFM_ERR_DIMS, "forward-only calls need TFM_BF16, E in {64, 128, 192, 256} and H a "
+                       "multiple of E");
+    return 0;
+  }
+  return cache8_total(d);
+}
+
+size_t tfm_infer8_workspace_bytes(const tfm_dims* dims, int32_t context_rows) {
+  const size_t base = tfm_infer_workspace_bytes(dims);
+  if (!base) return 0;
+  Dims d, dc;
+  check_dims(dims, d);
+  tfm_dims pc = *dims;
+  pc.R = context_rows;
+  if (check_dims(&pc, dc) != TFM_OK || cache8_check(dc) != TFM_OK) return 0;
+  return base + tfm::cache8_attend_bytes(layer_attend8(d, dc, nullptr), false);
+}
+
+int tfm_layer_fwd_context8(const tfm_dims* dims, const int32_t* n_train, const uint8_t* cell_mask,
+                           const void* X, const float* params, void* Y, void* kv_cache,
+                           size_t cache_bytes, void* cache8, size_t cache8_bytes, void* workspace,
+                           size_t workspace_bytes, void* stream) {
+  return infer_call(dims, -1, n_train, cell_mask, X, params, Y, kv_cache, cache_bytes, true, cache8,
+                    cache8_bytes, workspace, workspace_bytes, (hipStream_t)stream);
+}
+
+int tfm_layer_fwd_query8(const tfm_dims* dims, int32_t context_rows, const int32_t* n_train,
+                         const uint8_t* cell_mask, const void* X, const float* params,
+                         const void* cache8, size_t cache8_bytes, void* Y, void* workspace,
+                         size_t workspace_bytes, void* stream) {
+  if (context_rows < 0) return fail(TFM_ERR_DIMS, "context_rows=%d must be >= 1", context_rows);
+  return infer_call(dims, context_rows, n_train, cell_mask, X, params, Y, nullptr, 0, true,
+                    const_cast<void*>(cache8), cache8_bytes, workspace, workspace_bytes,
                     (hipStream_t)stream);
 }
 

@@ -86,10 +86,10 @@ class InferStack:
     (train rows first) through every layer once and keeps one key/value cache per layer;
     `query` then runs any number of chunks of unlabelled rows through every layer against
     those caches.  For the pre-norm block, layer l multiplies its input by
-    decay_base ** (first_layer + l)."""
+    decay_base ** (first_layer + l).  cache8: the caches hold 8 bits a value (tfm_cache.h)."""
 
     def __init__(self, dims, n_train, cell_mask, params, max_query_rows, device="cuda",
-                 decay_base=0.95, first_layer=0):
+                 decay_base=0.95, first_layer=0, cache8=False):
         self.n_train = np.ascontiguousarray(n_train, dtype=np.int32)
         self.cell_mask = np.ascontiguousarray(cell_mask, dtype=np.uint8)
         self.device = device
@@ -102,11 +102,21 @@ class InferStack:
         self.q_dims = None
         self.decay_base, self.first_layer, self.base = decay_base, first_layer, dims
         self.elt = torch.bfloat16
+        self.cache8 = bool(cache8)
         wb = max(tfm.infer_workspace_bytes(self.ctx_dims[0]),
                  tfm.infer_workspace_bytes(self._copy(dims, self.Rq)))
         cb = tfm.infer_cache_bytes(self.ctx_dims[0])
         if wb == 0 or cb == 0:
             raise tfm.TfmError(-1, tfm.last_error())
+        if self.cache8:
+            # one bfloat16 cache for all layers' context calls; scratch by the query rows of a call,
+            # which may need more the fewer they are
+            self.kv = torch.empty(cb, dtype=torch.uint8, device=device)
+            cb = tfm.infer_cache8_bytes(self.ctx_dims[0])
+            wb = max([wb] + [tfm.infer8_workspace_bytes(self._copy(dims, r), self.Rc)
+                             for r in range(1, self.Rq + 1)])
+            if cb == 0:
+                raise tfm.TfmError(-1, tfm.last_error())
         self.workspace = torch.empty(wb, dtype=torch.uint8, device=device)
         self.caches = [torch.empty(cb, dtype=torch.uint8, device=device) for _ in range(self.L)]
         S, E = dims.C + 1, dims.E
@@ -135,8 +145,13 @@ class InferStack:
         h = X
         for l in range(self.L):
             out = self.ctx_out[l % 2]
-            tfm.layer_fwd_context(self.ctx_dims[l], self.n_train, self.cell_mask, h,
-                                  self.params[l], out, self.caches[l], self.workspace)
+            if self.cache8:
+                tfm.layer_fwd_context8(self.ctx_dims[l], self.n_train, self.cell_mask, h,
+                                       self.params[l], out, self.kv, self.caches[l],
+                                       self.workspace)
+            else:
+                tfm.layer_fwd_context(self.ctx_dims[l], self.n_train, self.cell_mask, h,
+                                      self.params[l], out, self.caches[l], self.workspace)
             h = out
         return h
 
@@ -151,8 +166,9 @@ class InferStack:
         for l in range(self.L):
             B, _, S, E = Xq.shape
             out = self.q_flat[l % 2][:B * Rq * S * E].view(B, Rq, S, E)
-            tfm.layer_fwd_query(dims[l], self.Rc, self.n_train, self.cell_mask, h,
-                                self.params[l], self.caches[l], out, self.workspace)
+            query = tfm.layer_fwd_query8 if self.cache8 else tfm.layer_fwd_query
+            query(dims[l], self.Rc, self.n_train, self.cell_mask, h, self.params[l],
+                  self.caches[l], out, self.workspace)
             h = out
         return h
 
@@ -167,6 +183,34 @@ def cat_embed(dims, T, cat_cols, V, scale):
     e = tfm.make_embed((dims.B, dims.R - T, cat_cols), (dims.R * S * dims.E, S * dims.E, dims.E),
                        dims.E, V, dims.dtype, tfm.TFM_F32, scale)
     return e, T * S * dims.E
+
+
+def allowed_bits(allowed):
+    """Bool [..., K] as the words of tfm_adjust_logits, int32 [..., ceil(K / 32)]."""
+    K = allowed.shape[-1]
+    bits = torch.nn.functional.pad(allowed, (0, -K % 32)).unflatten(-1, (-1, 32)).to(torch.int64)
+    words = (bits << torch.arange(32, device=allowed.device)).sum(-1)
+    return torch.where(words >= 2 ** 31, words - 2 ** 32, words).to(torch.int32)
+
+
+def adjust_classes(logits, n_class=None, bias=None, allowed=None, history=None, n_history=None,
+                   repetition=None, presence=None, frequency=None):
+    """tfm_adjust_logits in place on logits float32 [N, K] side by side: bias float32 and allowed
+    bool [K] or [N, K]; history int32 [N, n]; the rest of a value per row."""
+    N, K = logits.shape
+    idx = words = None
+    ld_bias = ld_allowed = 0
+    if bias is not None:
+        ld_bias = K if bias.dim() == 2 else 0
+        idx = torch.arange(K, dtype=torch.int32, device=logits.device)
+        idx = idx.expand(N, K).contiguous() if ld_bias else idx
+    if allowed is not None:
+        words = allowed_bits(allowed)
+        ld_allowed = words.shape[-1] if allowed.dim() == 2 else 0
+    a = tfm.make_adjust(N, K, K, tfm.TFM_F32, 0 if history is None else history.shape[1],
+                        0 if bias is None else K, ld_bias=ld_bias, ld_allowed=ld_allowed)
+    tfm.adjust_logits(a, logits, n_class, history, n_history, repetition, presence, frequency, idx,
+                      bias, words, logits)
 
 
 class TrainStep:
@@ -386,11 +430,11 @@ class InferModel:
     key/value caches, the remaining rows run through every layer in chunks of unlabelled rows
     against those caches, and the decoder turns the outputs of each dataset's unlabelled rows
     into logits.  Allocation, call order and the row order of the result only.  cat_table, cat_cols,
-    cat_scale: as for TrainStep."""
+    cat_scale: as for TrainStep.  cache8: the key/value caches hold 8 bits a value (InferStack)."""
 
     def __init__(self, dims, ends, n_train, n_feat, params, ends_params, table=None,
                  chunk=256, device="cuda", decay_base=0.95, cat_table=None, cat_cols=0,
-                 cat_scale=1.0):
+                 cat_scale=1.0, cache8=False):
         if dims.dtype != tfm.TFM_BF16:
             raise ValueError("the forward-only path runs in bfloat16")
         self.dims, self.ends = dims, ends
@@ -408,7 +452,8 @@ class InferModel:
         dc.R = self.Rc
         self.ctx_dims = dc
         self.stack = InferStack(dc, self.n_train, self.cell_mask, params,
-                                max_query_rows=self.chunk, device=device, decay_base=decay_base)
+                                max_query_rows=self.chunk, device=device, decay_base=decay_base,
+                                cache8=cache8)
         self.ends_params = ends_params if isinstance(ends_params, torch.Tensor) else \
             torch.from_numpy(np.ascontiguousarray(ends_params, dtype=np.float32)).to(device)
         self.table = None
@@ -432,11 +477,17 @@ class InferModel:
                                               cat_scale)
 
     def draw(self, x, labels, u, cat_ids=None, n_class=None, temperature=None, top_k=None,
-             top_p=None, min_p=None):
+             top_p=None, min_p=None, adjust=None):
         """One class drawn for every unlabelled row (tfm_sample), in predict's row order: returns
         (classes int32 [T_test], their log-probabilities, the logits).  u: device float32 [T_test]
         in [0, 1); n_class: host int32 [B], the classes of each dataset (None: all K); the settings
-        are numbers, or device tensors of a value per row."""
+        are numbers, or device tensors of a value per row.
+
+        adjust: dict of what is done to the logits first (tfm_adjust_logits; the logits returned are
+        the adjusted ones), all of it optional: bias, device float32 [K] or [T_test, K]; allowed,
+        device bool of such a shape; history, device int32 [T_test, n] of classes drawn before (out
+        of range: none), with n_history, repetition, presence and frequency, numbers or device
+        tensors of a value per row."""
         logits = self.predict(x, labels, cat_ids)
         N = logits.shape[0]
         rows = self.dims.R - self.n_train
@@ -448,6 +499,10 @@ class InferModel:
             return v if v is None or isinstance(v, torch.Tensor) else \
                 torch.full((N,), v, dtype=dtype, device=logits.device)
 
+        if adjust is not None:
+            adjust_classes(logits, n_class, **{k: per_row(v, torch.int32 if k == "n_history" else
+                                                          torch.float32)
+                                               for k, v in adjust.items()})
         token = torch.empty(N, dtype=torch.int32, device=logits.device)
         logprob = torch.empty(N, dtype=torch.float32, device=logits.device)
         tfm.sample(tfm.make_sampling(N, self.K, self.K, tfm.TFM_F32), logits, n_class,

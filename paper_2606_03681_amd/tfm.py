@@ -33,7 +33,8 @@ EXPORTS = ("tfm_layer_param_count", "tfm_layer_saved_bytes", "tfm_layer_workspac
            "tfm_embed_workspace_bytes", "tfm_embed_fwd", "tfm_embed_bwd",
            "tfm_distill_workspace_bytes", "tfm_distill_loss", "tfm_sample",
            "tfm_adjust_logits", "tfm_cache8_bytes", "tfm_cache8_append",
-           "tfm_cache8_attend_workspace_bytes", "tfm_cache8_attend",
+           "tfm_cache8_attend_workspace_bytes", "tfm_cache8_attend", "tfm_infer_cache8_bytes",
+           "tfm_infer8_workspace_bytes", "tfm_layer_fwd_context8", "tfm_layer_fwd_query8",
            "tfm_clip_workspace_bytes",
            "tfm_clip_scale", "tfm_sfadamw_step", "tfm_muon_workspace_bytes", "tfm_muon_step")
 
@@ -181,7 +182,7 @@ def lib():
         vp, sz, i32 = ctypes.c_void_p, ctypes.c_size_t, ctypes.c_int
         for name in ("tfm_layer_param_count", "tfm_layer_saved_bytes",
                      "tfm_layer_workspace_bytes", "tfm_infer_workspace_bytes",
-                     "tfm_infer_cache_bytes"):
+                     "tfm_infer_cache_bytes", "tfm_infer_cache8_bytes"):
             getattr(L, name).restype = sz
             getattr(L, name).argtypes = [P(tfm_dims)]
         L.tfm_last_error.restype = ctypes.c_char_p
@@ -202,6 +203,14 @@ def lib():
         L.tfm_layer_fwd_query.restype = i32
         L.tfm_layer_fwd_query.argtypes = [P(tfm_dims), i32, vp, vp, vp, vp, vp, sz, vp, vp, sz,
                                           vp]
+        L.tfm_infer8_workspace_bytes.restype = sz
+        L.tfm_infer8_workspace_bytes.argtypes = [P(tfm_dims), i32]
+        L.tfm_layer_fwd_context8.restype = i32
+        L.tfm_layer_fwd_context8.argtypes = [P(tfm_dims), vp, vp, vp, vp, vp, vp, sz, vp, sz, vp,
+                                             sz, vp]
+        L.tfm_layer_fwd_query8.restype = i32
+        L.tfm_layer_fwd_query8.argtypes = [P(tfm_dims), i32, vp, vp, vp, vp, vp, sz, vp, vp, sz,
+                                           vp]
         E_ = P(tfm_ends)
         for name in ("tfm_ends_param_count", "tfm_ends_workspace_bytes"):
             getattr(L, name).restype = sz
@@ -291,6 +300,14 @@ def infer_workspace_bytes(dims):
 
 def infer_cache_bytes(dims):
     return lib().tfm_infer_cache_bytes(ctypes.byref(dims))
+
+
+def infer_cache8_bytes(dims):
+    return lib().tfm_infer_cache8_bytes(ctypes.byref(dims))
+
+
+def infer8_workspace_bytes(dims, context_rows):
+    return lib().tfm_infer8_workspace_bytes(ctypes.byref(dims), int(context_rows))
 
 
 def _ptr(t):
@@ -408,6 +425,31 @@ def layer_fwd_query(dims, context_rows, n_train, cell_mask, X, params, kv_cache,
     rc = lib().tfm_layer_fwd_query(ctypes.byref(dims), int(context_rows), ntp, cmp_, _ptr(X),
                                    _ptr(params), _ptr(kv_cache), _nbytes(kv_cache), _ptr(Y),
                                    _ptr(workspace), _nbytes(workspace), _stream(stream))
+    _check(rc)
+
+
+def layer_fwd_context8(dims, n_train, cell_mask, X, params, Y, kv_cache, cache8, workspace,
+                       stream=None):
+    """tfm_layer_fwd_context8: the context call, with the train rows' keys and values kept in cache8
+    (a device byte tensor of infer_cache8_bytes(dims)); kv_cache is scratch."""
+    nt, ntp = _host(n_train, np.int32)
+    cm, cmp_ = _host(cell_mask, np.uint8)
+    rc = lib().tfm_layer_fwd_context8(ctypes.byref(dims), ntp, cmp_, _ptr(X), _ptr(params), _ptr(Y),
+                                      _ptr(kv_cache), _nbytes(kv_cache), _ptr(cache8),
+                                      _nbytes(cache8), _ptr(workspace), _nbytes(workspace),
+                                      _stream(stream))
+    _check(rc)
+
+
+def layer_fwd_query8(dims, context_rows, n_train, cell_mask, X, params, cache8, Y, workspace,
+                     stream=None):
+    """tfm_layer_fwd_query8: the query call against the keys and values that a context8 call with
+    context_rows rows left in cache8; workspace: infer8_workspace_bytes(dims, context_rows)."""
+    nt, ntp = _host(n_train, np.int32)
+    cm, cmp_ = _host(cell_mask, np.uint8)
+    rc = lib().tfm_layer_fwd_query8(ctypes.byref(dims), int(context_rows), ntp, cmp_, _ptr(X),
+                                    _ptr(params), _ptr(cache8), _nbytes(cache8), _ptr(Y),
+                                    _ptr(workspace), _nbytes(workspace), _stream(stream))
     _check(rc)
 
 

@@ -177,6 +177,46 @@ def test_adjustment_pointers_refused():
     assert _call(_adjust(N=0), **{n: 0 for n in _A}) == 0
 
 
+def _dims(**kw):
+    base = dict(B=2, R=64, C=8, E=64, heads=4, H=128, dtype="bf16")
+    base.update(kw)
+    return tfm.make_dims(**base)
+
+
+def test_layer_calls_with_8_bit_caches_refused():
+    import numpy as np
+    lib, mask = tfm.lib(), np.ones((2, 9), np.uint8)
+
+    def ctx(d=None, nt=(5, 5), ptr=FAKE, pool=FAKE, cb=BIG, pb=BIG, wb=BIG):
+        n = np.array(nt, np.int32)
+        return lib.tfm_layer_fwd_context8(ctypes.byref(d or _dims()), n.ctypes.data,
+                                          mask.ctypes.data, FAKE, FAKE, FAKE, ptr, cb, pool, pb,
+                                          FAKE, wb, None)
+
+    def qry(rc, d=None, nt=(5, 5), pool=FAKE, pb=BIG, wb=BIG):
+        n = np.array(nt, np.int32)
+        return lib.tfm_layer_fwd_query8(ctypes.byref(d or _dims(R=8)), rc, n.ctypes.data,
+                                        mask.ctypes.data, FAKE, FAKE, pool, pb, FAKE, FAKE, wb, None)
+
+    assert ctx(_dims(dtype="f32")) == -1 and ctx(nt=(5, 65)) == -3
+    assert ctx(ptr=0) == -5 and ctx(pool=0) == -5 and ctx(pool=FAKE + 8) == -5
+    need = tfm.infer_cache8_bytes(_dims())
+    assert need == 2 * 9 * 4 * (2 * 64 * 16 + 2)
+    assert ctx(cb=16) == -7 and ctx(wb=16) == -7 and ctx(pb=need - 1) == -7
+    assert "cache8" in tfm.last_error()
+    assert qry(0) == -1 and qry(-3) == -1 and qry(32, nt=(5, 33)) == -3
+    assert qry(32, pool=0) == -5 and qry(32, pool=FAKE + 2) == -5
+    assert qry(100, pb=tfm.infer_cache8_bytes(_dims(R=100)) - 1) == -7
+    assert qry(32, wb=tfm.infer8_workspace_bytes(_dims(R=8), 32) - 1) == -7
+    assert tfm.infer_cache8_bytes(_dims(dtype="f32")) == 0
+    assert tfm.infer8_workspace_bytes(_dims(dtype="f32"), 32) == 0
+    assert tfm.infer8_workspace_bytes(_dims(), 0) == 0
+    for rows in (1, 8, 64, 300):
+        for rc in (1, 64, 700, 5000):
+            assert tfm.infer8_workspace_bytes(_dims(R=rows), rc) >= \
+                tfm.infer_workspace_bytes(_dims(R=rows))
+
+
 def test_binding_refuses_tensors_that_do_not_fit():
     """The Python calls look at types and shapes first (no GPU is touched for these)."""
     import torch
