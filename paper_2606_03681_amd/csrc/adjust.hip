@@ -1,9 +1,10 @@
 // Penalties, biases and masks on logits (declarations in vocab.h).
 //
 // A workgroup takes a slice of a row's classes, or several rows of few classes.  What is said about
-// single classes is gathered in LDS first, a word of how often the class occurs in the history and one
-// of its first bias entry (integers: no order matters), then one pass over the logits applies it.  A
-// slice whose row has neither history nor biases has no such words.
+// single classes is gathered in LDS first, then one pass over the logits, which are on their way
+// meanwhile, applies it: for each class a word with how often it occurs in the history (low half) and
+// the complement of its first bias entry (high half), or two words where either may not fit 16 bits.
+// Integers: no order matters.  A slice whose row has neither history nor biases has no such words.
 #include "mfma.h"
 #include "vocab.h"
 
@@ -24,7 +25,6 @@ struct Vec {
   }
 };
 
-// One class: x, how often it was seen, its bias entry, whether it is allowed.
 struct Rule {
   float r, pres, freq;
 };
@@ -53,76 +53,125 @@ __device__ __forceinline__ int said_of(const AdjustGeo& g, int64_t n) {
   return !g.history ? 0 : g.n_history ? min(max(g.n_history[n], 0), g.n_hist) : g.n_hist;
 }
 
+// Notes about the classes of a slice: PACK, one word each.
+template <bool PACK>
+struct Notes {
+  uint32_t* seen;   // PACK: both halves
+  uint32_t* first;  // else
+  __device__ __forceinline__ void bias(uint32_t v, int j) const {  // before count()
+    if (PACK)
+      atomicMax(&seen[v], (0xffffu - (uint32_t)j) << 16);
+    else
+      atomicMin(&first[v], (uint32_t)j);
+  }
+  __device__ __forceinline__ void count(uint32_t v) const { atomicAdd(&seen[v], 1u); }
+  // how often class i occurs, and its first entry or NONE
+  static __device__ __forceinline__ void split(uint32_t a, uint32_t b, uint32_t& n, uint32_t& j) {
+    n = PACK ? a & 0xffffu : a;
+    j = PACK ? (a >> 16 ? 0xffffu - (a >> 16) : NONE) : b;
+  }
+};
+
 // A slice of one row.  WIDE: rows start at multiples of 16 bytes.
-template <class T, bool WIDE>
-__global__ __launch_bounds__(256) void k_adjust(AdjustGeo g, const T* logits, T* out, int slices,
+template <class T, bool WIDE, bool PACK>
+__global__ __launch_bounds__(256, PACK ? 8 : 4) void k_adjust(AdjustGeo g, const T* logits, T* out, int slices,
                                                 int64_t items) {
-  __shared__ __attribute__((aligned(16))) uint32_t seen[SLICE], first[SLICE];
-  constexpr int V = Vec<T>::V;
+  __shared__ __attribute__((aligned(16))) uint32_t words[PACK ? SLICE : 2 * SLICE];
+  constexpr int V = Vec<T>::V, NV = SLICE / (256 * V);
+  const Notes<PACK> notes{words, words + (PACK ? 0 : SLICE)};
   const int tid = threadIdx.x;
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t n = it / slices;
     const int v0 = (int)(it - n * slices) * SLICE, w = min(SLICE, g.V - v0);
+    const T* from = logits + n * g.ld + v0;
+    T* to = out + n * g.ld_out + v0;
+    uint4 x[NV];
+    uint32_t bits[NV];
+    const uint32_t* mask = g.allowed ? g.allowed + n * g.ld_allowed + v0 / 32 : nullptr;
+    if constexpr (WIDE) {
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int i = (k * 256 + tid) * V;
+        if (i + V <= w) x[k] = *reinterpret_cast<const uint4*>(from + i);
+        bits[k] = mask && i < w ? mask[i / 32] : NONE;
+      }
+    }
     const int m = said_of(g, n), nb = g.n_bias;
     const bool any = m > 0 || nb > 0;
     const Rule u = rule_of(g, n);
     const int nc = classes_of(g, n);
     if (any) {
-      __syncthreads();
-      for (int i = 4 * tid; i < w; i += 1024) {
-        *reinterpret_cast<uint4*>(seen + i) = make_uint4(0, 0, 0, 0);
-        *reinterpret_cast<uint4*>(first + i) = make_uint4(NONE, NONE, NONE, NONE);
-      }
-      __syncthreads();
       const int32_t* h = g.history + n * g.ld_history;
-      for (int j0 = 0; j0 < m; j0 += 2048) {
-        uint32_t v[8];
+      uint32_t v[8];
+      auto ask = [&](int j0) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int j = j0 + i * 256 + tid;
           v[i] = j < m ? (uint32_t)h[j] - (uint32_t)v0 : NONE;
         }
+      };
+      ask(0);
+      __syncthreads();  // the last slice's notes have been read
+      for (int i = 4 * tid; i < (PACK ? w : SLICE + w); i += 1024) {
+        const uint32_t z = PACK || i < SLICE ? 0 : NONE;
+        *reinterpret_cast<uint4*>(words + i) = make_uint4(z, z, z, z);
+      }
+      __syncthreads();
+      if (nb > 0) {
+        for (int j = tid; j < nb; j += 256) {
+          const uint32_t c = (uint32_t)g.bias_idx[n * g.ld_bias + j] - (uint32_t)v0;
+          if (c < (uint32_t)w) notes.bias(c, j);
+        }
+        if (PACK) __syncthreads();
+      }
+      for (int j0 = 0; j0 < m;) {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          if (v[i] < (uint32_t)w) atomicAdd(&seen[v[i]], 1u);
-      }
-      for (int j = tid; j < nb; j += 256) {
-        const uint32_t v = (uint32_t)g.bias_idx[n * g.ld_bias + j] - (uint32_t)v0;
-        if (v < (uint32_t)w) atomicMin(&first[v], (uint32_t)j);
+          if (v[i] < (uint32_t)w) notes.count(v[i]);
+        j0 += 2048;
+        if (j0 < m) ask(j0);
       }
       __syncthreads();
     }
-    const T* from = logits + n * g.ld + v0;
-    T* to = out + n * g.ld_out + v0;
     const float* bias = g.bias + n * g.ld_bias;
-    const uint32_t* mask = g.allowed ? g.allowed + n * g.ld_allowed + v0 / 32 : nullptr;
     const int here = nc - v0;  // classes of the slice that count
     if constexpr (WIDE) {
-      for (int i = tid * V; i < w; i += 256 * V) {
-        const uint32_t bits = mask ? mask[i / 32] >> (i % 32) : NONE;
+#pragma unroll
+      for (int k = 0; k < NV; ++k) {
+        const int i = (k * 256 + tid) * V;
+        if (i >= w) break;
+        const uint32_t b = bits[k] >> (i % 32);
         if (i + V <= w) {
-          Vec<T> x;
-          const uint4 z = *reinterpret_cast<const uint4*>(from + i);
-          x.w[0] = z.x; x.w[1] = z.y; x.w[2] = z.z; x.w[3] = z.w;
+          Vec<T> z;
+          z.w[0] = x[k].x; z.w[1] = x[k].y; z.w[2] = x[k].z; z.w[3] = x[k].w;
           float y[V];
 #pragma unroll
-          for (int j = 0; j < V; ++j) y[j] = x.get(j);
+          for (int j = 0; j < V; ++j) y[j] = z.get(j);
           if (any) {
-            uint32_t s[V], f[V];
+            uint32_t s[V], f[V], some = 0;
 #pragma unroll
             for (int j = 0; j < V; j += 4) {
-              const uint4 a = *reinterpret_cast<const uint4*>(seen + i + j);
-              const uint4 b = *reinterpret_cast<const uint4*>(first + i + j);
+              const uint4 a = *reinterpret_cast<const uint4*>(notes.seen + i + j);
               s[j] = a.x; s[j + 1] = a.y; s[j + 2] = a.z; s[j + 3] = a.w;
-              f[j] = b.x; f[j + 1] = b.y; f[j + 2] = b.z; f[j + 3] = b.w;
+              some |= a.x | a.y | a.z | a.w;
+              if constexpr (!PACK) {
+                const uint4 c = *reinterpret_cast<const uint4*>(notes.first + i + j);
+                f[j] = c.x; f[j + 1] = c.y; f[j + 2] = c.z; f[j + 3] = c.w;
+                some |= ~(c.x & c.y & c.z & c.w);
+              }
             }
+            if (some) {
 #pragma unroll
-            for (int j = 0; j < V; ++j)
-              if (s[j] || f[j] != NONE) y[j] = adjusted(y[j], s[j], f[j], bias, u);
+              for (int j = 0; j < V; ++j) {
+                uint32_t count, first;
+                notes.split(s[j], PACK ? 0 : f[j], count, first);
+                if (count || first != NONE) y[j] = adjusted(y[j], count, first, bias, u);
+              }
+            }
           }
 #pragma unroll
           for (int j = 0; j < V; ++j)
-            if (!(bits >> j & 1) || i + j >= here) y[j] = -INFINITY;
+            if (!(b >> j & 1) || i + j >= here) y[j] = -INFINITY;
           uint4 o;
           if constexpr (sizeof(T) == 4)
             o = make_uint4(__float_as_uint(y[0]), __float_as_uint(y[1]), __float_as_uint(y[2]),
@@ -133,15 +182,23 @@ __global__ __launch_bounds__(256) void k_adjust(AdjustGeo g, const T* logits, T*
         } else {
           for (int j = 0; i + j < w; ++j) {
             float y = ld(from + i + j);
-            if (any) y = adjusted(y, seen[i + j], first[i + j], bias, u);
-            st(to + i + j, (bits >> j & 1) && i + j < here ? y : -INFINITY);
+            if (any) {
+              uint32_t count, first;
+              notes.split(notes.seen[i + j], PACK ? 0 : notes.first[i + j], count, first);
+              y = adjusted(y, count, first, bias, u);
+            }
+            st(to + i + j, (b >> j & 1) && i + j < here ? y : -INFINITY);
           }
         }
       }
     } else {
       for (int i = tid; i < w; i += 256) {
         float y = ld(from + i);
-        if (any) y = adjusted(y, seen[i], first[i], bias, u);
+        if (any) {
+          uint32_t count, first;
+          notes.split(notes.seen[i], PACK ? 0 : notes.first[i], count, first);
+          y = adjusted(y, count, first, bias, u);
+        }
         const bool ok = i < here && (!mask || mask[i / 32] >> (i % 32) & 1);
         st(to + i, ok ? y : -INFINITY);
       }
@@ -206,10 +263,15 @@ hipError_t launch_adjust(const AdjustGeo& g, const T* logits, T* out, hipStream_
   const unsigned blocks = (unsigned)(items < kMaxBlocks ? items : kMaxBlocks);
   const bool wide = (uintptr_t)logits % 16 == 0 && (uintptr_t)out % 16 == 0 &&
                     g.ld * sizeof(T) % 16 == 0 && g.ld_out * sizeof(T) % 16 == 0;
-  if (wide)
-    k_adjust<T, true><<<blocks, 256, 0, s>>>(g, logits, out, slices, items);
+  const bool pack = g.n_hist < 0xffff && g.n_bias < 0xffff;
+  if (wide && pack)
+    k_adjust<T, true, true><<<blocks, 256, 0, s>>>(g, logits, out, slices, items);
+  else if (wide)
+    k_adjust<T, true, false><<<blocks, 256, 0, s>>>(g, logits, out, slices, items);
+  else if (pack)
+    k_adjust<T, false, true><<<blocks, 256, 0, s>>>(g, logits, out, slices, items);
   else
-    k_adjust<T, false><<<blocks, 256, 0, s>>>(g, logits, out, slices, items);
+    k_adjust<T, false, false><<<blocks, 256, 0, s>>>(g, logits, out, slices, items);
   return hipGetLastError();
 }
 template hipError_t launch_adjust(const AdjustGeo&, const float*, float*, hipStream_t);
