@@ -116,9 +116,15 @@ struct Values {
   uint4 v[D / 16];
 };
 
+// Whether tiles go through LDS, for all four waves: where registers hold no tile beside 32 columns' sums.
+// Many columns at d = 128, bf16, pages of 64 and more (8 sequences of 1000 rows, 2000 keys, 16 heads):
+// 349 us with 16 columns and the tile in registers, 238 us staged with 32; at d = 64 the tile in
+// registers is the faster one (122 us, 139 us staged), as with pages under 64 (218 us, 246 us).
+template <int D, bool F32, int QB, bool SPLIT>
+constexpr bool staged() { return !SPLIT && D == 128 && !F32 && QB == 2; }
 // Waves per SIMD that the registers of a kernel leave room for.
 template <int D, bool F32, int QB, bool SPLIT>
-constexpr int waves() { return D <= 32 && QB == 4 ? 3 : D == 128 && QB == 2 ? 1 : 2; }
+constexpr int waves() { return D <= 32 && QB == 4 ? 3 : D == 128 && QB == 2 && SPLIT ? 1 : 2; }
 
 template <int D, class T, int QB, bool SPLIT, bool UNI>
 __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void k_cache8_attend(Cache8Attend a, const T* __restrict__ q,
@@ -130,6 +136,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   constexpr int DB = D / 16, CH = KQ<D>::CH, KW = D / 16;  // KW: dwords of a key per lane
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 2 : 1;
+  constexpr bool STAGE = staged<D, F32, QB, SPLIT>();  // tiles go through LDS, for all four waves
   typedef typename KQ<D>::frag QF;
   const Cache8Geo& g = a.g;
   const int lane = threadIdx.x & 63, wave = wave_id(), c = lane & 15, lg = lane >> 4;
@@ -145,7 +152,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   const int rows = a.n_rows ? min(max(a.n_rows[b], 0), a.L) : a.L;
   const int ncols = rows * G;
   const int col0 = (SPLIT ? ct : ct * 4 + wave) * 16 * QB;
-  if (col0 >= ncols) return;
+  if ((STAGE ? ct * 64 * QB : col0) >= ncols) return;  // (a wave without columns reads tiles for others)
   const int k0 = (int)sp * chunk, shift = g.shift;
   // The table's entries from ebase (a multiple of 64) on, one a lane, and the 64 after them: a tile's
   // pages come from these registers, so that none waits for its page's number.  (Read before the
@@ -160,7 +167,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
 
   // the keys that each column sees
   auto row_of = [&](int col) { return (int)((uint32_t)col / (uint32_t)G); };
-  int upto[QB], lo = len, hi = len;
+  int upto[QB], lo = len, hi = len, hi_all = len;  // hi_all: of the workgroup's columns
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) upto[qb] = len;
   if (a.causal) {
@@ -179,13 +186,15 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
     }
     lo = __builtin_amdgcn_readfirstlane(lo);
     hi = __builtin_amdgcn_readfirstlane(hi);
+    hi_all = min(max(len - rows + row_of(min((ct + 1) * 64 * QB, ncols) - 1) + 1, 0), len);
   }
 
   // the queries' operands, in LDS at D >= 64, where registers are short
   constexpr bool QLDS = D >= 64 || (D == 32 && QB == 4);
   constexpr int QBYTES = QLDS ? NQ * QB * CH * 1024 : 0;  // of a wave
   constexpr int OBYTES = SPLIT ? 4 * 16 * QB * (D + 4) * 4 : 0;
-  constexpr int LBYTES = 4 * QBYTES > OBYTES ? 4 * QBYTES : OBYTES;
+  constexpr int TBYTES = 128 * D;  // of a tile: 64 rows of keys, then D rows of values
+  constexpr int LBYTES = STAGE ? 4 * QBYTES + 2 * TBYTES : 4 * QBYTES > OBYTES ? 4 * QBYTES : OBYTES;
   __shared__ __attribute__((aligned(16))) uint8_t lds[LBYTES > 0 ? LBYTES : 16];
   QF qf[NQ][QB][CH];  // (dead behind the stores below where it is in LDS)
   uint8_t* ql = lds + wave * QBYTES + lane * 16;
@@ -244,7 +253,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   };
   const float scale = fabsf(a.scale_log2);
 
-  const int kend = min(splits > 1 ? k0 + chunk : len, hi);
+  const int kend = STAGE && col0 >= ncols ? k0 : min(splits > 1 ? k0 + chunk : len, hi);
   constexpr int STEP = SPLIT ? 4 * KT : KT;
   const int page = g.page;
   const int64_t hd = (int64_t)g.heads * page * D;  // bytes of a page
@@ -314,6 +323,47 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db][qb] = zero4();
   }
+  // A staged tile: each thread brings two 16-byte pieces of keys and two of values.  Pieces are swapped
+  // within their row by bits of the row's number, so that the eight rows of which eight lanes read a
+  // piece lie in different banks.
+  int cur = 0;  // the buffer that is read
+  auto swap_k = [](int row) { return (row & 3) | (row >> 2 & 4); };
+  uint4 kp0, kp1, vp0, vp1;
+  uint32_t gpower = 0;
+  bool ghere = false;
+  auto bring = [&](int t0) {
+    look(t0);
+    const int p = pid_of(t0, 0);
+    const int64_t pg = max(p, 0);
+    const int row = threadIdx.x >> 3, j = threadIdx.x & 7, d = threadIdx.x >> 2, u = threadIdx.x & 3;
+    const uint8_t* kt = g.keys + pg * hd + ((int64_t)kh * page + (t0 & (page - 1)) + row) * D + 16 * j;
+    const uint8_t* vt = g.values + pg * hd + ((int64_t)kh * D + d) * page + (t0 & (page - 1)) + 16 * u;
+    kp0 = *reinterpret_cast<const uint4*>(kt);
+    vp0 = *reinterpret_cast<const uint4*>(vt);
+    kp1 = *reinterpret_cast<const uint4*>(kt + 32 * D);
+    vp1 = *reinterpret_cast<const uint4*>(vt + 64 * (int64_t)page);
+    ghere = p >= 0;
+    gpower = *reinterpret_cast<const uint16_t*>(g.powers + (pg * g.heads + kh) * 2);
+  };
+  auto put = [&](int buf) {
+    uint8_t* at = lds + 4 * QBYTES + buf * TBYTES;
+    const int row = threadIdx.x >> 3, j = threadIdx.x & 7, d = threadIdx.x >> 2, u = threadIdx.x & 3;
+    uint8_t* vt = at + 64 * D + d * 64 + 16 * (u ^ (d >> 1 & 3));  // (row 64 on swaps alike)
+    *reinterpret_cast<uint4*>(at + row * D + 16 * (j ^ swap_k(row))) = kp0;
+    *reinterpret_cast<uint4*>(vt) = vp0;
+    *reinterpret_cast<uint4*>(at + (row + 32) * D + 16 * (j ^ swap_k(row))) = kp1;
+    *reinterpret_cast<uint4*>(vt + 64 * 64) = vp1;
+  };
+  // 16 codes of key t of the lane's four (piece w of its channels), and of values' row block db.
+  const int krow = 16 * (c >> 2) + (c & 3);
+  auto staged_keys = [&](int t, int w) {
+    return *reinterpret_cast<const uint4*>(lds + 4 * QBYTES + cur * TBYTES + (krow + 4 * t) * D +
+                                           16 * ((lg * (D / 64) + w) ^ swap_k(krow)));
+  };
+  auto staged_values = [&](int db) {
+    return *reinterpret_cast<const uint4*>(lds + 4 * QBYTES + cur * TBYTES + 64 * D +
+                                           (16 * db + c) * 64 + 16 * (lg ^ (c >> 1 & 3)));
+  };
   auto key_frag = [&](const Keys<D>& x, int t, int ch) {
     QF kf;
     if constexpr (D == 16) {
@@ -376,6 +426,20 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
     const float cs = fmaxf(scale * exp2i(ek - 127), 0x1p-126f);
     const bool partial = t0 + KT > lo || __any(!here);
     int top = ev;
+    bool dirty = false;  // a staged tile has NaN codes that its readers leave out
+    auto clean = [](uint32_t* w) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const uint32_t m = nan_bytes(w[j]);
+        w[j] &= ~(m | (m - (m >> 7)));  // 0x80 to 0xff
+      }
+    };
+    auto values_of = [&](int db) {
+      if constexpr (STAGE)
+        return staged_values(db);
+      else
+        return y.v[db];
+    };
     // What values say before the weights are there: the largest power among the blocks that any column
     // sees (others' bytes may be anything), and where the NaN codes are.
     auto look_at_values = [&]() {
@@ -384,15 +448,17 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
         top = seen ? ev : 0;
         uint32_t nans = 0;
 #pragma unroll
-        for (int db = 0; db < DB; ++db)
-          nans |= nan_bytes(y.v[db].x) | nan_bytes(y.v[db].y) | nan_bytes(y.v[db].z) |
-                  nan_bytes(y.v[db].w);
+        for (int db = 0; db < DB; ++db) {
+          const uint4 u = values_of(db);
+          nans |= nan_bytes(u.x) | nan_bytes(u.y) | nan_bytes(u.z) | nan_bytes(u.w);
+        }
         if (__any(nans != 0)) {
           // NaN codes (or what lies behind the last key): out of the products, whose weight for them
           // may be 0, and NaN in the sums of the columns that see them
 #pragma unroll
           for (int db = 0; db < DB; ++db) {
-            uint32_t* w = reinterpret_cast<uint32_t*>(&y.v[db]);
+            uint4 u = values_of(db);
+            uint32_t* w = STAGE ? reinterpret_cast<uint32_t*>(&u) : reinterpret_cast<uint32_t*>(&y.v[db]);
             f32x4 cnt[QB];
 #pragma unroll
             for (int qb = 0; qb < QB; ++qb) cnt[qb] = zero4();
@@ -416,12 +482,9 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
 #pragma unroll
               for (int i = 0; i < 4; ++i)
                 if (cnt[qb][i] > 0.f) oacc[db][qb][i] = __builtin_nanf("");
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              const uint32_t m = nan_bytes(w[j]);
-              w[j] &= ~(m | (m - (m >> 7)));  // 0x80 to 0xff
-            }
+            if constexpr (!STAGE) clean(w);
           }
+          dirty = true;
         }
       }
     };
@@ -445,8 +508,8 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
       // (a block that no column sees: any power will do)
       return exp2i(min(ev - unit, 0) + V_BIAS);
     };
-    auto value_frag = [&](int db, int kc, float two) {
-      return kc ? codes_f16(y.v[db].z, y.v[db].w, two) : codes_f16(y.v[db].x, y.v[db].y, two);
+    auto value_frag = [&](const uint4& u, int kc, float two) {
+      return kc ? codes_f16(u.z, u.w, two) : codes_f16(u.x, u.y, two);
     };
     auto add = [&](const f16x8& vf, const f16x8 (*pf)[2], int db, int kc, int qb) {
 #pragma unroll
@@ -477,7 +540,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
 #pragma unroll
       for (int db = 0; db < DB; ++db)
 #pragma unroll
-        for (int kc = 0; kc < 2; ++kc) vf[db][kc] = value_frag(db, kc, two);
+        for (int kc = 0; kc < 2; ++kc) vf[db][kc] = value_frag(y.v[db], kc, two);
       codes_read();
       f32x4 s[4];
 #pragma unroll
@@ -500,6 +563,15 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
         for (int t = 0; t < 4; ++t) s[qb][t] = zero4();
 #pragma unroll
       for (int ch = 0; ch < CH; ++ch) {
+        if constexpr (STAGE) {  // two products' keys at a time
+          if (ch % 2 == 0) {
+#pragma unroll
+            for (int t = 0; t < 4; ++t) {
+              const uint4 u = staged_keys(t, ch / 2);
+              x.k[t][0] = u.x; x.k[t][1] = u.y; x.k[t][2] = u.z; x.k[t][3] = u.w;
+            }
+          }
+        }
         QF f[NQ][QB];
 #pragma unroll
         for (int n = 0; n < NQ; ++n)
@@ -507,7 +579,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
           for (int qb = 0; qb < QB; ++qb) f[n][qb] = query_frag(n, qb, ch);
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
-          const QF kf = key_frag(x, t, ch);
+          const QF kf = key_frag(x, t, STAGE ? ch % 2 : ch);
 #pragma unroll
           for (int n = NQ - 1; n >= 0; --n)
 #pragma unroll
@@ -519,14 +591,32 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
       for (int qb = 0; qb < QB; ++qb) weigh(s[qb], qb, cs, t0, partial, here, pf[qb]);
       look_at_values();
       const float two = raise();
+      constexpr int AT = STAGE ? 2 : DB;  // blocks of values between two products into one sum
+      auto sums = [&](auto fetch) {
 #pragma unroll
-      for (int kc = 0; kc < 2; ++kc)
+        for (int d0 = 0; d0 < DB; d0 += AT) {
+          uint4 u[AT];
 #pragma unroll
-        for (int db = 0; db < DB; ++db) {
-          const f16x8 vf = value_frag(db, kc, two);
+          for (int i = 0; i < AT; ++i) u[i] = fetch(d0 + i);
 #pragma unroll
-          for (int qb = 0; qb < QB; ++qb) add(vf, pf[qb], db, kc, qb);
+          for (int kc = 0; kc < 2; ++kc)
+#pragma unroll
+            for (int i = 0; i < AT; ++i) {
+              const f16x8 vf = value_frag(u[i], kc, two);
+#pragma unroll
+              for (int qb = 0; qb < QB; ++qb) add(vf, pf[qb], d0 + i, kc, qb);
+            }
         }
+      };
+      if (STAGE && dirty) {
+        sums([&](int db) {
+          uint4 u = values_of(db);
+          clean(reinterpret_cast<uint32_t*>(&u));
+          return u;
+        });
+      } else {
+        sums(values_of);
+      }
     }
     first = false;
   };
@@ -545,7 +635,29 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   };
 
   int t0 = k0 + (SPLIT ? wave * KT : 0);
-  if (t0 < kend) {
+  if constexpr (STAGE) {
+    const int kall = min(splits > 1 ? k0 + chunk : len, hi_all);
+    if (k0 < kall) {
+      Keys<D> x;
+      Values<D> none;
+      auto turn = [&] { x.power = gpower, x.here = ghere; };
+      bring(k0);
+      put(0);
+      turn();
+      lds_barrier();
+      for (; t0 < kall; t0 += KT) {
+        const bool more = t0 + KT < kall;
+        if (more) bring(t0 + KT);
+        if (t0 < kend) compute(x, none, t0, -1, [] {});
+        if (more) {
+          put(cur ^ 1);
+          turn();
+        }
+        lds_barrier();
+        cur ^= 1;
+      }
+    }
+  } else if (t0 < kend) {
     Keys<D> x;
     Values<D> y;
     look(t0);
@@ -738,7 +850,15 @@ Cut cut_of(const Cache8Attend& a, bool f32) {
   const int64_t cols = (int64_t)a.L * (a.heads / a.g.heads), probs = (int64_t)a.plan_B * a.g.heads;
   const int64_t keys = a.plan_rows;
   c.split = cols <= 32;
-  c.qb = c.split ? (cols <= 16 ? 1 : 2) : (f32 ? 1 : a.g.d <= 32 ? 4 : a.g.d == 128 ? 1 : 2);
+  c.qb = c.split ? (cols <= 16 ? 1 : 2)
+                 : f32 ? 1 : a.g.d <= 32 ? 4 : 2;
+  if (!c.split && c.qb == 2 && a.g.d == 128) {
+    // Staged tiles, whose workgroups take 128 columns instead of 64, need one for every CU: 8 heads,
+    // 1024 rows on 1100 keys, 1 / 2 / 4 sequences (128 / 256 / 512 workgroups): 36 / 39 / 48 us staged,
+    // 28 / 37 / 70 us not; 128 rows on 8000 keys, 2 / 8 sequences: 45 / 66 us and 35 / 109 us.
+    const int64_t wgs = (cols + 127) / 128 * probs * ((keys + 1023) / 1024);
+    if (a.g.page < KT || cols <= 64 || wgs < 256) c.qb = 1;  // (33 to 64 leave half of it idle)
+  }
   const int per = 16 * c.qb * (c.split ? 1 : 4);
   c.coltiles = (int)((cols + per - 1) / per);
   const int64_t blocks = probs * c.coltiles, want = 2048;
@@ -770,12 +890,18 @@ hipError_t go(const Cache8Attend& a, const Cut& c, const T* q, T* out, hipStream
   for (int64_t p0 = 0; p0 < probs; p0 += most) {
     const uint32_t np = (uint32_t)(probs - p0 < most ? probs - p0 : most);
     const unsigned blocks = (unsigned)(np * each);
-    if (a.g.page >= KT)
-      k_cache8_attend<D, T, QB, SPLIT, true><<<blocks, 256, 0, s>>>(
-          a, q, out, part, ml, (uint32_t)p0, np, c.coltiles, c.splits, c.chunk, wide);
-    else
-      k_cache8_attend<D, T, QB, SPLIT, false><<<blocks, 256, 0, s>>>(
-          a, q, out, part, ml, (uint32_t)p0, np, c.coltiles, c.splits, c.chunk, wide);
+    auto launch = [&](auto* kernel) {
+      kernel<<<blocks, 256, 0, s>>>(a, q, out, part, ml, (uint32_t)p0, np, c.coltiles, c.splits,
+                                    c.chunk, wide);
+    };
+    if constexpr (staged<D, sizeof(T) == 4, QB, SPLIT>()) {  // (only for such pages: cut_of)
+      launch(k_cache8_attend<D, T, QB, SPLIT, true>);
+    } else {
+      if (a.g.page >= KT)
+        launch(k_cache8_attend<D, T, QB, SPLIT, true>);
+      else
+        launch(k_cache8_attend<D, T, QB, SPLIT, false>);
+    }
   }
   if (c.splits > 1) {
     int share = 1;  // some eight splits to a group
@@ -792,7 +918,12 @@ hipError_t go_d(const Cache8Attend& a, const T* q, T* out, hipStream_t s) {
   const Cut c = cut_of(a, sizeof(T) == 4);
   if (c.split)
     return c.qb == 1 ? go<D, T, 1, true>(a, c, q, out, s) : go<D, T, 2, true>(a, c, q, out, s);
-  return go<D, T, sizeof(T) == 4 ? 1 : D <= 32 ? 4 : D == 128 ? 1 : 2, false>(a, c, q, out, s);
+  if constexpr (sizeof(T) == 4)
+    return go<D, T, 1, false>(a, c, q, out, s);
+  else if constexpr (D == 128)
+    return c.qb == 1 ? go<D, T, 1, false>(a, c, q, out, s) : go<D, T, 2, false>(a, c, q, out, s);
+  else
+    return go<D, T, D <= 32 ? 4 : 2, false>(a, c, q, out, s);
 }
 
 }  // namespace

@@ -9,9 +9,13 @@ rounding an output to bfloat16 and float32.  With A = sum |q k| |scale| of a row
               off by a = (d + 8) U A, in the exponent of 2 each operand once more (4 U A)
   weights     e^x is off by its argument's error, at most 2 a + 8 U A together with that of the
               largest (which numerator and denominator share), and 4 U of the function itself;
-              h = 2^-12 (bfloat16) or 2^-23 (float32) from storing it, at least 2^-39 of the largest
+              h = 2^-12 (bfloat16) or 2^-23 (float32) from storing it, or 2^-33 of the largest where
+              that is more: half's last step is 2^-24, weights are held times 2^8, and the score in
+              front of which they are taken is at most the largest
+  values      exact, or 2^-41 of the largest where their block is 2^22 below it
   sums        n terms in any order of lanes, tiles and splits: chains of n / 16 + 64 additions
-  out         e = 4 a + 16 U A + 16 U + h + 2 (n / 16 + 64) U, of sum p |V|, and n 2^-38 max |V|
+  out         e = 4 a + 16 U A + 16 U + h + 2 (n / 16 + 64) U, of sum p |V|, and
+              n (2^-33 + 2^-40) max |V|
   lse         2 a + 8 U A + (n / 16 + 80) U and 4 U |lse|
 """
 
@@ -253,7 +257,7 @@ def _check_attend(rng, Bn, L, H, kv, d, page, mp, lens, n_rows, dtype, causal, h
     A = (d + 8) * U * sabs
     h = 2.0 ** -12 if dtype == "bf16" else 2.0 ** -23
     e = 4 * A + 16 * U * sabs + 16 * U + h + 2 * (n / 16 + 64) * U
-    bound = e[..., None] * mag + n * 2.0 ** -38 * vmax[..., None]
+    bound = e[..., None] * mag + n * (2.0 ** -33 + 2.0 ** -40) * vmax[..., None]
     bound = bound + (B if dtype == "bf16" else U) * (np.abs(want) + bound)
     fine = np.isfinite(want) & live[..., None, None]
     nan = np.isnan(want) & live[..., None, None]
@@ -326,6 +330,38 @@ def test_attend_long(Bn, L, H, kv, d, page, lens, causal, dtype):
     pages = _table(rng, Bn, mp, Bn * mp + 1)
     host = _random_pool(rng, Bn * mp + 1, kv, page, d)
     _check_attend(rng, Bn, L, H, kv, d, page, mp, lens, None, dtype, causal, host, pages)
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("dtype,Bn,L,H,kv,page,mp,causal,pad,offset", [
+    ("bf16", 64, 70, 4, 4, 64, 3, 1, 0, 0), ("bf16", 32, 33, 16, 8, 256, 1, 1, 3, 5),
+    ("bf16", 64, 65, 4, 4, 128, 2, 0, 0, 0), ("bf16", 4, 130, 8, 8, 64, 60, 1, 8, 8),
+    ("f32", 16, 40, 8, 2, 64, 3, 1, 0, 0),
+])
+def test_attend_many_columns_of_wide_heads(dtype, Bn, L, H, kv, page, mp, causal, pad, offset, paged):
+    """d = 128 and enough rows and sequences for workgroups that read tiles together: some of their
+    waves have no columns, or fewer keys than others; sequences of no key, of one and of all; NaN codes
+    that no row looks at, and one that the last row of each sequence sees."""
+    rng = np.random.default_rng(Bn + L + page)
+    most, n_pages = mp * page, Bn * mp + 2
+    lens = rng.integers(0, most + 1, Bn)
+    lens[:4] = [most, 0, 1, most - 1][:min(4, Bn)]
+    n_rows = rng.integers(0, L + 1, Bn)
+    n_rows[:2] = L
+    pages = _table(rng, Bn, mp, n_pages, 0.1) if paged else None
+    host = _random_pool(rng, n_pages, kv, page, 128)
+    if not paged:
+        flat = np.arange(most).reshape(mp, 1, page)
+        for b in range(Bn):
+            at = slice(b * mp, (b + 1) * mp)
+            gone = np.broadcast_to(flat >= lens[b], (mp, kv, page)).copy()
+            if causal and lens[b] and b % 3 == 0:
+                gone[(lens[b] - 1) // page, 0, (lens[b] - 1) % page] = True
+            host[0][at][gone] = 0x7F
+            host[1][at] = np.where(gone[:, :, None], np.uint8(0xFF), host[1][at])
+        host[2][::5, :, 1] = rng.choice([79, 100, 150, 175], host[2][::5, :, 1].shape)
+    _check_attend(rng, Bn, L, H, kv, 128, page, mp, lens, n_rows, dtype, causal, host, pages,
+                  pad=pad, offset=offset)
 
 
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
