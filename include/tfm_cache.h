@@ -35,7 +35,7 @@ extern "C" {
  * Sequence b's row r is row r % page of the page pages[b][r / page] (pages: int32 [B][max_pages],
  * or null: page b max_pages + r / page).  A page index outside [0, n_pages) is absent: its rows are
  * neither written nor seen.  Pages may be shared by sequences that only read them; a page that an
- * append writes must belong to one sequence.
+ * append writes must belong to one sequence and stand in its table once.
  * Limits: 1 <= heads <= 4096, 1 <= n_pages <= 2^31 - 1, at most 2^46 bytes. */
 typedef struct {
   int32_t heads, d, page, n_pages;
@@ -88,10 +88,10 @@ int tfm_cache8_append(const tfm_cache8* c, const tfm_cache8_rows* r, const void*
  *
  * Rows of q and out (dtype both) lie by their strides as above; out's rows must not overlap.  out may
  * be q itself (with equal strides: in place); it shares no element with q otherwise, and none with
- * the pool, lse and the workspace.  A query row that is not finite has undefined outputs, others not.
+ * the pool, lse and the workspace.  A query row with elements of 2^127 and more, infinite or NaN has
+ * undefined outputs, others not.
  * Limits: B, L >= 0, heads a multiple of the cache's with at most 2^16 of them, L heads <= 2^26,
- * B L heads <= 2^31 - 1;
- * max_pages, strides as above; scale finite. */
+ * B L heads <= 2^31 - 1; max_pages, strides as above; scale in [-2^64, 2^64]. */
 typedef struct {
   int32_t B, L, max_pages, max_len;
   int32_t heads, causal;

@@ -139,7 +139,8 @@ int query_check(const tfm_cache8* c, const tfm_cache8_query* a, tfm::Cache8Atten
   if ((int64_t)a->L * a->heads > (1 << 26))
     return fail(TFM_ERR_DIMS, "%d rows of %d heads are more than 2^26", a->L, a->heads);
   if (a->max_len < 0) return fail(TFM_ERR_DIMS, "max_len=%d is negative", a->max_len);
-  if (!std::isfinite(a->scale)) return fail(TFM_ERR_DIMS, "scale is not finite");
+  if (!(std::fabs(a->scale) <= 0x1p64f))  // (times log2 e and a power of at most 2^48: a float32)
+    return fail(TFM_ERR_DIMS, "scale=%g outside [-2^64, 2^64]", (double)a->scale);
   const int32_t n[3] = {a->B, a->L, a->heads};
   rc = strides_check("stride_q", a->stride_q, n, c->d, false);
   if (rc) return rc;
@@ -216,8 +217,9 @@ int tfm_cache8_attend(const tfm_cache8* c, const tfm_cache8_query* a, const void
   if (q == out && !std::equal(a->stride_q, a->stride_q + 3, a->stride_out))
     return fail(TFM_ERR_POINTER, "out is q, with other strides");
   if (overlap(out, span, pool, (double)pool_size(c)) ||
-      overlap(out, span, lse, 4.0 * a->B * a->L * a->heads))
-    return fail(TFM_ERR_POINTER, "out overlaps the pool or lse");
+      overlap(out, span, lse, 4.0 * a->B * a->L * a->heads) ||
+      overlap(lse, 4.0 * a->B * a->L * a->heads, pool, (double)pool_size(c)))
+    return fail(TFM_ERR_POINTER, "one of out, the pool and lse overlaps another");
   const size_t need = tfm::cache8_attend_bytes(t, a->dtype == TFM_F32);
   if (need && !aligned(workspace, 16))
     return fail(TFM_ERR_POINTER, "workspace null or not 16-byte aligned");

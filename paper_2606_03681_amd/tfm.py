@@ -577,6 +577,9 @@ def _side_rows(call, a, name, t, dtype, width, ld):
                              f"{(a.N - 1) * ld + width} wanted")
         if t.stride(-1) != 1 and t.shape[-1] > 1:
             raise ValueError(f"{call}: the rows of {name} are {t.stride(-1)} elements a step")
+        if t.dim() == 2 and 1 < a.N == t.shape[0] and t.stride(0) != ld:
+            raise ValueError(f"{call}: the rows of {name} are {t.stride(0)} elements apart, "
+                             f"{ld} wanted")
     return name, t, dtype, None
 
 
@@ -714,7 +717,7 @@ def cache8_append(c, r, k, v, pages, lens, n_new, pool, stream=None):
              ("pages", pages, i32, (r.B, r.max_pages)), ("lens", lens, i32, (r.B,)),
              ("n_new", n_new, i32, (r.B,)), ("pool", pool, None, None))
     rc = lib().tfm_cache8_append(ctypes.byref(c), ctypes.byref(r),
-                                 *_ptrs(k, v, pages, lens, n_new, pool), pool.nbytes,
+                                 *_ptrs(k, v, pages, lens, n_new, pool), _nbytes(pool),
                                  _stream(stream))
     _check(rc)
 
@@ -736,7 +739,7 @@ def cache8_attend(c, a, q, pages, lens, n_rows, pool, out, lse, workspace, strea
              ("n_rows", n_rows, i32, (a.B,)), ("pool", pool, None, None),
              ("lse", lse, torch.float32, n), ("workspace", workspace, None, None))
     rc = lib().tfm_cache8_attend(ctypes.byref(c), ctypes.byref(a),
-                                 *_ptrs(q, pages, lens, n_rows, pool), pool.nbytes,
+                                 *_ptrs(q, pages, lens, n_rows, pool), _nbytes(pool),
                                  *_ptrs(out, lse, workspace), _nbytes(workspace), _stream(stream))
     _check(rc)
 

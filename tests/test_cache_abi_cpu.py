@@ -79,7 +79,8 @@ def test_rows_refused(kw):
 @pytest.mark.parametrize("kw", [
     dict(B=-1), dict(L=-1), dict(max_pages=-1), dict(max_pages=(1 << 30) // 64 + 1), dict(dtype=-1),
     dict(heads=0), dict(heads=3), dict(heads=(1 << 16) + 2), dict(B=1 << 16, L=1 << 15),
-    dict(B=1, L=1 << 25), dict(max_len=-1), dict(scale=NAN), dict(scale=INF), dict(stride_q=(0, -1, 0)),
+    dict(B=1, L=1 << 25), dict(max_len=-1), dict(scale=NAN), dict(scale=INF), dict(scale=-INF),
+    dict(scale=2.0 ** 64 * 1.001), dict(scale=-3e38), dict(stride_q=(0, -1, 0)),
     dict(stride_out=(5 * 128, 128, 31)), dict(stride_out=(5 * 128, 100, 32)),
     dict(stride_out=(100, 128, 32)), dict(stride_out=(0, 128, 32)),
     dict(stride_q=((1 << 40) + 1, 0, 0)),
@@ -105,7 +106,7 @@ def test_cache_pointers_and_buffers_refused():
     assert _append(k=FAR + 64) == -5 and "overlaps" in tfm.last_error()
     assert _append(v=FAR - 64) == -5
     assert _attend(out=FAR + 64) == -5 and "overlaps" in tfm.last_error()
-    assert _attend(lse=(FAKE << 8) + 4) == -5
+    assert _attend(lse=(FAKE << 8) + 4) == -5 and _attend(lse=FAR + 16) == -5
     assert _attend(a=_query(stride_q=(0, 128, 32)), out=FAKE) == -5
     lib = tfm.lib()
     c, r, a = (ctypes.byref(x) for x in (_cache(), _rows(), _query()))

@@ -316,3 +316,18 @@ def test_a_serving_loop_of_all_of_them():
     from paper_2606_03681_amd.tfm import cache8_views
     for x, y in zip(cache8_views(c, pool), host):
         assert np.array_equal(x.view(torch.uint8).cpu().numpy(), y)
+
+
+def test_adjust_refuses_rows_that_lie_otherwise_than_said():
+    import torch
+    from paper_2606_03681_amd import tfm
+    N, V = 3, 40
+    x = torch.zeros(N, V, device="cuda")
+    wide = torch.zeros(N, 8, dtype=torch.int32, device="cuda")
+    none = (None,) * 6
+    for history, ld in ((wide[:, :4], None), (wide[:, ::2], 8), (wide[:1, :4], 4), (wide, 4)):
+        a = tfm.make_adjust(N, V, V, "f32", 4, ld_history=ld)
+        with pytest.raises(ValueError, match="history"):
+            tfm.adjust_logits(a, x, None, history, None, *none, None, x)
+    a = tfm.make_adjust(N, V, V, "f32", 4, ld_history=8)
+    tfm.adjust_logits(a, x, None, wide[:, :4], None, *none, None, x)
