@@ -804,12 +804,33 @@ __global__ __launch_bounds__(256) void k_cache8_join(Cache8Attend a, T* __restri
   f32x4 o = zero4();
   if (on) {  // splits behind the last key were not written
     const int len = min(max(a.lens[b], 0), a.max_rows), live = min(splits, (len + chunk - 1) / chunk);
-    for (int s = sub; s < live; s += share) m = fmaxf(m, part_ml[(at * splits + s) * 2]);
-    for (int s = sub; s < live; s += share) {
-      const float2 ml = *reinterpret_cast<const float2*>(part_ml + (at * splits + s) * 2);
-      const float f = exp2_hw(ml.x - m);
-      l = fmaf(ml.y, f, l);
-      o += *reinterpret_cast<const f32x4*>(part + (at * splits + s) * D + d0) * f;
+    // Splits whose sums are under way at a time (references first, then sums, one after another: 12.5 us
+    // instead of 8.5 for 128 columns of 256 splits, 16.1 instead of 17.4 for 64,000 of 5).
+    constexpr int N = 8;
+    for (int s0 = sub; s0 < live; s0 += N * share) {
+      float2 ml[N];
+      f32x4 x[N];
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        const int64_t k = at * splits + min(s0 + i * share, live - 1);
+        ml[i] = *reinterpret_cast<const float2*>(part_ml + k * 2);
+        x[i] = *reinterpret_cast<const f32x4*>(part + k * D + d0);
+      }
+      float now = m;
+#pragma unroll
+      for (int i = 0; i < N; ++i)
+        if (s0 + i * share < live) now = fmaxf(now, ml[i].x);
+      const float old = exp2_hw(m - now);
+      l *= old;
+      o *= old;
+      m = now;
+#pragma unroll
+      for (int i = 0; i < N; ++i) {
+        if (s0 + i * share >= live) break;
+        const float f = exp2_hw(ml[i].x - m);
+        l = fmaf(ml[i].y, f, l);
+        o += x[i] * f;
+      }
     }
   }
   if (share > 1) {
