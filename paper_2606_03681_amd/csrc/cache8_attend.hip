@@ -118,7 +118,7 @@ struct Values {
 
 // Whether tiles go through LDS, for all four waves: where registers hold no tile beside 32 columns' sums.
 // Many columns at d = 128, bf16, pages of 64 and more (8 sequences of 1000 rows, 2000 keys, 16 heads):
-// 349 us with 16 columns and the tile in registers, 238 us staged with 32; at d = 64 the tile in
+// 349 us with 16 columns and the tile in registers, 238 us staged with 32 (keys in two pieces); at d = 64 the tile in
 // registers is the faster one (122 us, 139 us staged), as with pages under 64 (218 us, 246 us).
 template <int D, bool F32, int QB, bool SPLIT>
 constexpr bool staged() { return !SPLIT && D == 128 && !F32 && QB == 2; }
@@ -805,7 +805,7 @@ __global__ __launch_bounds__(256) void k_cache8_join(Cache8Attend a, T* __restri
   if (on) {  // splits behind the last key were not written
     const int len = min(max(a.lens[b], 0), a.max_rows), live = min(splits, (len + chunk - 1) / chunk);
     // Splits whose sums are under way at a time (references first, then sums, one after another: 12.5 us
-    // instead of 8.5 for 128 columns of 256 splits, 16.1 instead of 17.4 for 64,000 of 5).
+    // instead of 8.5 for 128 columns of 256 splits, 16.1 instead of 17.4 for 64,000 of 3).
     constexpr int N = 8;
     for (int s0 = sub; s0 < live; s0 += N * share) {
       float2 ml[N];
@@ -883,7 +883,11 @@ Cut cut_of(const Cache8Attend& a, bool f32) {
   const int per = 16 * c.qb * (c.split ? 1 : 4);
   c.coltiles = (int)((cols + per - 1) / per);
   const int64_t blocks = probs * c.coltiles, want = 2048;
-  const int least = c.split ? 512 : 1024;  // keys worth a workgroup of their own
+  // Keys worth a workgroup of their own, whose sums go through memory.  With 512 workgroups and more the
+  // CUs are full and a split only evens them out: 8 sequences of 1000 rows on 2000 keys, 16 heads, d = 64:
+  // 100 us in one piece, 127 in two; 4 of up to 1000 rows on 3000 to 5000 keys, 16 heads on 4, d = 128:
+  // 254 us in one piece, 223 in two, 209 in three.
+  const int least = c.split ? 512 : blocks >= 512 ? 2048 : 1024;
   int64_t s = blocks > 0 ? (want + blocks - 1) / blocks : 1;
   s = s < (keys + least - 1) / least ? s : (keys + least - 1) / least;
   if (s < 1) s = 1;
