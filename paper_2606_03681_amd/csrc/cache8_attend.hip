@@ -15,21 +15,27 @@
 // Row m of the t-th of the tile's four 16-row products is key 16 (m / 4) + 4 t + m % 4, so that a lane's
 // 16 scores are those of 16 keys in a row: one block's, since pages are multiples of 16, and in the
 // order in which the lane reads 16 bytes of V^T.  Nothing moves between lanes, and codes go from memory
-// to registers without LDS.
+// to registers without LDS (but see staged()).
 //
 // p is held as half with 2^8 in front: 2^-12 of each weight, and 2^-33 of the largest where half has no
 // more bits (bfloat16 would have doubled the output's own rounding error).  The reference is looked at
 // only where a lane's weights sum to more than half can hold, the first tile's among them, whose
 // reference is the lowest float: then it becomes the largest score, the sums are rescaled and the tile
-// weighed again.  With the largest score as reference 16 weights sum to at most 2^12, and a later score
-// may be up to 2^7 of it, so that this is rare, and other tiles need no maximum.  Values are held with 2^7 in front: exact unless their block is
-// 2^22 below the largest, 2^-41 of that one's largest code then.  Float32 queries are three bfloat16
-// parts (24 bits) and their weights two halves.
+// weighed again.  With the largest score as reference 16 weights sum to at most 2^12, and a later one
+// may be up to 2^7 of it, so that this is rare, and other tiles need no maximum.  Values are held with
+// 2^7 in front: exact unless their block is 2^22 below the largest, 2^-41 of that one's largest code
+// then.  Float32 queries are three bfloat16 parts (24 bits) and their weights two halves.
 //
 // Few columns (SPLIT): the four waves of a workgroup share the columns and take turns over the tiles;
 // many: each wave has columns of its own.  A tile's keys are read while the one before it is weighed
-// and summed, its values from then on.  Where the workgroups are too
-// few the keys are split over more of them, and a second launch joins their sums.
+// and summed, its values from then on.  Where the workgroups are too few the keys are split over more
+// of them, and a second launch joins their sums.
+//
+// Bounds and figures.  Few columns: the codes' bytes; 64 sequences of 1 to 16,384 rows, one row of 32
+// heads on 8, d = 128: 207 us, 5.2 TB/s.  Many columns: vector instructions, 445 of a wave and tile at
+// d = 32 and 64 columns (64 exponentials at two issue slots each, scores to weights, codes to
+// bfloat16 and half), 32 matrix instructions beside them; 1616 sequences of 768 rows, 256 rows of 6
+// heads, d = 32: 445 us, 550 TFLOP/s, the vector units 83 to 95 % busy.
 #include <float.h>
 
 #include "cache8.h"
@@ -122,17 +128,16 @@ struct Values {
 // registers is the faster one (122 us, 139 us staged), as with pages under 64 (218 us, 246 us).
 template <int D, bool F32, int QB, bool SPLIT>
 constexpr bool staged() { return !SPLIT && D == 128 && !F32 && QB == 2; }
-// Waves per SIMD that the registers of a kernel leave room for.
+// Waves per SIMD that the registers of a kernel leave room for.  (Three at D <= 32: 476 us for the 1616
+// sequences above with two, 442 with three, queries in LDS for it.)
 template <int D, bool F32, int QB, bool SPLIT>
 constexpr int waves() { return D <= 32 && QB == 4 ? 3 : D == 128 && QB == 2 && SPLIT ? 1 : 2; }
 
 template <int D, class T, int QB, bool SPLIT, bool UNI>
-__global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void k_cache8_attend(Cache8Attend a, const T* __restrict__ q,
-                                                       T* __restrict__ out, float* __restrict__ part,
-                                                       float* __restrict__ part_ml, uint32_t prob0,
-                                                       uint32_t nprob,
-                                                       int coltiles, int splits, int chunk,
-                                                       int wide) {
+__global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void k_cache8_attend(
+    Cache8Attend a, const T* __restrict__ q, T* __restrict__ out, float* __restrict__ part,
+    float* __restrict__ part_ml, uint32_t prob0, uint32_t nprob, int coltiles, int splits, int chunk,
+    int wide) {
   constexpr int DB = D / 16, CH = KQ<D>::CH, KW = D / 16;  // KW: dwords of a key per lane
   constexpr bool F32 = sizeof(T) == 4;
   constexpr int NQ = F32 ? 3 : 1, NP = F32 ? 2 : 1;
@@ -871,8 +876,9 @@ Cut cut_of(const Cache8Attend& a, bool f32) {
   const int64_t cols = (int64_t)a.L * (a.heads / a.g.heads), probs = (int64_t)a.plan_B * a.g.heads;
   const int64_t keys = a.plan_rows;
   c.split = cols <= 32;
-  c.qb = c.split ? (cols <= 16 ? 1 : 2)
-                 : f32 ? 1 : a.g.d <= 32 ? 4 : 2;
+  // (Columns of a wave: as many as its registers hold.  d = 128, 16 heads on 4, 4 sequences of up to
+  // 1000 rows: 288 us with 32, spilled or one wave a SIMD, 207 with 16 and two.)
+  c.qb = c.split ? (cols <= 16 ? 1 : 2) : f32 ? 1 : a.g.d <= 32 ? 4 : 2;
   if (!c.split && c.qb == 2 && a.g.d == 128) {
     // Staged tiles, whose workgroups take 128 columns instead of 64, need one for every CU: 8 heads,
     // 1024 rows on 1100 keys, 1 / 2 / 4 sequences (128 / 256 / 512 workgroups): 36 / 39 / 48 us staged,
