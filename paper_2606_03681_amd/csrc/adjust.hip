@@ -5,6 +5,12 @@
 // meanwhile, applies it: for each class a word with how often it occurs in the history (low half) and
 // the complement of its first bias entry (high half), or two words where either may not fit 16 bits.
 // Integers: no order matters.  A slice whose row has neither history nor biases has no such words.
+//
+// Bound: HBM for long rows without much to note, else latency.  64 rows of 131,072 bfloat16 classes,
+// each with up to 8192 earlier tokens, 32 biases and a mask: 20 us (7 of bytes; each of a row's 32 slices
+// reads its whole history, from the caches, and counts with atomics in LDS); one row of 32,000 float32
+// classes: 6 us, launch and three dependent loads.  With two words for each class in all cases (half as
+// many workgroups to a CU) and the logits read behind the notes the 64 rows took 28 us.
 #include "mfma.h"
 #include "vocab.h"
 
@@ -206,12 +212,32 @@ __global__ __launch_bounds__(256, PACK ? 8 : 4) void k_adjust(AdjustGeo g, const
   }
 }
 
-// R whole rows, R V <= SLICE.
+// R whole rows, R V <= SLICE / 4 and, where R > 1, R n_hist and R n_bias at most SLICE.
+constexpr int MOST_ROWS = 64;
 template <class T>
 __global__ __launch_bounds__(256) void k_adjust_rows(AdjustGeo g, const T* logits, T* out, int R,
                                                      int64_t items) {
-  __shared__ uint32_t seen[SLICE], first[SLICE];
+  __shared__ uint32_t seen[SLICE / 4], first[SLICE / 4];
+  __shared__ int said[MOST_ROWS];
   const int tid = threadIdx.x, V = g.V;
+  // f(r, j) for j < n of each row r, four loads of it under way at a time; then(r, j, its value)
+  auto each = [&](int rows, uint32_t n, auto f, auto then) {
+    const uint32_t total = rows * n;
+    for (uint32_t i0 = tid; i0 < total; i0 += 1024) {
+      uint32_t r[4], v[4];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t i = min(i0 + k * 256, total - 1);
+        r[k] = i / n;
+        v[k] = f(r[k], i - r[k] * n);
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const uint32_t i = i0 + k * 256;
+        if (i < total) then(r[k], i - r[k] * n, v[k]);
+      }
+    }
+  };
   for (int64_t it = blockIdx.x; it < items; it += gridDim.x) {
     const int64_t n0 = it * R;
     const int rows = (int)min((int64_t)R, g.N - n0), w = rows * V;
@@ -219,20 +245,24 @@ __global__ __launch_bounds__(256) void k_adjust_rows(AdjustGeo g, const T* logit
     if (any) {
       __syncthreads();
       for (int i = tid; i < w; i += 256) seen[i] = 0, first[i] = NONE;
+      if (tid < rows) said[tid] = said_of(g, n0 + tid);
       __syncthreads();
-      if (g.history) {
-        for (int64_t i = tid; i < (int64_t)rows * g.n_hist; i += 256) {
-          const int r = (int)(i / g.n_hist), j = (int)(i - (int64_t)r * g.n_hist);
-          if (j >= said_of(g, n0 + r)) continue;
-          const uint32_t v = (uint32_t)g.history[(n0 + r) * g.ld_history + j];
-          if (v < (uint32_t)V) atomicAdd(&seen[r * V + v], 1u);
-        }
-      }
-      for (int64_t i = tid; i < (int64_t)rows * g.n_bias; i += 256) {
-        const int r = (int)(i / g.n_bias), j = (int)(i - (int64_t)r * g.n_bias);
-        const uint32_t v = (uint32_t)g.bias_idx[(n0 + r) * g.ld_bias + j];
-        if (v < (uint32_t)V) atomicMin(&first[r * V + v], (uint32_t)j);
-      }
+      if (g.history)
+        each(
+            rows, g.n_hist,
+            [&](int r, int j) {
+              return j < said[r] ? (uint32_t)g.history[(n0 + r) * g.ld_history + j] : NONE;
+            },
+            [&](int r, int, uint32_t v) {
+              if (v < (uint32_t)V) atomicAdd(&seen[r * V + v], 1u);
+            });
+      if (g.n_bias > 0)
+        each(
+            rows, g.n_bias,
+            [&](int r, int j) { return (uint32_t)g.bias_idx[(n0 + r) * g.ld_bias + j]; },
+            [&](int r, int j, uint32_t v) {
+              if (v < (uint32_t)V) atomicMin(&first[r * V + v], (uint32_t)j);
+            });
       __syncthreads();
     }
     for (int i = tid; i < w; i += 256) {
@@ -252,7 +282,11 @@ __global__ __launch_bounds__(256) void k_adjust_rows(AdjustGeo g, const T* logit
 template <class T>
 hipError_t launch_adjust(const AdjustGeo& g, const T* logits, T* out, hipStream_t s) {
   if (g.V <= SLICE / 4) {
-    const int R = SLICE / 4 / g.V < 64 ? SLICE / 4 / g.V : 64;
+    // (883 rows of 4 classes, 2764 earlier ones each: 191 us with as many rows as there is room for, on
+    // 14 workgroups, 12 with one)
+    const int note = g.n_hist > g.n_bias ? g.n_hist : g.n_bias;
+    int R = SLICE / 4 / g.V < MOST_ROWS ? SLICE / 4 / g.V : MOST_ROWS;
+    if ((int64_t)R * note > SLICE) R = SLICE / note > 1 ? SLICE / note : 1;
     const int64_t items = (g.N + R - 1) / R;
     k_adjust_rows<T><<<(unsigned)(items < kMaxBlocks ? items : kMaxBlocks), 256, 0, s>>>(
         g, logits, out, R, items);
