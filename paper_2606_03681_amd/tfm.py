@@ -117,6 +117,12 @@ def make_sampling(N, V, ld, dtype):
     return tfm_sampling(int(N), int(V), int(_DTYPES.get(dtype, dtype)), int(ld))
 
 
+# packed, these structures take half the time that filling their fields does (1.2 and 2.8 us)
+_ADJUST = struct.Struct("5i5q")
+_ROWS = struct.Struct("4i3q3q")
+_QUERY = struct.Struct("7if3q3q")
+
+
 class tfm_adjust(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("N", "V", "dtype", "n_hist", "n_bias")] + \
         [(n, ctypes.c_int64) for n in ("ld", "ld_out", "ld_history", "ld_bias", "ld_allowed")]
@@ -125,12 +131,10 @@ class tfm_adjust(ctypes.Structure):
 def make_adjust(N, V, ld, dtype, n_hist=0, n_bias=0, ld_out=None, ld_history=None, ld_bias=None,
                 ld_allowed=None):
     """Elements between the rows of each array: ld_out like ld, the others side by side if None."""
-    V, n_hist, n_bias = int(V), int(n_hist), int(n_bias)
-    return tfm_adjust(int(N), V, int(_DTYPES.get(dtype, dtype)), n_hist, n_bias, int(ld),
-                      int(ld if ld_out is None else ld_out),
-                      n_hist if ld_history is None else int(ld_history),
-                      n_bias if ld_bias is None else int(ld_bias),
-                      (V + 31) // 32 if ld_allowed is None else int(ld_allowed))
+    return tfm_adjust.from_buffer_copy(_ADJUST.pack(
+        N, V, _DTYPES.get(dtype, dtype), n_hist, n_bias, ld, ld if ld_out is None else ld_out,
+        n_hist if ld_history is None else ld_history, n_bias if ld_bias is None else ld_bias,
+        (V + 31) // 32 if ld_allowed is None else ld_allowed))
 
 
 class tfm_cache8(ctypes.Structure):
@@ -144,11 +148,6 @@ def make_cache8(heads, d, page, n_pages):
 class tfm_cache8_rows(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in ("B", "L", "max_pages", "dtype")] + \
         [(n, ctypes.c_int64 * 3) for n in ("stride_k", "stride_v")]
-
-
-# packed, these structures take half the time that filling their fields does (1.2 and 2.8 us)
-_ROWS = struct.Struct("4i3q3q")
-_QUERY = struct.Struct("7if3q3q")
 
 
 def make_cache8_rows(B, L, max_pages, dtype, stride_k, stride_v):
@@ -570,7 +569,7 @@ def _embed_rows(call, e, name, t):
 
 def _side_rows(call, a, name, t, dtype, width, ld):
     """Rows of what goes with a row of logits, ld elements apart: room for the last."""
-    if t is not None and a.N and width:
+    if t is not None and a.N and width and not (t.shape == (a.N, width) and t.stride() == (ld, 1)):
         room = t.untyped_storage().nbytes() // t.element_size() - t.storage_offset()
         if (a.N - 1) * ld + width > room:
             raise ValueError(f"{call}: {name} has room for {room} elements, "
