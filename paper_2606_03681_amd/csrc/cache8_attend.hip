@@ -20,8 +20,8 @@
 // p is held as half with 2^8 in front: 2^-12 of each weight, and 2^-33 of the largest where half has no
 // more bits (bfloat16 would have doubled the output's own rounding error).  The reference is looked at
 // only where a lane's weights sum to more than half can hold, the first tile's among them, whose
-// reference is the lowest float: then it becomes the largest score, the sums are rescaled and the tile
-// weighed again.  With the largest score as reference 16 weights sum to at most 2^12, and a later one
+// reference is the lowest float: then it becomes its column's largest score, the column's sums are
+// rescaled and the tile weighed again.  With the largest score as reference 16 weights sum to at most 2^12, and a later one
 // may be up to 2^7 of it, so that this is rare, and other tiles need no maximum.  Values are held with
 // 2^7 in front: exact unless their block is 2^22 below the largest, 2^-41 of that one's largest code
 // then.  Float32 queries are three bfloat16 parts (24 bits) and their weights two halves.
@@ -411,7 +411,10 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
 #pragma unroll
       for (int t = 1; t < 4; ++t)
         mx = fmaxf(mx, fmaxf(fmaxf(s[t][0], s[t][1]), fmaxf(s[t][2], s[t][3])));
-      const float now = fmaxf(ref[qb], rows4_max(mx * cs));
+      // (of the columns that need it alone: a row's bits do not depend on the rows beside it)
+      const bool more = rows4_max(sum <= P_MOST ? 0.f : 1.f) > 0.f;
+      mx = rows4_max(mx * cs);
+      const float now = more ? fmaxf(ref[qb], mx) : ref[qb];
       if (!first) {
         const float corr = exp2_hw(ref[qb] - now);
         lsum[qb] *= corr;

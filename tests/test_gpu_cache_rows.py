@@ -1,0 +1,88 @@
+"""What a row of cached attention depends on: itself and what it attends to, whatever the rows beside
+it are (include/tfm_cache.h), bit for bit where the sizes are the same."""
+
+import numpy as np
+import pytest
+
+from oracle import cache as oc
+from paper_2606_03681_amd import workloads as wl
+
+from test_gpu_cache import _dev, _ints, _pool_to_device
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.fail("no GPU visible")
+    from paper_2606_03681_amd import tfm
+    tfm.lib()
+
+
+def _neighbours(q, row, how, keys):
+    """q with every row but one replaced."""
+    x = {"none": np.zeros_like(q), "rising": np.broadcast_to(np.abs(q) * 4, q.shape),
+         "falling": -np.abs(q) * 4, "nan": np.full_like(q, np.nan), "huge": np.full_like(q, 1e37)}[how]
+    x = x.copy()
+    x[:, row] = q[:, row]
+    return x
+
+
+@pytest.mark.parametrize("Bn,L,H,kv,d,page,n,dtype,causal", [
+    (1, 5, 4, 2, 32, 16, 700, "f32", 0), (1, 5, 4, 2, 64, 64, 700, "bf16", 1),
+    (1, 20, 1, 1, 128, 32, 700, "bf16", 0), (2, 9, 6, 2, 16, 64, 1500, "bf16", 1),
+    (1, 70, 2, 2, 16, 64, 700, "bf16", 0), (2, 60, 4, 4, 32, 64, 700, "bf16", 0),
+    (1, 60, 2, 1, 32, 16, 700, "bf16", 1), (1, 50, 2, 1, 64, 64, 700, "bf16", 0),
+    (1, 50, 2, 1, 64, 256, 700, "f32", 1), (1, 40, 2, 1, 128, 64, 700, "bf16", 1),
+    (64, 70, 4, 4, 128, 64, 180, "bf16", 0),                  # tiles that a workgroup reads together
+])
+def test_a_row_does_not_see_the_rows_beside_it(Bn, L, H, kv, d, page, n, dtype, causal):
+    """Keys that grow along the sequence: the neighbours' references move at every tile, or at none."""
+    import torch
+    from paper_2606_03681_amd import tfm
+    rng = np.random.default_rng(L + d + page)
+    mp = -(-n // page)
+    size = np.broadcast_to(np.linspace(0.02, 1, mp * page)[:, None], (mp * page, d))
+    size = np.broadcast_to(size.reshape(mp, 1, page, d), (mp, kv, page, d))
+    host = (oc.encode(size * 440), oc.encode(np.clip(rng.normal(size=(mp, kv, d, page)) * 100, -448, 448)),
+            np.broadcast_to(np.uint8([119, 120]), (mp, kv, 2)).copy())
+    c = tfm.make_cache8(kv, d, page, mp)
+    pool = _pool_to_device(*host)
+    pages, lens = _ints(np.broadcast_to(np.arange(mp), (Bn, mp))), _ints([n] * Bn)
+    q = rng.normal(size=(Bn, L, H, d))
+    row = L // 2
+    first = None
+    for how in ("none", "rising", "falling", "nan", "huge"):
+        qt = _dev(_neighbours(q, row, how, size), dtype)
+        a = tfm.make_cache8_query(Bn, L, H, mp, dtype, qt.stride()[:3], qt.stride()[:3], 1.0, causal)
+        ws = torch.empty(tfm.cache8_attend_workspace_bytes(c, a), dtype=torch.uint8, device="cuda")
+        out, lse = torch.empty_like(qt), torch.empty((Bn, L, H), device="cuda")
+        tfm.cache8_attend(c, a, qt, pages, lens, None, pool, out, lse, ws)
+        got = out[:, row].clone(), lse[:, row].clone()
+        assert bool(torch.isfinite(got[0]).all()) and bool(torch.isfinite(got[1]).all())
+        first = first or got
+        assert torch.equal(first[0], got[0]) and torch.equal(first[1], got[1]), how
+
+
+@pytest.mark.parametrize("name", ["ragged-small-bf16", "d16-bf16", "d64-bf16", "prenorm-d64-bf16"])
+def test_a_query_row_does_not_see_the_rows_beside_it(name):
+    import torch
+    from paper_2606_03681_amd import tfm
+    from paper_2606_03681_amd.stack import InferStack, to_device
+    w = wl.make_workload(name)
+    R = w.cfg["R"]
+    Rc = R - (R // 3 + 5)
+    n_train = np.minimum(w.n_train, Rc).astype(np.int32)
+    dims = tfm.make_dims(dtype=w.dtype, block=w.block, R=Rc,
+                         **{k: v for k, v in w.dims.items() if k not in ("dtype", "R")})
+    st = InferStack(dims, n_train, w.cell_mask, w.params, max_query_rows=R - Rc, cache8=True)
+    st.context(to_device(np.ascontiguousarray(w.X[:, :Rc]), "bf16"))
+    X = to_device(np.ascontiguousarray(w.X[:, Rc:]), "bf16")
+    row = X.shape[1] // 2
+    want = st.query(X)[:, row].clone()
+    for by in (0.0, 50.0, float("nan")):
+        Y = X * by
+        Y[:, row] = X[:, row]
+        assert torch.equal(st.query(Y)[:, row], want), by
