@@ -135,7 +135,7 @@ constexpr int waves() { return D <= 32 && QB == 4 ? 3 : D == 128 && QB == 2 && S
 
 template <int D, class T, int QB, bool SPLIT, bool UNI>
 __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void k_cache8_attend(
-    Cache8Attend a, const T* __restrict__ q, T* __restrict__ out, float* __restrict__ part,
+    Cache8Attend a, const T* q, T* out /* may be q */, float* __restrict__ part,
     float* __restrict__ part_ml, uint32_t prob0, uint32_t nprob, int coltiles, int splits, int chunk,
     int wide) {
   constexpr int DB = D / 16, CH = KQ<D>::CH, KW = D / 16;  // KW: dwords of a key per lane
@@ -206,6 +206,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   const bool neg = a.scale_log2 < 0;
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
+    if (STAGE && col0 >= ncols) break;  // (the last column is another wave's, which may write it in place)
     const int col = min(col0 + qb * 16 + c, ncols - 1), i = row_of(col), h = kh * G + col - i * G;
     const T* p = q + b * a.sq[0] + i * a.sq[1] + h * a.sq[2] + lg * (D / 4);
     uint16_t e[NQ][D / 4];

@@ -7,7 +7,7 @@ import pytest
 from oracle import cache as oc
 from paper_2606_03681_amd import workloads as wl
 
-from test_gpu_cache import _dev, _ints, _pool_to_device
+from test_gpu_cache import _dev, _in_buffer, _ints, _pool_to_device, _random_pool
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +86,32 @@ def test_a_query_row_does_not_see_the_rows_beside_it(name):
         Y = X * by
         Y[:, row] = X[:, row]
         assert torch.equal(st.query(Y)[:, row], want), by
+
+
+@pytest.mark.parametrize("Bn,L,H,kv,d,page,n,dtype,causal,pad", [
+    (64, 70, 4, 4, 128, 64, 180, "bf16", 1, 0),       # tiles that a workgroup reads together
+    (64, 70, 4, 4, 128, 64, 0, "bf16", 0, 0),         # without a key
+    (64, 130, 4, 4, 128, 128, 100, "bf16", 0, 5),     # on no vector's boundary
+    (2, 40, 4, 2, 128, 32, 3000, "bf16", 1, 0), (2, 3, 8, 2, 64, 64, 5000, "bf16", 0, 0),
+    (1, 50, 2, 1, 64, 64, 5000, "f32", 1, 1), (3, 1, 4, 1, 16, 16, 2000, "f32", 0, 0),
+    (3, 20, 2, 2, 32, 256, 700, "f32", 1, 0), (1, 140, 3, 3, 32, 64, 4000, "bf16", 0, 0),
+])
+def test_in_place(Bn, L, H, kv, d, page, n, dtype, causal, pad):
+    """out = q gives the bits of an output elsewhere: keys in one piece or in several."""
+    import torch
+    from paper_2606_03681_amd import tfm
+    rng = np.random.default_rng(Bn + L + d)
+    mp = max(1, -(-n // page))
+    host = _random_pool(rng, mp, kv, page, d)
+    c, pool = tfm.make_cache8(kv, d, page, mp), _pool_to_device(*host)
+    pages = _ints(np.broadcast_to(np.arange(mp), (Bn, mp)))
+    lens, n_rows = _ints(rng.integers(n // 2, n + 1, Bn)), _ints(rng.integers(0, L + 1, Bn))
+    x = rng.normal(size=(Bn, L, H, d))
+    whole, q, stride = _in_buffer(x, dtype, pad, pad)
+    a = tfm.make_cache8_query(Bn, L, H, mp, dtype, stride, stride, 0.2, causal)
+    ws = torch.empty(tfm.cache8_attend_workspace_bytes(c, a), dtype=torch.uint8, device="cuda")
+    apart = whole.clone()
+    out = apart[pad:].as_strided(q.shape, q.stride())
+    tfm.cache8_attend(c, a, q, pages, lens, n_rows, pool, out, None, ws)
+    tfm.cache8_attend(c, a, q, pages, lens, n_rows, pool, q, None, ws)
+    assert torch.equal(whole, apart)
