@@ -214,7 +214,9 @@ __global__ __launch_bounds__(256) void k_cache8_append(Cache8Append a, const T* 
 template <class T>
 hipError_t launch_cache8_append(const Cache8Append& a, const T* k, const T* v, hipStream_t s) {
   const Cache8Geo& g = a.g;
-  const int slots = (int)(((int64_t)a.L + g.page - 2) / g.page + 1);
+  // Pages that a sequence's rows may touch, of those that it has.
+  const int64_t touched = ((int64_t)a.L + g.page - 2) / g.page + 1;
+  const int slots = (int)(touched < g.max_pages ? touched : g.max_pages);
   const int64_t items = (int64_t)a.B * slots * g.heads;
   bool wide = (uintptr_t)k % 16 == 0 && (uintptr_t)v % 16 == 0;
   for (int i = 0; i < 3; ++i)

@@ -1,5 +1,5 @@
-"""What a row of cached attention depends on: itself and what it attends to, whatever the rows beside
-it are (include/tfm_cache.h), bit for bit where the sizes are the same."""
+"""What calls on an 8-bit cache (include/tfm_cache.h) depend on and do not: rows beside a row, in place
+or not, more rows than there is room for."""
 
 import numpy as np
 import pytest
@@ -7,7 +7,8 @@ import pytest
 from oracle import cache as oc
 from paper_2606_03681_amd import workloads as wl
 
-from test_gpu_cache import _dev, _in_buffer, _ints, _pool_to_device, _random_pool
+from test_gpu_cache import (_dev, _in_buffer, _ints, _pool_to_device, _pool_to_host,
+                            _random_pool)
 
 pytestmark = pytest.mark.gpu
 
@@ -115,3 +116,25 @@ def test_in_place(Bn, L, H, kv, d, page, n, dtype, causal, pad):
     tfm.cache8_attend(c, a, q, pages, lens, n_rows, pool, out, None, ws)
     tfm.cache8_attend(c, a, q, pages, lens, n_rows, pool, q, None, ws)
     assert torch.equal(whole, apart)
+
+
+@pytest.mark.parametrize("heads,page,max_pages,L,first,n_new", [
+    (4096, 16, 1, 2 ** 31 - 1, 0, None), (4096, 16, 3, 2 ** 31 - 1, 17, None),
+    (8, 256, 2, 2 ** 31 - 1, 500, 2 ** 31 - 1), (64, 64, 2, 10 ** 6, 0, 3),
+])
+def test_append_of_more_rows_than_the_table_has_room_for(heads, page, max_pages, L, first, n_new):
+    """One row, broadcast to a number of rows far past the sequence's pages: those that have room."""
+    from paper_2606_03681_amd import tfm
+    rng = np.random.default_rng(heads + max_pages)
+    host = _random_pool(rng, max_pages, heads, page, 16, (90, 91))
+    c, pool = tfm.make_cache8(heads, 16, page, max_pages), _pool_to_device(*host)
+    x = rng.normal(size=16).astype(np.float32)
+    r = tfm.make_cache8_rows(1, L, max_pages, "f32", (0, 0, 0), (0, 0, 0))
+    t = _dev(x)
+    tfm.cache8_append(c, r, t, t, None, _ints([first]), None if n_new is None else _ints([n_new]), pool)
+    n = min(max_pages * page - first, L if n_new is None else n_new)
+    rows = np.broadcast_to(x.astype(float), (1, n, 1, 16))
+    for h in (0, heads // 2, heads - 1):
+        want = oc.append(*(p[:, h:h + 1] for p in host), rows, rows, max_pages, None, [first])
+        for a, b in zip(_pool_to_host(c, pool), want):
+            assert np.array_equal(a[:, h:h + 1], b)
