@@ -81,15 +81,15 @@ int tfm_cache8_append(const tfm_cache8* c, const tfm_cache8_rows* r, const void*
  * to [0, max_pages page], n_rows to [0, L].  max_len is a promise that no sequence is longer: it
  * chooses how the rows of a cache are split over workgroups.
  *
- * Scores, statistics and sums are held in float32.  Codes are exact as bfloat16 (keys) and half
+ * Scores, statistics and sums are held in float32, as is scale log2(e).  Codes are exact as bfloat16 (keys) and half
  * (values of blocks less than 2^22 below the row's largest); a float32 query goes in three bfloat16
  * parts whose sum it is.  Weights are rounded to half (by 2^-12 of each, or 2^-33 of the row's largest
  * where that is more), with a float32 output to two halves (2^-23).
  *
  * Rows of q and out (dtype both) lie by their strides as above; out's rows must not overlap.  out may
  * be q itself (with equal strides: in place); it shares no element with q otherwise, and none with
- * the pool, lse and the workspace.  A query row with elements of 2^127 and more, infinite or NaN has
- * undefined outputs, others not.
+ * the pool, lse and the workspace.  A query row with elements of 2^112 and more, infinite or NaN, or
+ * with a score of 2^127 and more has undefined outputs, others not.
  * Limits: B, L >= 0, heads a multiple of the cache's with at most 2^16 of them, L heads <= 2^26,
  * B L heads <= 2^31 - 1; max_pages, strides as above; scale in [-2^64, 2^64]. */
 typedef struct {

@@ -432,7 +432,9 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   auto compute = [&](Keys<D>& x, Values<D>& y, int t0, int only, auto codes_read) {
     const int ek = power_byte(x.power & 0xff), ev = power_byte(x.power >> 8);
     const bool here = x.here && (UNI || only < 0 || lg == only);
-    const float cs = fmaxf(scale * exp2i(ek - 127), 0x1p-126f);
+    // (not 0, by which a masked score, -inf, could not be multiplied; a score of queries below 2^112 is
+    // below 2^128 before it, so that the least factor adds at most 2^-21 to an exponent)
+    const float cs = fmaxf(scale * exp2i(ek - 127), 0x1p-149f);
     const bool partial = t0 + KT > lo || __any(!here);
     int top = ev;
     bool dirty = false;  // a staged tile has NaN codes that its readers leave out

@@ -8,9 +8,10 @@ from oracle import cache as oc
 from paper_2606_03681_amd import workloads as wl
 
 from test_gpu_cache import (_dev, _in_buffer, _ints, _pool_to_device, _pool_to_host,
-                            _random_pool)
+                            _random_pool, _rounded)
 
 pytestmark = pytest.mark.gpu
+U = 2.0 ** -24
 
 
 @pytest.fixture(scope="module", autouse=True)
@@ -138,3 +139,38 @@ def test_append_of_more_rows_than_the_table_has_room_for(heads, page, max_pages,
         want = oc.append(*(p[:, h:h + 1] for p in host), rows, rows, max_pages, None, [first])
         for a, b in zip(_pool_to_host(c, pool), want):
             assert np.array_equal(a[:, h:h + 1], b)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("d,page,L", [(16, 16, 1), (32, 64, 40), (64, 16, 3), (128, 64, 40)])
+@pytest.mark.parametrize("size,scale,power", [
+    (2.0 ** 111, 0.0, 127), (2.0 ** 111, -2.0 ** -100, 79), (2.0 ** 111, 2.0 ** -125, 127),
+    (1.9 * 2.0 ** 110, 2.0 ** -119, 128), (2.0 ** 111, 2.0 ** -74, 79), (2.0 ** -40, 2.0 ** 64, 79),
+    (2.0 ** -60, -2.0 ** 20, 150),
+])
+def test_scales_of_huge_and_tiny_queries(d, page, L, size, scale, power, dtype):
+    """Queries up to the largest allowed, at factors of the score down to 0.  Bounds of test_gpu_cache.py
+    with h = 2^-11 (bfloat16), the largest error of rounding to half, and 2^-21 for the least factor."""
+    import torch
+    from paper_2606_03681_amd import tfm
+    rng = np.random.default_rng(d + L)
+    n = 300
+    mp = -(-n // page)
+    host = _random_pool(rng, mp, 1, page, d, (power, power + 1))
+    host[0][0, 0, :8] = 0x7E                                   # 448 in every channel
+    q = _rounded(rng.uniform(0.5, 1, size=(1, L, 2, d)) * size, dtype)
+    c, pool = tfm.make_cache8(1, d, page, mp), _pool_to_device(*host)
+    qt = _dev(q, dtype)
+    a = tfm.make_cache8_query(1, L, 2, mp, dtype, qt.stride()[:3], qt.stride()[:3], scale)
+    ws = torch.empty(tfm.cache8_attend_workspace_bytes(c, a), dtype=torch.uint8, device="cuda")
+    out, lse = torch.empty_like(qt), torch.empty((1, L, 2), device="cuda")
+    tfm.cache8_attend(c, a, qt, None, _ints([n]), None, pool, out, lse, ws)
+    want, want_lse, mag, sabs, vmax = oc.attend(q, *host, mp, None, [n], None, scale, False)
+    A = (d + 8) * U * sabs
+    rounding = {"bf16": (2.0 ** -11, 2.0 ** -8), "f32": (2.0 ** -23, U)}[dtype]
+    e = 4 * A + 16 * U * sabs + 16 * U + rounding[0] + 2 * (n / 16 + 64) * U + 2 * 2.0 ** -21
+    bound = e[..., None] * mag + n * (2.0 ** -33 + 2.0 ** -40) * vmax[..., None]
+    bound = bound + rounding[1] * (np.abs(want) + bound)
+    assert np.all(np.abs(out.double().cpu().numpy() - want) <= bound)
+    lb = 2 * A + 8 * U * sabs + (n / 16 + 80) * U + 4 * U * np.abs(want_lse) + 2.0 ** -21
+    assert np.all(np.abs(lse.double().cpu().numpy() - want_lse) <= lb)
