@@ -352,8 +352,8 @@ def layer_fwd(dims, n_train, cell_mask, X, params, Y, saved, workspace, stream=N
     nt, ntp = _host(n_train, np.int32)
     cm, cmp_ = _host(cell_mask, np.uint8)
     rc = lib().tfm_layer_fwd(ctypes.byref(dims), ntp, cmp_, _ptr(X), _ptr(params), _ptr(Y),
-                             _ptr(saved), saved.numel() * saved.element_size(),
-                             _ptr(workspace), workspace.numel() * workspace.element_size(),
+                             _ptr(saved), _nbytes(saved),
+                             _ptr(workspace), _nbytes(workspace),
                              _stream(stream))
     _check(rc)
 
@@ -364,7 +364,7 @@ def layer_fwd_noalloc(dims, n_train, cell_mask, X, params, Y, saved, stream=None
     nt, ntp = _host(n_train, np.int32)
     cm, cmp_ = _host(cell_mask, np.uint8)
     rc = lib().tfm_layer_fwd_noalloc(ctypes.byref(dims), ntp, cmp_, _ptr(X), _ptr(params),
-                                     _ptr(Y), _ptr(saved), saved.numel() * saved.element_size(),
+                                     _ptr(Y), _ptr(saved), _nbytes(saved),
                                      _stream(stream))
     _check(rc)
 
@@ -375,9 +375,9 @@ def layer_bwd(dims, n_train, cell_mask, X, params, saved, dY, dX, grads, accumul
     nt, ntp = _host(n_train, np.int32)
     cm, cmp_ = _host(cell_mask, np.uint8)
     rc = lib().tfm_layer_bwd(ctypes.byref(dims), ntp, cmp_, _ptr(X), _ptr(params), _ptr(saved),
-                             saved.numel() * saved.element_size(), _ptr(dY), _ptr(dX),
+                             _nbytes(saved), _ptr(dY), _ptr(dX),
                              _ptr(grads), int(bool(accumulate)), _ptr(workspace),
-                             workspace.numel() * workspace.element_size(), _stream(stream))
+                             _nbytes(workspace), _stream(stream))
     _check(rc)
 
 
@@ -388,7 +388,7 @@ def thinking_rows_fwd(dims, n_train, cell_mask, T, table, X, workspace, stream=N
     cm, cmp_ = _host(cell_mask, np.uint8)
     rc = lib().tfm_thinking_rows_fwd(ctypes.byref(dims), ntp, cmp_, int(T), _ptr(table), _ptr(X),
                                      _ptr(workspace),
-                                     workspace.numel() * workspace.element_size(),
+                                     _nbytes(workspace),
                                      _stream(stream))
     _check(rc)
 
@@ -401,13 +401,19 @@ def thinking_rows_bwd(dims, n_train, cell_mask, T, dX, dtable, accumulate, works
     cm, cmp_ = _host(cell_mask, np.uint8)
     rc = lib().tfm_thinking_rows_bwd(ctypes.byref(dims), ntp, cmp_, int(T), _ptr(dX),
                                      _ptr(dtable), int(bool(accumulate)), _ptr(workspace),
-                                     workspace.numel() * workspace.element_size(),
+                                     _nbytes(workspace),
                                      _stream(stream))
     _check(rc)
 
 
 def _nbytes(t):
-    return 0 if t is None else t.nbytes
+    """Bytes that the library may use from a buffer's first on."""
+    if t is None:
+        return 0
+    if not t.is_contiguous():
+        raise ValueError(f"a buffer of shape {tuple(t.shape)} and strides {t.stride()}: its elements "
+                         "have to lie side by side")
+    return t.nbytes
 
 
 def layer_fwd_context(dims, n_train, cell_mask, X, params, Y, kv_cache, workspace, stream=None):
