@@ -86,7 +86,9 @@ class InferStack:
     (train rows first) through every layer once and keeps one key/value cache per layer;
     `query` then runs any number of chunks of unlabelled rows through every layer against
     those caches.  For the pre-norm block, layer l multiplies its input by
-    decay_base ** (first_layer + l).  cache8: the caches hold 8 bits a value (tfm_cache.h)."""
+    decay_base ** (first_layer + l).  cache8: the caches hold 8 bits a value (tfm_cache.h), half the
+    bytes but for the last page of 64 rows of each column; `context` needs one layer's bfloat16 cache
+    beside them while it runs."""
 
     def __init__(self, dims, n_train, cell_mask, params, max_query_rows, device="cuda",
                  decay_base=0.95, first_layer=0, cache8=False):
@@ -109,9 +111,8 @@ class InferStack:
         if wb == 0 or cb == 0:
             raise tfm.TfmError(-1, tfm.last_error())
         if self.cache8:
-            # one bfloat16 cache for all layers' context calls; scratch by the query rows of a call,
-            # which may need more the fewer they are
-            self.kv = torch.empty(cb, dtype=torch.uint8, device=device)
+            # scratch by the query rows of a call, which may need more the fewer they are
+            self.kv_bytes = cb
             cb = tfm.infer_cache8_bytes(self.ctx_dims[0])
             wb = max([wb] + [tfm.infer8_workspace_bytes(self._copy(dims, r), self.Rc)
                              for r in range(1, self.Rq + 1)])
@@ -143,12 +144,13 @@ class InferStack:
     def context(self, X):
         """X: [B, Rc, C+1, E] bfloat16.  Returns the last layer's output (owned buffer)."""
         h = X
+        if self.cache8:  # one bfloat16 cache for all layers, during this call
+            kv = torch.empty(self.kv_bytes, dtype=torch.uint8, device=self.device)
         for l in range(self.L):
             out = self.ctx_out[l % 2]
             if self.cache8:
                 tfm.layer_fwd_context8(self.ctx_dims[l], self.n_train, self.cell_mask, h,
-                                       self.params[l], out, self.kv, self.caches[l],
-                                       self.workspace)
+                                       self.params[l], out, kv, self.caches[l], self.workspace)
             else:
                 tfm.layer_fwd_context(self.ctx_dims[l], self.n_train, self.cell_mask, h,
                                       self.params[l], out, self.caches[l], self.workspace)

@@ -174,3 +174,62 @@ def test_scales_of_huge_and_tiny_queries(d, page, L, size, scale, power, dtype):
     assert np.all(np.abs(out.double().cpu().numpy() - want) <= bound)
     lb = 2 * A + 8 * U * sabs + (n / 16 + 80) * U + 4 * U * np.abs(want_lse) + 2.0 ** -21
     assert np.all(np.abs(lse.double().cpu().numpy() - want_lse) <= lb)
+
+
+def _stack(w, Rc, n_train, cache8, chunk):
+    from paper_2606_03681_amd import tfm
+    from paper_2606_03681_amd.stack import InferStack
+    dims = tfm.make_dims(dtype=w.dtype, block=w.block, R=Rc,
+                         **{k: v for k, v in w.dims.items() if k not in ("dtype", "R")})
+    return dims, InferStack(dims, n_train, w.cell_mask, w.params[:1], max_query_rows=chunk,
+                            cache8=cache8)
+
+
+def test_a_stack_keeps_its_8_bit_caches_alone():
+    """What a stack of one layer holds after its context call: half the cache's bytes less, but for
+    rows up to a whole page (and torch's blocks of 2 MiB)."""
+    import torch
+    from paper_2606_03681_amd import tfm
+    from paper_2606_03681_amd.stack import to_device
+    w = wl.make_workload("ragged-small-bf16")
+    Rc, n_train = 1024, np.minimum(w.n_train, 1024).astype(np.int32)
+    X = to_device(np.resize(w.X, (w.X.shape[0], Rc) + w.X.shape[2:]), "bf16")
+    held = []
+    for cache8 in (False, True):
+        torch.cuda.synchronize()
+        before = torch.cuda.memory_allocated()
+        dims, st = _stack(w, Rc, n_train, cache8, 1)
+        st.context(X)
+        torch.cuda.synchronize()
+        # (the query call's scratch is another matter)
+        held.append(torch.cuda.memory_allocated() - before - st.workspace.numel())
+        del st
+    saved = tfm.infer_cache_bytes(dims) - tfm.infer_cache8_bytes(dims)
+    assert saved > 0.4 * tfm.infer_cache_bytes(dims)
+    assert held[1] <= held[0] - saved + 8 * 512, (held, saved)
+
+
+def test_context_and_query_replayed_from_a_graph():
+    """Captured with the scratch that the context call takes, eager work between the replays."""
+    import torch
+    from paper_2606_03681_amd.stack import to_device
+    w = wl.make_workload("d16-bf16")
+    R = w.cfg["R"]
+    Rc = R - (R // 3 + 5)
+    n_train = np.minimum(w.n_train, Rc).astype(np.int32)
+    _, eager = _stack(w, Rc, n_train, True, R - Rc)
+    _, st = _stack(w, Rc, n_train, True, R - Rc)
+    X, Xq = (to_device(np.ascontiguousarray(x), "bf16") for x in (w.X[:, :Rc], w.X[:, Rc:]))
+    x, xq = X.clone(), Xq.clone()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        c = st.context(x)
+        y = st.query(xq)
+    for by in (1.0, -0.5, 3.0, 1.0):
+        x.copy_(X * by)
+        xq.copy_(Xq * by)
+        graph.replay()
+        want = eager.context(X * by).clone(), eager.query(Xq * by).clone()
+        torch.cuda.synchronize()
+        assert torch.equal(c, want[0]) and torch.equal(y, want[1])
