@@ -93,17 +93,14 @@ def append(keys, values, powers, k, v, max_pages, pages=None, lens=None, n_new=N
 
 def rows_of(keys, values, powers, max_pages, pages, b, length, head):
     """Keys, values [n, d] of one sequence and head, and which of the rows are there."""
-    n_pages, _, page, d = keys.shape
-    K, V, here = np.zeros((length, d)), np.zeros((length, d)), np.zeros(length, bool)
-    for j in range(length):
-        entry, slot = divmod(j, page)
-        p = page_of(pages, max_pages, n_pages, b, entry)
-        if p is None:
-            continue
-        here[j] = True
-        two = 2.0 ** (clamp_power(powers[p, head]) - 127)
-        K[j] = decode(keys[p, head, slot]) * two[0]
-        V[j] = decode(values[p, head, :, slot]) * two[1]
+    n_pages, page = keys.shape[0], keys.shape[2]
+    entry, slot = np.divmod(np.arange(length), page)
+    p = b * max_pages + entry if pages is None else np.asarray(pages)[b, entry].astype(np.int64)
+    here = (p >= 0) & (p < n_pages)
+    p = np.where(here, p, 0)
+    two = np.where(here[:, None], 2.0 ** (clamp_power(powers[p, head]) - 127), 0.0)
+    K = np.where(here[:, None], decode(keys[p, head, slot]) * two[:, :1], 0.0)
+    V = np.where(here[:, None], decode(values[p, head, :, slot]) * two[:, 1:], 0.0)
     return K, V, here
 
 
