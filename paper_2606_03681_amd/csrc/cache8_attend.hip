@@ -11,19 +11,19 @@
 //                   largest power that the wave's columns have seen so far
 //
 // The weights' sum is of the unrounded ones, in float32 (as one more product, 1 P^T, it would cost fewer
-// cycles, but the rounded weights put lse off by up to 2^-12).
+// cycles, but the rounded weights put lse off by up to 2^-11).
 // Row m of the t-th of the tile's four 16-row products is key 16 (m / 4) + 4 t + m % 4, so that a lane's
 // 16 scores are those of 16 keys in a row: one block's, since pages are multiples of 16, and in the
 // order in which the lane reads 16 bytes of V^T.  Nothing moves between lanes, and codes go from memory
 // to registers without LDS (but see staged()).
 //
-// p is held as half with 2^8 in front: 2^-12 of each weight, and 2^-33 of the largest where half has no
+// p is held as half with 2^8 in front: 2^-11 of each weight, and 2^-33 of the largest where half has no
 // more bits (bfloat16 would have doubled the output's own rounding error).  The reference is looked at
 // only where a lane's weights sum to more than half can hold, the first tile's among them, whose
 // reference is the lowest float: then it becomes its column's largest score, the column's sums are
 // rescaled and the tile weighed again.  With the largest score as reference 16 weights sum to at most 2^12, and a later one
 // may be up to 2^7 of it, so that this is rare, and other tiles need no maximum.  Values are held with
-// 2^7 in front: exact unless their block is 2^22 below the largest, 2^-41 of that one's largest code
+// 2^7 in front: exact unless their block is 2^22 below the largest, 2^-40 of that one's largest code
 // then.  Float32 queries are three bfloat16 parts (24 bits) and their weights two halves.
 //
 // Few columns (SPLIT): the four waves of a workgroup share the columns and take turns over the tiles;
