@@ -198,7 +198,7 @@ def allowed_bits(allowed):
 def adjust_classes(logits, n_class=None, bias=None, allowed=None, history=None, n_history=None,
                    repetition=None, presence=None, frequency=None):
     """tfm_adjust_logits in place on logits float32 [N, K] side by side: bias float32 and allowed
-    bool [K] or [N, K]; history int32 [N, n]; the rest of a value per row."""
+    bool [K] or [N, K]; history int32 [N, n], a part of longer rows too; the rest of a value per row."""
     N, K = logits.shape
     idx = words = None
     ld_bias = ld_allowed = 0
@@ -209,8 +209,10 @@ def adjust_classes(logits, n_class=None, bias=None, allowed=None, history=None, 
     if allowed is not None:
         words = allowed_bits(allowed)
         ld_allowed = words.shape[-1] if allowed.dim() == 2 else 0
-    a = tfm.make_adjust(N, K, K, tfm.TFM_F32, 0 if history is None else history.shape[1],
-                        0 if bias is None else K, ld_bias=ld_bias, ld_allowed=ld_allowed)
+    n_hist = 0 if history is None else history.shape[1]
+    a = tfm.make_adjust(N, K, K, tfm.TFM_F32, n_hist, 0 if bias is None else K,
+                        ld_history=history.stride(0) if n_hist and N > 1 else n_hist,
+                        ld_bias=ld_bias, ld_allowed=ld_allowed)
     tfm.adjust_logits(a, logits, n_class, history, n_history, repetition, presence, frequency, idx,
                       bias, words, logits)
 
