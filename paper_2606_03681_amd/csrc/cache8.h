@@ -9,6 +9,14 @@ constexpr int CACHE8_E_MIN = 79, CACHE8_E_MAX = 175;  // bytes of a block's powe
 constexpr float CACHE8_TOP = 448.0f;                  // largest e4m3 value
 constexpr uint8_t CACHE8_NAN = 0x7f;
 
+// A power's byte as it counts.
+__device__ __forceinline__ int power_byte(uint32_t e) {
+  return min(max((int)e, CACHE8_E_MIN), CACHE8_E_MAX);
+}
+__device__ __forceinline__ float two_to(int e) {  // 2^e, e in [-126, 127]
+  return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
 // A pool and the page table of a batch of sequences.
 struct Cache8Geo {
   int32_t heads, d, page, shift;  // page = 1 << shift
@@ -58,7 +66,7 @@ struct Cache8Attend {
   Cache8Geo g;
   int32_t B, L, heads, causal;
   int32_t max_rows;          // of a sequence: the table's room, or less by the caller's word
-  int32_t plan_B, plan_rows; // B and max_rows by which the work is cut (not less than these two)
+  int32_t plan_B;            // B by which the work is cut (not less than B)
   float scale_log2;          // the scores' factor, with log2(e)
   int64_t sq[3], so[3];
   const int32_t *lens, *n_rows;  // n_rows nullable

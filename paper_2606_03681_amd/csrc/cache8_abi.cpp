@@ -97,12 +97,6 @@ double reach_of(const int64_t* stride, int32_t a, int32_t b, int32_t c) {
   return (double)(a - 1) * (double)stride[0] + (double)(b - 1) * (double)stride[1] +
          (double)(c - 1) * (double)stride[2];
 }
-// Whether [p, p + bytes) and [q, q + more) share memory.
-bool overlap(const void* p, double bytes, const void* q, double more) {
-  return p && q && (double)(uintptr_t)p < (double)(uintptr_t)q + more &&
-         (double)(uintptr_t)q < (double)(uintptr_t)p + bytes;
-}
-
 tfm::Cache8Geo geo_of(const tfm_cache8* c, void* pool, int32_t max_pages, const int32_t* pages) {
   return tfm::cache8_geo(c->heads, c->d, c->page, c->n_pages, pool, max_pages, pages);
 }
@@ -151,7 +145,7 @@ int query_check(const tfm_cache8* c, const tfm_cache8_query* a, tfm::Cache8Atten
   t.B = a->B; t.L = a->L; t.heads = a->heads; t.causal = a->causal != 0;
   const int64_t room = (int64_t)a->max_pages * c->page;
   t.max_rows = (int32_t)(a->max_len > 0 && a->max_len < room ? a->max_len : room);
-  t.plan_B = t.B; t.plan_rows = t.max_rows;
+  t.plan_B = t.B;
   t.scale_log2 = (float)(a->scale * 1.4426950408889634);
   for (int i = 0; i < 3; ++i) t.sq[i] = a->stride_q[i], t.so[i] = a->stride_out[i];
   return TFM_OK;
@@ -176,8 +170,8 @@ int tfm_cache8_append(const tfm_cache8* c, const tfm_cache8_rows* r, const void*
     return fail(TFM_ERR_POINTER, "k and v must be non-null and aligned to their elements");
   if (!aligned_or_null(pages, 4) || !aligned_or_null(lens, 4) || !aligned_or_null(n_new, 4))
     return fail(TFM_ERR_POINTER, "pages, lens and n_new must be 4-byte aligned");
-  if (overlap(k, (reach_of(r->stride_k, r->B, r->L, c->heads) + c->d) * es, pool, (double)pool_size(c)) ||
-      overlap(v, (reach_of(r->stride_v, r->B, r->L, c->heads) + c->d) * es, pool, (double)pool_size(c)))
+  if (tfm::overlap(k, (reach_of(r->stride_k, r->B, r->L, c->heads) + c->d) * es, pool, (double)pool_size(c)) ||
+      tfm::overlap(v, (reach_of(r->stride_v, r->B, r->L, c->heads) + c->d) * es, pool, (double)pool_size(c)))
     return fail(TFM_ERR_POINTER, "k or v overlaps the pool");
   hipStream_t st = (hipStream_t)stream;
   tfm::Cache8Append a;
@@ -216,9 +210,9 @@ int tfm_cache8_attend(const tfm_cache8* c, const tfm_cache8_query* a, const void
   const double span = (reach_of(a->stride_out, a->B, a->L, a->heads) + c->d) * es;
   if (q == out && !std::equal(a->stride_q, a->stride_q + 3, a->stride_out))
     return fail(TFM_ERR_POINTER, "out is q, with other strides");
-  if (overlap(out, span, pool, (double)pool_size(c)) ||
-      overlap(out, span, lse, 4.0 * a->B * a->L * a->heads) ||
-      overlap(lse, 4.0 * a->B * a->L * a->heads, pool, (double)pool_size(c)))
+  if (tfm::overlap(out, span, pool, (double)pool_size(c)) ||
+      tfm::overlap(out, span, lse, 4.0 * a->B * a->L * a->heads) ||
+      tfm::overlap(lse, 4.0 * a->B * a->L * a->heads, pool, (double)pool_size(c)))
     return fail(TFM_ERR_POINTER, "one of out, the pool and lse overlaps another");
   const size_t need = tfm::cache8_attend_bytes(t, a->dtype == TFM_F32);
   if (need && !aligned(workspace, 16))

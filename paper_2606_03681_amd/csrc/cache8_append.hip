@@ -28,12 +28,6 @@ __device__ __forceinline__ int power_of(float m) {
   const int e = (int)(u >> 23) - 8 + ((u & 0x7fffffu) > 0x600000u);
   return min(max(e, CACHE8_E_MIN), CACHE8_E_MAX);
 }
-__device__ __forceinline__ int power_byte(uint32_t e) {
-  return min(max((int)e, CACHE8_E_MIN), CACHE8_E_MAX);
-}
-__device__ __forceinline__ float two_to(int e) {  // 2^e, -126 <= e <= 127
-  return __uint_as_float((uint32_t)(e + 127) << 23);
-}
 __device__ __forceinline__ bool fits(float x) { return fabsf(x) <= 0x1.cp56f; }  // 448 2^48
 
 // Four codes of x f, NaN where x does not fit.

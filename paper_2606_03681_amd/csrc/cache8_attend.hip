@@ -53,13 +53,6 @@ constexpr int P_BIAS = 8, V_BIAS = 7;  // weights and values are held times 2 to
 constexpr float P_MOST = 61440.f;       // a lane's 16 weights may sum to this, and half holds each
 constexpr int V_GAP = 20;               // powers of two by which blocks of a product may differ
 
-__device__ __forceinline__ float exp2i(int e) {  // 2^e, e in [-126, 127]
-  return __uint_as_float((uint32_t)(e + 127) << 23);
-}
-__device__ __forceinline__ int power_byte(uint32_t e) {
-  return min(max((int)e, CACHE8_E_MIN), CACHE8_E_MAX);
-}
-
 // 8 codes (two dwords) as bfloat16 and, times a power of two, as half.
 __device__ __forceinline__ bf16x8 codes_bf16(uint32_t lo, uint32_t hi) {
   const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
@@ -266,15 +259,9 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   // the pages of the keys 16 (c / 4) .. and 16 lg .. of a tile (UNI: one page, the same in every lane)
   const int gk = UNI ? 0 : c >> 2, gv = UNI ? 0 : lg;
   auto look = [&](int t0) {  // before pid_of of tile t0
-    const int e = t0 >> shift;
-    if (e - ebase < 64) return;
-    if (e - ebase < 128) {
-      ebase += 64;
-      near = far;
-    } else {
-      ebase = e & ~63;
-      near = entries(ebase);
-    }
+    if ((t0 >> shift) - ebase < 64) return;  // (a step is 16 entries at most)
+    ebase += 64;
+    near = far;
     far = entries(ebase + 64);
   };
   auto pid_of = [&](int t0, int grp) {
@@ -434,7 +421,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
     const bool here = x.here && (UNI || only < 0 || lg == only);
     // (not 0, by which a masked score, -inf, could not be multiplied; a score of queries below 2^112 is
     // below 2^128 before it, so that the least factor adds at most 2^-21 to an exponent)
-    const float cs = fmaxf(scale * exp2i(ek - 127), 0x1p-149f);
+    const float cs = fmaxf(scale * two_to(ek - 127), 0x1p-149f);
     const bool partial = t0 + KT > lo || __any(!here);
     int top = ev;
     bool dirty = false;  // a staged tile has NaN codes that its readers leave out
@@ -509,7 +496,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
         now = __builtin_amdgcn_readfirstlane(max(now, __shfl_xor(now, 32, 64)));
       }
       if (now > unit) {
-        const float f = exp2i(unit - now);
+        const float f = two_to(unit - now);
 #pragma unroll
         for (int db = 0; db < DB; ++db)
 #pragma unroll
@@ -517,7 +504,7 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
         unit = now;
       }
       // (a block that no column sees: any power will do)
-      return exp2i(min(ev - unit, 0) + V_BIAS);
+      return two_to(min(ev - unit, 0) + V_BIAS);
     };
     auto value_frag = [&](const uint4& u, int kc, float two) {
       return kc ? codes_f16(u.z, u.w, two) : codes_f16(u.x, u.y, two);
@@ -706,8 +693,8 @@ __global__ __launch_bounds__(256, (waves<D, sizeof(T) == 4, QB, SPLIT>())) void 
   // the sums in units of 1, over all lanes of a column
 #pragma unroll
   for (int qb = 0; qb < QB; ++qb) {
-    const float one = exp2i(unit - 127 - V_BIAS - P_BIAS);
-    lsum[qb] = rows4_sum(lsum[qb]) * exp2i(-P_BIAS);
+    const float one = two_to(unit - 127 - V_BIAS - P_BIAS);
+    lsum[qb] = rows4_sum(lsum[qb]) * two_to(-P_BIAS);
 #pragma unroll
     for (int db = 0; db < DB; ++db) oacc[db][qb] *= one;
   }
@@ -880,7 +867,7 @@ struct Cut {
 Cut cut_of(const Cache8Attend& a, bool f32) {
   Cut c;
   const int64_t cols = (int64_t)a.L * (a.heads / a.g.heads), probs = (int64_t)a.plan_B * a.g.heads;
-  const int64_t keys = a.plan_rows;
+  const int64_t keys = a.max_rows;
   c.split = cols <= 32;
   // (Columns of a wave: as many as its registers hold.  d = 128, 16 heads on 4, 4 sequences of up to
   // 1000 rows: 288 us with 32, spilled or one wave a SIMD, 207 with 16 and two.)

@@ -80,6 +80,12 @@ hipError_t launch_sgemm(const SgemmArgs& a, bool ta, bool tb, int epi, hipStream
 // p[i] = v for i in [0, n) (a kernel, so that the call can sit in a captured graph).
 hipError_t launch_fill_f32(float* p, int64_t n, float v, hipStream_t s);
 
+// Whether [p, p + bytes) and [q, q + more) share memory (null: they do not).
+inline bool overlap(const void* p, double bytes, const void* q, double more) {
+  return p && q && (double)(uintptr_t)p < (double)(uintptr_t)q + more &&
+         (double)(uintptr_t)q < (double)(uintptr_t)p + bytes;
+}
+
 // Shared with the C-ABI source of the layer: set the thread's last error (returns code), and
 // validate a tfm_dims as every layer entry point does (0 or a negative code).
 int abi_fail(int code, const char* msg);

@@ -1167,7 +1167,7 @@ tfm::Cache8Attend layer_attend8(const Dims& d, const Dims& dc, void* pool) {
   tfm::Cache8Attend a{};
   a.g = layer_cache8(dc, pool);
   a.plan_B = d.B * d.S;  // by which the scratch is sized, whatever columns are active
-  a.plan_rows = a.max_rows = dc.R;
+  a.max_rows = dc.R;
   a.L = d.R; a.heads = d.heads;
   a.scale_log2 = 1.0f;
   a.sq[0] = (int64_t)d.heads * d.R * d.d; a.sq[1] = d.d; a.sq[2] = (int64_t)d.R * d.d;

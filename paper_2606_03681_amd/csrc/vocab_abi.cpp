@@ -157,12 +157,6 @@ int adjust_check(const tfm_adjust* a) {
   return rc;
 }
 
-// Whether [p, p + bytes) and [q, q + more) share memory.
-bool overlap(const void* p, double bytes, const void* q, double more) {
-  return p && q && (double)(uintptr_t)p < (double)(uintptr_t)q + more &&
-         (double)(uintptr_t)q < (double)(uintptr_t)p + bytes;
-}
-
 }  // namespace
 
 extern "C" {
@@ -300,7 +294,7 @@ int tfm_adjust_logits(const tfm_adjust* a, const void* logits, const int32_t* n_
     return fail(TFM_ERR_POINTER, "n_class, n_history, repetition, presence, frequency and allowed "
                                  "must be 4-byte aligned");
   const double last = a->N - 1, wide = (last * a->ld + a->V) * es, room = (last * a->ld_out + a->V) * es;
-  if (!(logits == out && a->ld == a->ld_out) && overlap(logits, wide, out, room))
+  if (!(logits == out && a->ld == a->ld_out) && tfm::overlap(logits, wide, out, room))
     return fail(TFM_ERR_POINTER, "out overlaps logits without being logits, rows as far apart");
   struct { const char* name; const void* p; double bytes; } others[] = {
       {"n_class", n_class, 4. * a->N}, {"n_history", n_history, 4. * a->N},
@@ -311,7 +305,7 @@ int tfm_adjust_logits(const tfm_adjust* a, const void* logits, const int32_t* n_
       {"bias", a->n_bias ? bias : nullptr, 4. * (last * a->ld_bias + a->n_bias)},
       {"allowed", allowed, 4. * (last * a->ld_allowed + (a->V + 31) / 32)}};
   for (const auto& o : others)
-    if (overlap(o.p, o.bytes, out, room)) return fail(TFM_ERR_POINTER, "out overlaps %s", o.name);
+    if (tfm::overlap(o.p, o.bytes, out, room)) return fail(TFM_ERR_POINTER, "out overlaps %s", o.name);
   hipStream_t st = (hipStream_t)stream;
   tfm::AdjustGeo g;
   g.N = a->N; g.ld = a->ld; g.ld_out = a->ld_out;
