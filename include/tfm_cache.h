@@ -81,8 +81,8 @@ int tfm_cache8_append(const tfm_cache8* c, const tfm_cache8_rows* r, const void*
  * to [0, max_pages page], n_rows to [0, L].  max_len is a promise that no sequence is longer: it
  * chooses how the rows of a cache are split over workgroups.
  *
- * Scores, statistics and sums are held in float32, as is scale log2(e).  Codes are exact as bfloat16 (keys) and half
- * (values of blocks less than 2^22 below the row's largest); a float32 query goes in three bfloat16
+ * Scores, statistics and sums are held in float32, as is scale log2(e).  Codes are exact as bfloat16
+ * (keys) and half (values of blocks less than 2^22 below the row's largest); a float32 query goes in three bfloat16
  * parts whose sum it is (subnormal ones may be lost).  Weights are rounded to half (by 2^-11 of each, or
  * 2^-33 of the row's largest where that is more), with a float32 output to two halves (2^-23).
  *
@@ -118,7 +118,8 @@ int tfm_cache8_attend(const tfm_cache8* c, const tfm_cache8_query* a, const void
  *       and the context alone, up to the order of sums, which goes by dims and context_rows.
  *
  * cache8 (tfm_infer_cache8_bytes of the context's dims, opaque layout) is a pool of pages of 64 rows
- * with a power of two for each page and head: half the bfloat16 cache's bytes, three bits of fraction.
+ * with a power of two for each page and head: half the bfloat16 cache's bytes, but for a column's last
+ * page, and three bits of fraction.
  * Limits and conditions are those of the two calls; tfm_infer8_workspace_bytes is the scratch of
  * query8 (dims->R: the query rows), tfm_infer_workspace_bytes that of context8. */
 size_t tfm_infer_cache8_bytes(const tfm_dims* dims);

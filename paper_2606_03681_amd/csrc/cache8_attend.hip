@@ -21,9 +21,9 @@
 // more bits (bfloat16 would have doubled the output's own rounding error).  The reference is looked at
 // only where a lane's weights sum to more than half can hold, the first tile's among them, whose
 // reference is the lowest float: then it becomes its column's largest score, the column's sums are
-// rescaled and the tile weighed again.  With the largest score as reference 16 weights sum to at most 2^12, and a later one
-// may be up to 2^7 of it, so that this is rare, and other tiles need no maximum.  Values are held with
-// 2^7 in front: exact unless their block is 2^22 below the largest, 2^-40 of that one's largest code
+// rescaled and the tile weighed again.  With the largest score as reference 16 weights sum to at most
+// 2^12, and a later one may be up to 2^7 of it, so that this is rare, and other tiles need no maximum.
+// Values are held with 2^7 in front: exact unless their block is 2^22 below the largest, 2^-40 of that one's largest code
 // then.  Float32 queries are three bfloat16 parts (24 bits) and their weights two halves.
 //
 // Few columns (SPLIT): the four waves of a workgroup share the columns and take turns over the tiles;
@@ -32,10 +32,12 @@
 // of them, and a second launch joins their sums.
 //
 // Bounds and figures.  Few columns: the codes' bytes; 64 sequences of 1 to 16,384 rows, one row of 32
-// heads on 8, d = 128: 207 us, 5.2 TB/s.  Many columns: vector instructions, 445 of a wave and tile at
+// heads on 8, d = 128: 207 us, 5.2 TB/s.  Many columns: vector instructions, 436 of a wave and tile at
 // d = 32 and 64 columns (64 exponentials at two issue slots each, scores to weights, codes to
 // bfloat16 and half), 32 matrix instructions beside them; 1616 sequences of 768 rows, 256 rows of 6
-// heads, d = 32: 445 us, 550 TFLOP/s, the vector units 83 to 95 % busy.
+// heads, d = 32: 439 us, 560 TFLOP/s, the vector units 83 to 96 % busy.  (Of the 436, 64 are the sum
+// and 64 the scores' factor and reference: attn_item.hip, which sums on the matrix cores and starts its
+// accumulators at the reference, needs neither and is the faster on bfloat16 keys.)
 #include <float.h>
 
 #include "cache8.h"
@@ -117,12 +119,14 @@ struct Values {
 
 // Whether tiles go through LDS, for all four waves: where registers hold no tile beside 32 columns' sums.
 // Many columns at d = 128, bf16, pages of 64 and more (8 sequences of 1000 rows, 2000 keys, 16 heads):
-// 349 us with 16 columns and the tile in registers, 238 us staged with 32 (keys in two pieces); at d = 64 the tile in
-// registers is the faster one (122 us, 139 us staged), as with pages under 64 (218 us, 246 us).
+// 349 us with 16 columns and the tile in registers, 190 us staged with 32.  With keys in two pieces, the
+// tile in registers was the faster one at d = 64 (122 us, 139 us staged; now, in one piece, 107), as with
+// pages under 64 (218 us, 246 us).
 template <int D, bool F32, int QB, bool SPLIT>
 constexpr bool staged() { return !SPLIT && D == 128 && !F32 && QB == 2; }
 // Waves per SIMD that the registers of a kernel leave room for.  (Three at D <= 32: 476 us for the 1616
-// sequences above with two, 442 with three, queries in LDS for it.)
+// sequences above with two, 442 with three, queries in LDS for it; with pages under 64 two registers do
+// not fit and go through scratch.)
 template <int D, bool F32, int QB, bool SPLIT>
 constexpr int waves() { return D <= 32 && QB == 4 ? 3 : D == 128 && QB == 2 && SPLIT ? 1 : 2; }
 
@@ -870,7 +874,9 @@ Cut cut_of(const Cache8Attend& a, bool f32) {
   const int64_t keys = a.max_rows;
   c.split = cols <= 32;
   // (Columns of a wave: as many as its registers hold.  d = 128, 16 heads on 4, 4 sequences of up to
-  // 1000 rows: 288 us with 32, spilled or one wave a SIMD, 207 with 16 and two.)
+  // 1000 rows: 288 us with 32, spilled or one wave a SIMD, 207 with 16 and two.  From 33 columns on
+  // every wave has its own, and waves without any wait: one head of one sequence on 16,000 keys, 16 / 32
+  // / 33 / 64 / 128 columns: 10 / 11 / 29 / 29 / 30 us at d = 32, 12 / 14 / 25 / 30 / 30 at d = 128.)
   c.qb = c.split ? (cols <= 16 ? 1 : 2) : f32 ? 1 : a.g.d <= 32 ? 4 : 2;
   if (!c.split && c.qb == 2 && a.g.d == 128) {
     // Staged tiles, whose workgroups take 128 columns instead of 64, need one for every CU: 8 heads,
