@@ -82,9 +82,10 @@ int tfm_cache8_append(const tfm_cache8* c, const tfm_cache8_rows* r, const void*
  * chooses how the rows of a cache are split over workgroups.
  *
  * Scores, statistics and sums are held in float32, as is scale log2(e).  Codes are exact as bfloat16
- * (keys) and half (values of blocks less than 2^22 below the row's largest); a float32 query goes in three bfloat16
- * parts whose sum it is (subnormal ones may be lost).  Weights are rounded to half (by 2^-11 of each, or
- * 2^-33 of the row's largest where that is more), with a float32 output to two halves (2^-23).
+ * (keys) and half (values of blocks less than 2^22 below the row's largest); a float32 query goes in
+ * three bfloat16 parts whose sum it is (subnormal ones may be lost).  Weights are rounded to half (by
+ * 2^-11 of each, or 2^-33 of the row's largest where that is more), with a float32 output to two halves
+ * (2^-23).
  *
  * Rows of q and out (dtype both) lie by their strides as above; out's rows must not overlap.  out may
  * be q itself (with equal strides: in place); it shares no element with q otherwise, and none with

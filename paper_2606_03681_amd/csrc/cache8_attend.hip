@@ -23,8 +23,9 @@
 // reference is the lowest float: then it becomes its column's largest score, the column's sums are
 // rescaled and the tile weighed again.  With the largest score as reference 16 weights sum to at most
 // 2^12, and a later one may be up to 2^7 of it, so that this is rare, and other tiles need no maximum.
-// Values are held with 2^7 in front: exact unless their block is 2^22 below the largest, 2^-40 of that one's largest code
-// then.  Float32 queries are three bfloat16 parts (24 bits) and their weights two halves.
+// Values are held with 2^7 in front: exact unless their block is 2^22 below the largest, 2^-40 of that
+// one's largest code then.  Float32 queries are three bfloat16 parts (24 bits) and their weights two
+// halves.
 //
 // Few columns (SPLIT): the four waves of a workgroup share the columns and take turns over the tiles;
 // many: each wave has columns of its own.  A tile's keys are read while the one before it is weighed
