@@ -132,12 +132,12 @@ int tfm_distill_loss(const tfm_distill* d, const void* logits, const int32_t* to
  *   x = -inf where v >= n_class[n]
  *
  * in float32, each step rounded once, and a bfloat16 output once more; penalties over different
- * histories take a call for each.  Entries of history and bias_idx outside [0, V) are absent; n_history is cut to [0, n_hist].  A NaN logit that is allowed
- * stays one.  Rows of logits, out, history (n_hist entries), bias_idx and bias (n_bias entries each)
- * and allowed (ceil(V / 32) words) lie ld elements of their own apart; ld_history, ld_bias and
- * ld_allowed may be 0, one row for all.  out may be logits itself (with ld_out == ld: in place) but
- * must not overlap it otherwise, nor anything else that the call reads; the elements between rows are
- * left as they were.
+ * histories take a call for each.  Entries of history and bias_idx outside [0, V) are absent;
+ * n_history is cut to [0, n_hist].  A NaN logit that is allowed stays one.  Rows of logits, out,
+ * history (n_hist entries), bias_idx and bias (n_bias entries each) and allowed (ceil(V / 32) words)
+ * lie ld elements of their own apart; ld_history, ld_bias and ld_allowed may be 0, one row for all.
+ * out may be logits itself (with ld_out == ld: in place) but must not overlap it otherwise, nor
+ * anything else that the call reads; the elements between rows are left as they were.
  * Limits: N, V, ld, ld_out as for tfm_sample; 0 <= n_hist, n_bias <= 2^27; ld_history, ld_bias and
  * ld_allowed 0 or at least a row, at most 2^40, and the last row at most 2^48 elements from the first. */
 typedef struct {
